@@ -361,6 +361,184 @@ ff_status ff_set_timing(ff_handle h, int enable);
 ff_status ff_kernel_timing(ff_handle h, int kernel, int64_t* launches, double* total_ms,
                            double* alg_flop);
 
+/* ---------------------------------------------------------------------------
+ * Operators around one layer: what makes its tokens, runs it (in bf16 or from
+ * the quantiser's codes) and steps its weights.
+ *
+ * They keep no state: a call takes everything in its argument block, enqueues
+ * its work on `stream` and returns without waiting.  Nothing is allocated;
+ * workspaces are the caller's (256-byte aligned, contents undefined before and
+ * after, free again once the enqueued work has run).  Rows are contiguous,
+ * `ld` elements apart (ld >= the row's length), from a pointer aligned to one
+ * element; 16-byte aligned rows of whole 16-byte pieces are the fast form.
+ * Where not said otherwise outputs must not overlap inputs or each other.  A
+ * count of rows, tokens or matrices may be 0 (nothing is done), every other
+ * size is >= 1.  A zeroed argument block with the required fields set is valid.
+ * Sums are fp32 or, of 8-bit integers, exact; each output is rounded once, to
+ * nearest even.  The same call gives the same bits.
+ */
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *     s = x + residual
+ *     y_j = s_j / sqrt(mean_j s_j^2 + eps) * weight_j
+ * and either y, or y in 8 bits for a layer whose weights are the quantiser's
+ * codes (V = beta alpha^T (.) Z: col_scale = alpha, and the layer's product is
+ * scale_t beta_i sum_j q_tj Z_ij):
+ *     h_j = y_j col_scale_j,  scale = max_j |h_j| / 127,  q_j = rint(h_j / scale).
+ * A row of h that is not finite gets a NaN scale and zero codes; one whose largest
+ * magnitude is below 2^-118 a zero scale and zero codes.  normalise = 0 leaves the division
+ * by the root mean square out (codes of any rows; eps is not used).  sum may be
+ * x or residual themselves (the same rows and ld), and so may y. */
+typedef struct {
+  int64_t rows, cols;       /* cols <= 2^24 */
+  ff_dtype dtype;           /* x, residual, weight, sum and y */
+  const void* x;
+  int64_t ldx;
+  const void* residual;     /* or NULL */
+  int64_t ldr;
+  const void* weight;       /* cols; NULL = ones */
+  double eps;               /* >= 0 */
+  int normalise;            /* 1, or 0 (see above) */
+  void* sum;                /* receives s; or NULL */
+  int64_t ldsum;
+  void* y;                  /* receives y; NULL with q */
+  int64_t ldy;
+  const float* col_scale;   /* q only: cols; NULL = ones */
+  int8_t* q;                /* receives the codes; NULL with y */
+  int64_t ldq;
+  float* q_scale;           /* q only: rows */
+  void* stream;
+} ff_norm_args;
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_HIP. */
+ff_status ff_rms_norm(const ff_norm_args* args);
+
+/* Gradient of the norm y of rows s (the sum above):
+ *     ds = d(loss)/ds through y, plus dsum (the gradient that reaches s by other ways);
+ *          it is the gradient of x and of the residual alike
+ *     dweight_j = sum over the rows of dy_j s_j / sqrt(mean s^2 + eps).
+ * ds may be dy, s or dsum themselves (the same rows and ld). */
+typedef struct {
+  int64_t rows, cols;       /* cols <= 2^24 */
+  ff_dtype dtype;
+  const void* s;
+  int64_t lds;
+  const void* dy;
+  int64_t lddy;
+  const void* dsum;         /* or NULL */
+  int64_t lddsum;
+  const void* weight;       /* or NULL */
+  double eps;
+  void* ds;
+  int64_t ldds;
+  void* dweight;            /* cols, dtype; or NULL */
+  void* workspace;          /* with dweight */
+  size_t workspace_bytes;
+  void* stream;
+} ff_norm_grad_args;
+/* Bytes of workspace (the pointers of args are not looked at, except whether
+ * dweight is NULL).  Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_rms_norm_backward_workspace_size(const ff_norm_grad_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP.  With no rows
+ * dweight is set to zeros. */
+ff_status ff_rms_norm_backward(const ff_norm_grad_args* args);
+
+/* FF_ACT_GELU is the tanh form z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3)),
+ * FF_ACT_SILU z sigmoid(z). */
+typedef enum { FF_ACT_NONE = 0, FF_ACT_RELU = 1, FF_ACT_GELU = 2, FF_ACT_SILU = 3 } ff_activation;
+
+/* A linear layer W (m x n) on `tokens` rows x:
+ *     z = x W^T + bias,  y = act(z) + residual            (ff_linear)
+ *     z_ti = x_scale_t row_scale_i sum_j x_tj W_ij + bias_i   (ff_linear_q8)
+ * ff_linear: x, W, bias, residual, y and preact are bf16.  ff_linear_q8: x and
+ * W are int8 (rows of ff_rms_norm, codes Z that fit 8 bits), the rest bf16.
+ * y may be the residual itself (the same rows and ld). */
+typedef struct {
+  int64_t tokens, n, m;     /* n, m <= 2^20, n <= 131072 for ff_linear_q8 */
+  const void* x;            /* tokens x n */
+  int64_t ldx;
+  const void* w;            /* m x n */
+  int64_t ldw;
+  const float* x_scale;     /* ff_linear_q8: tokens */
+  const float* row_scale;   /* ff_linear_q8: m (the quantiser's beta) */
+  const void* bias;         /* m; or NULL */
+  const void* residual;     /* tokens x m; or NULL */
+  int64_t ldr;
+  ff_activation activation;
+  void* y;                  /* tokens x m */
+  int64_t ldy;
+  void* preact;             /* receives z, tokens x m; or NULL */
+  int64_t ldz;
+  void* workspace;          /* may be NULL where its size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} ff_linear_args;
+/* Bytes of workspace of ff_linear (q8 = 0) or ff_linear_q8 (q8 = 1): copies of
+ * operands whose rows are not in the fast form, and partial sums where k is
+ * split.  Reads the sizes, ldx, ldw and the alignment of x and w.
+ * Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_linear_workspace_size(const ff_linear_args* args, int q8, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP. */
+ff_status ff_linear(const ff_linear_args* args);
+ff_status ff_linear_q8(const ff_linear_args* args);
+
+/* Gradient of ff_linear (the residual's is dy itself):
+ *     g = dy act'(preact)       dx = g W       dw = g^T x       db = sum over the tokens of g
+ * All bf16; g is rounded before it is used (it is an output of its own: the
+ * token gradients that ff_config.g takes). */
+typedef struct {
+  int64_t tokens, n, m;     /* n, m <= 2^20, tokens <= 2^21 */
+  const void* dy;           /* tokens x m */
+  int64_t lddy;
+  const void* x;            /* tokens x n; needed for dw */
+  int64_t ldx;
+  const void* w;            /* m x n; needed for dx */
+  int64_t ldw;
+  const void* preact;       /* tokens x m; needed with an activation */
+  int64_t ldz;
+  ff_activation activation;
+  void* g;                  /* tokens x m; NULL: not stored (FF_ACT_NONE: g is dy) */
+  int64_t ldg;
+  void* dx;                 /* tokens x n; or NULL */
+  int64_t lddx;
+  void* dw;                 /* m x n; or NULL */
+  int64_t lddw;
+  void* db;                 /* m; or NULL */
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+} ff_linear_grad_args;
+/* Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_linear_backward_workspace_size(const ff_linear_grad_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP.  With no tokens dw
+ * and db are set to zeros. */
+ff_status ff_linear_backward(const ff_linear_grad_args* args);
+
+/* Orthogonalisation of updates G (m x n) by `steps` Newton-Schulz products:
+ *     X = G / (||G||_F + eps);  A = X X^T, X <- a X + (b A + c A A) X;  out = scale X
+ * (the smaller of X X^T and X^T X, the same X).  Products and sums as in
+ * an fp32 computation for FF_F32; for FF_BF16 with operands rounded to fp16.
+ * The coefficients have to keep every singular value that starts in [0, 1]
+ * below 16 through the steps (checked).  out may not overlap G. */
+typedef struct {
+  int64_t batch, m, n;      /* batch <= 65535, m, n <= 2^20 */
+  ff_dtype dtype;           /* G and out */
+  const void* G;            /* batch x m x n */
+  int64_t ldg, stride_g;    /* elements from row to row, from matrix to matrix */
+  void* out;
+  int64_t ldo, stride_o;
+  int steps;                /* 1 .. 64 */
+  double a, b, c;
+  double eps;               /* >= 0 */
+  double scale;             /* finite */
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+} ff_ortho_args;
+/* Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_orthogonalize_workspace_size(const ff_ortho_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP. */
+ff_status ff_orthogonalize(const ff_ortho_args* args);
+
 /* Static description of a status code. */
 const char* ff_status_string(ff_status s);
 

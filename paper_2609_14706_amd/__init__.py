@@ -4,7 +4,9 @@ Estimates the Kronecker-factored Hessian A (x) B of a linear layer from
 gradient samples G_i with the flip-flop iteration (WaterKron and FlipFlop
 Hessian, Section 5), and quantises its weights with WaterKron (two-sided
 GPTQ with waterfilling scales, Section 3), entirely in the HIP library
-``libff.so`` whose C ABI is ``include/ff.h``.  This package is the thin
+``libff.so`` whose C ABI is ``include/ff.h``.  Around the layer are its
+operators (layer.py): the norm, the layer in bf16 or from the quantiser's codes, their
+gradients, the orthogonalisation of an update.  This package is the thin
 binding (ctypes + torch memory).
 """
 from .binding import (FF_APPLY, FF_APPLY_INV, FF_BF16, FF_ERR_HIP, FF_ERR_INVALID_ARG,
@@ -18,5 +20,8 @@ from .binding import (FF_APPLY, FF_APPLY_INV, FF_BF16, FF_ERR_HIP, FF_ERR_INVALI
                       ff_quantize_workspace_size, ff_set_timing, ff_status_string,
                       ff_whiten_split_state,
                       ff_workspace_size, header_functions, load_library, LIB_PATH)
+from .layer import (ACTIVATIONS, ff_linear_args, ff_linear_grad_args, ff_norm_args, ff_norm_grad_args,
+                    ff_ortho_args, linear, linear_backward, linear_q8, orthogonalize, quantize_rows,
+                    rms_norm, rms_norm_backward, rms_norm_q8)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -24,6 +24,7 @@
 #include <vector>
 
 #include "ff.h"
+#include "ff_error.hpp"
 #include "ff_forkjoin.hpp"
 #include "ff_kernels.hpp"
 
@@ -37,6 +38,20 @@ ff_status fail(ff_status s, const std::string& msg) {
   g_last_error = msg;
   return s;
 }
+}  // namespace
+
+namespace ff {
+ff_status report(ff_status s, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {  // no room for the message: the status says it
+    g_last_error.clear();
+  }
+  return s;
+}
+}  // namespace ff
+
+namespace {
 
 #define FF_HIP(call)                                                                     \
   do {                                                                                   \

@@ -1,0 +1,535 @@
+// Linear layers with bias, activation and residual in the product's epilogue:
+//   y_ti = act(s_t b_i sum_j x_tj w_ij + bias_i) + r_ti
+// for bf16 (s = b = 1) and for 8-bit rows and codes (V = beta alpha^T (.) Z
+// with alpha folded into the rows: s the rows' scales, b = beta), whose
+// integer sums are exact.
+//
+// Many tokens are bound by the matrix cores: 256 x 256 or 128 x 128 tiles
+// (ff_tile_nt.hpp), tiles that run together on an XCD sharing operand rows in
+// its L2, k split and joined by a second kernel where tiles are few.  Few
+// tokens (up to 64) are bound by reading w once: k_skinny gives every wave 16
+// output rows' share of k straight from memory to the matrix cores, with no
+// LDS between, and joins the waves' sums at the end.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "ff_layer_kernels.hpp"
+#include "ff_tile_nt.hpp"
+#include "ff_vec.hpp"
+
+namespace ff {
+namespace {
+
+// z sigmoid(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi): the tanh form of gelu.
+constexpr float kGelu = 1.5957691216057308f, kCube = 0.044715f;
+
+__device__ __forceinline__ float act_of(float z, int act) {
+  if (act == kActRelu) return z < 0.0f ? 0.0f : z;
+  if (act == kActSilu) return z / (1.0f + __expf(-z));
+  if (act == kActGelu) return z / (1.0f + __expf(-kGelu * (z + kCube * z * z * z)));
+  return z;
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+  if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+  if (act == kActSilu) {
+    const float p = 1.0f / (1.0f + __expf(-z));
+    return p * (1.0f + z * (1.0f - p));
+  }
+  if (act == kActGelu) {
+    const float p = 1.0f / (1.0f + __expf(-kGelu * (z + kCube * z * z * z)));
+    const float t = z * p * (1.0f - p);  // zero for large |z|, where z^2 may be infinite
+    return t == 0.0f ? p : p + t * kGelu * (1.0f + 3.0f * kCube * z * z);
+  }
+  return 1.0f;
+}
+
+// W consecutive outputs of row t from column i on (W = 1, 2, 4 or 8), `count` of
+// them inside the matrix.
+template <int W>
+__device__ __forceinline__ void finish(const LinearArgs& a, int64_t t, int64_t i, const float* acc, int count) {
+  if (count <= 0) return;
+  float z[W];
+  const float st = a.x_scale != nullptr ? a.x_scale[t] : 1.0f;
+  bf16_t r[W], b[W];
+  if (count >= W) {
+    if (a.residual != nullptr) __builtin_memcpy(r, a.residual + t * a.ldr + i, sizeof r);
+    if (a.bias != nullptr) __builtin_memcpy(b, a.bias + i, sizeof b);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      r[k] = b[k] = 0;
+      if (k < count) {
+        if (a.residual != nullptr) r[k] = a.residual[t * a.ldr + i + k];
+        if (a.bias != nullptr) b[k] = a.bias[i + k];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    z[k] = acc[k];
+    if (a.row_scale != nullptr) z[k] *= st * (k < count ? a.row_scale[i + k] : 0.0f);
+    if (a.bias != nullptr) z[k] += bf16_to_f32(b[k]);
+  }
+  bf16_t zo[W], y[W];
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    zo[k] = f32_to_bf16(z[k]);
+    float v = act_of(z[k], a.act);
+    if (a.residual != nullptr) v += bf16_to_f32(r[k]);
+    y[k] = f32_to_bf16(v);
+  }
+  if (count >= W) {
+    if (a.preact != nullptr) __builtin_memcpy(a.preact + t * a.ldz + i, zo, sizeof zo);
+    __builtin_memcpy(a.y + t * a.ldy + i, y, sizeof y);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+      if (k < count) {
+        if (a.preact != nullptr) a.preact[t * a.ldz + i + k] = zo[k];
+        a.y[t * a.ldy + i + k] = y[k];
+      }
+  }
+}
+
+// Tile `t` of mt x nt: strips of eight tile rows, in a strip column by column,
+// so that the 32 workgroups of an XCD read 8 + 4 operand tiles a k step.
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t mt, uint32_t nt, uint32_t& i, uint32_t& j) {
+  const uint32_t strip = t / (8 * nt), u = t - strip * 8 * nt;
+  const uint32_t r = min(8u, mt - strip * 8);
+  i = strip * 8 + u % r;
+  j = u / r;
+}
+
+// Scalar of a type's accumulator.
+template <class T> struct Scalar { typedef float type; };
+template <> struct Scalar<nt::I8> { typedef int32_t type; };
+
+// grid: tiles x splits.  P: null (one split), or splits x tokens x m sums.
+template <class T, int TI, int TJ>
+__global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(LinearArgs a, uint32_t mt,
+                                                                             uint32_t ntl, uint32_t splits,
+                                                                             typename Scalar<T>::type* P) {
+  typedef nt::Tile<T, TI, TJ> G;
+  __shared__ typename G::Ring sm;
+  const uint32_t tiles = mt * ntl;
+  const uint32_t w = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t z = w / tiles;
+  uint32_t ti, tj;
+  tile_at(w - z * tiles, mt, ntl, ti, tj);
+  const int64_t t0 = (int64_t)ti * G::BM, i0 = (int64_t)tj * G::BN;
+  const nt::Rows A{(const char*)a.x + t0 * a.ldx * T::kBytes, (int)min((int64_t)G::BM, a.tokens - t0),
+                   (uint32_t)(a.ldx * T::kBytes)};
+  const nt::Rows B{(const char*)a.w + i0 * a.ldw * T::kBytes, (int)min((int64_t)G::BN, a.m - i0),
+                   (uint32_t)(a.ldw * T::kBytes)};
+  const int kbytes = (int)(a.n * T::kBytes), pairs = (kbytes + nt::kPair - 1) / nt::kPair;
+  const int p0 = (int)((int64_t)pairs * z / splits), p1 = (int)((int64_t)pairs * (z + 1) / splits);
+  typename G::Acc acc;
+  G::zero(acc);
+  G::loop(
+      sm, A, B, p0, p1,
+      [&](int p, const char*& pa, const char*& pb) {
+        const int k = __builtin_amdgcn_readfirstlane(p) * nt::kPair;
+        pa = A.p + k;
+        pb = B.p + k;
+      },
+      [&](int p) { return kbytes - p * nt::kPair; }, acc);
+  // The sums go through LDS (each lane its own 16-byte slots: no barrier, no
+  // bank conflict) so that one short loop serves all of them: unrolled, the
+  // epilogue of a 256 x 256 tile is 32 copies long.
+  typedef typename Scalar<T>::type S;
+  typedef __attribute__((ext_vector_type(4))) S S4;
+  constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;  // tile rows a phase, pieces of a row
+  static_assert(TJ % 4 == 0 && sizeof(S4) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
+  S4* stage = reinterpret_cast<S4*>(&sm) + threadIdx.x;
+  const int64_t col = i0 + G::col_of();
+  const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
+#pragma unroll
+  for (int h = 0; h < TI / HI; ++h) {
+#pragma unroll
+    for (int i = 0; i < HI; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          S4 o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = acc[h * HI + i][4 * v + e][r];
+          stage[((i * 4 + r) * V + v) * nt::kThreads] = o;
+        }
+#pragma unroll 1
+    for (int q = 0; q < HI * 4; ++q) {
+      S v[TJ];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const S4 o = stage[(q * V + k) * nt::kThreads];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * k + e] = o[e];
+      }
+      const int64_t t = t0 + G::row_of(h * HI + (q >> 2), q & 3);
+      if (t >= a.tokens) continue;
+      if (P != nullptr) {
+        S* o = P + ((int64_t)z * a.tokens + t) * a.m + col;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+          if (j < count) o[j] = v[j];
+      } else {
+        float f[TJ];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) f[j] = (float)v[j];
+        finish<TJ>(a, t, col, f, count);
+      }
+    }
+  }
+}
+
+// Sum of the splits' partial sums, in their order, and the epilogue: four
+// outputs a thread.
+template <class S>
+__global__ __launch_bounds__(256) void k_join(LinearArgs a, const S* P, int splits) {
+  const int64_t per_row = (a.m + 3) / 4, total = a.tokens * per_row;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += (int64_t)gridDim.x * 256) {
+    const int64_t t = id / per_row, i = (id - t * per_row) * 4;
+    const int count = (int)min((int64_t)4, a.m - i);
+    S v[4] = {0, 0, 0, 0};
+    for (int z = 0; z < splits; ++z) {
+      const S* p = P + ((int64_t)z * a.tokens + t) * a.m + i;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < count) v[k] += p[k];
+    }
+    float f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = (float)v[k];
+    finish<4>(a, t, i, f, count);
+  }
+}
+
+// 16 bytes of a row at byte k of `bytes`; zeros beyond.
+template <int EB>
+__device__ __forceinline__ u32x4 row_bytes(const char* row, int k, int bytes) {
+  u32x4 v = {0, 0, 0, 0};
+  if (k + 16 <= bytes) {
+    __builtin_memcpy(&v, row + k, 16);
+  } else {
+    // the last, partial piece (whole elements)
+#pragma unroll
+    for (int e = 0; e < 16 / EB - 1; ++e)
+      if (k + e * EB < bytes) {
+        const uint32_t b = EB == 1 ? (uint32_t)(uint8_t)row[k + e] : (uint32_t)*(const uint16_t*)(row + k + e * EB);
+        v[e * EB / 4] |= b << (8 * (e * EB % 4));
+      }
+  }
+  return v;
+}
+
+// Few tokens.  One workgroup: 16 RW output rows; its waves take k in turn,
+// 128 bytes a step: lane l holds bytes 32 (l / 16) .. + 31 of the step of row
+// (token) l % 16, two matrix instructions' worth; which k a lane holds does not
+// matter as long as both operands agree.  Accumulator element r of lane l:
+// output row 4 (l / 16) + r, token l % 16.
+template <class T, int NT, int RW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_skinny(LinearArgs a) {
+  typedef typename Scalar<T>::type S;
+  __shared__ S sh[WAVES][RW * NT * 256];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t i0 = (int64_t)blockIdx.x * (16 * RW);
+  const int bytes = (int)(a.n * T::kBytes), steps = (bytes + 127) / 128;
+  const char* wr[RW];
+#pragma unroll
+  for (int r = 0; r < RW; ++r)  // rows beyond the matrix: its last one, not stored
+    wr[r] = (const char*)a.w + min(i0 + r * 16 + (lane & 15), a.m - 1) * a.ldw * T::kBytes;
+  const char* xr[NT];
+  bool live[NT];
+#pragma unroll
+  for (int q = 0; q < NT; ++q) {
+    const int64_t t = q * 16 + (lane & 15);
+    live[q] = t < a.tokens;
+    xr[q] = (const char*)a.x + (live[q] ? t : 0) * a.ldx * T::kBytes;
+  }
+  typename T::acc acc[RW][NT];
+#pragma unroll
+  for (int r = 0; r < RW; ++r)
+#pragma unroll
+    for (int q = 0; q < NT; ++q) acc[r][q] = typename T::acc{0, 0, 0, 0};
+  const int kl = 32 * (lane >> 4);
+  const int full = bytes / 128;
+  auto products = [&](const u32x4 (&wv)[RW][2], const u32x4 (&xv)[NT][2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < RW; ++r)
+#pragma unroll
+        for (int q = 0; q < NT; ++q) acc[r][q] = T::mfma(wv[r][h], xv[q][h], acc[r][q]);
+  };
+  // U steps' loads go out before their products
+  constexpr int U = RW + NT <= 2 ? 4 : RW + NT <= 5 ? 2 : 1;
+  auto steps_at = [&](int s, auto count) {
+    constexpr int C = decltype(count)::value;
+    u32x4 wv[C][RW][2], xv[C][NT][2];
+#pragma unroll
+    for (int u = 0; u < C; ++u) {
+      const int k = (s + u * WAVES) * 128 + kl;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int r = 0; r < RW; ++r) __builtin_memcpy(&wv[u][r][h], wr[r] + k + 16 * h, 16);
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+          xv[u][q][h] = u32x4{0, 0, 0, 0};
+          if (live[q]) __builtin_memcpy(&xv[u][q][h], xr[q] + k + 16 * h, 16);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < C; ++u) products(wv[u], xv[u]);
+  };
+  int s = wave;
+  for (; s + (U - 1) * WAVES < full; s += U * WAVES) steps_at(s, std::integral_constant<int, U>());
+  for (; s < full; s += WAVES) steps_at(s, std::integral_constant<int, 1>());
+  if (full < steps && full % WAVES == wave) {  // the last step: k ends inside it
+    u32x4 wv[RW][2], xv[NT][2];
+    const int k = full * 128 + kl;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int r = 0; r < RW; ++r) wv[r][h] = row_bytes<T::kBytes>(wr[r], k + 16 * h, bytes);
+#pragma unroll
+      for (int q = 0; q < NT; ++q)
+        xv[q][h] = live[q] ? row_bytes<T::kBytes>(xr[q], k + 16 * h, bytes) : u32x4{0, 0, 0, 0};
+    }
+    products(wv, xv);
+  }
+#pragma unroll
+  for (int r = 0; r < RW; ++r)
+#pragma unroll
+    for (int q = 0; q < NT; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)  // token-major: 16 RW consecutive outputs of a token
+        sh[wave][(q * 16 + (lane & 15)) * (16 * RW) + r * 16 + 4 * (lane >> 4) + e] = acc[r][q][e];
+  __syncthreads();
+  for (int o = threadIdx.x; o < RW * NT * 256; o += 64 * WAVES) {
+    const int64_t t = o / (16 * RW), i = i0 + o % (16 * RW);
+    if (t >= a.tokens || i >= a.m) continue;
+    S v = sh[0][o];
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) v += sh[k][o];
+    const float f = (float)v;
+    finish<1>(a, t, i, &f, 1);
+  }
+}
+
+template <int EB>
+__global__ __launch_bounds__(256) void k_pack_rows(const char* src, int64_t ld, int64_t rows, int64_t n, char* dst,
+                                                   int64_t ldd) {
+  const int64_t chunks = ldd * EB / 16, total = rows * chunks;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += (int64_t)gridDim.x * 256) {
+    const int64_t r = id / chunks, c = id - r * chunks;
+    const u32x4 v = row_bytes<EB>(src + r * ld * EB, (int)(c * 16), (int)(n * EB));
+    *reinterpret_cast<u32x4*>(dst + r * ldd * EB + c * 16) = v;
+  }
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void k_zero(E* dst, int64_t ld, int64_t rows, int64_t cols) {
+  const int64_t total = rows * cols;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += (int64_t)gridDim.x * 256)
+    dst[id / cols * ld + id % cols] = E(0);
+}
+
+// 64 x 64 elements through LDS (rows of 33 words: a transposed read of pairs
+// spreads over the banks); 256 threads, 16 elements each way a thread.
+struct __align__(16) Turn {
+  bf16_t e[64][66];
+};
+
+template <bool GRAD>
+__global__ __launch_bounds__(256) void k_turn(ActGradArgs a) {
+  __shared__ Turn sm;
+  __shared__ float sums[4][64];
+  const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = (tid >> 3) + 32 * h, c = (tid & 7) * 8;
+    const int64_t row = r0 + r, col = c0 + c;
+    const int count = row < a.rows ? (int)min((int64_t)8, max((int64_t)0, a.cols - col)) : 0;
+    Vec<bf16_t> v;
+    v.w = u32x4{0, 0, 0, 0};
+    if (count > 0) v = load_row(a.dy + row * a.lddy + col, count);
+    if (GRAD && a.z != nullptr && count > 0) {
+      const Vec<bf16_t> z = load_row(a.z + row * a.ldz + col, count);
+      float f[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = v.get(k) * act_slope(z.get(k), a.act);
+      v.set(f);
+    }
+    if (GRAD && a.g != nullptr && count > 0) store_row(a.g + row * a.ldg + col, v, count);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sm.e[r][c + k] = k < count ? v.bits(k) : (bf16_t)0;
+  }
+  __syncthreads();
+  if (GRAD && a.part != nullptr) {
+    const int c = tid & 63, g = tid >> 6;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += bf16_to_f32(sm.e[g * 16 + k][c]);
+    sums[g][c] = s;
+    __syncthreads();
+    if (g == 0 && c0 + c < a.cols)
+      a.part[(int64_t)blockIdx.y * a.cols + c0 + c] = s + sums[1][c] + sums[2][c] + sums[3][c];
+  }
+  if (a.gt == nullptr) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int c = (tid >> 3) + 32 * h, r = (tid & 7) * 8;
+    if (c0 + c >= a.cols || r0 + r >= a.ldgt) continue;
+    Vec<bf16_t> v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v.w[k] = (uint32_t)sm.e[r + 2 * k][c] | ((uint32_t)sm.e[r + 2 * k + 1][c] << 16);
+    store_row(a.gt + (c0 + c) * a.ldgt + r0 + r, v, 8);  // ldgt is a multiple of 8
+  }
+}
+
+template <class T, int TI, int TJ>
+hipError_t tiles(const LinearArgs& a, const LinearPlan& p, void* partial, hipStream_t s) {
+  typedef nt::Tile<T, TI, TJ> G;
+  const int64_t mt = (a.tokens + G::BM - 1) / G::BM, ntl = (a.m + G::BN - 1) / G::BN;
+  const int64_t wgs = mt * ntl * p.splits;
+  if (wgs > 0x7fffffff || (p.splits > 1 && partial == nullptr)) return hipErrorInvalidValue;
+  typedef typename Scalar<T>::type S;
+  hipLaunchKernelGGL((k_tile<T, TI, TJ>), dim3((uint32_t)wgs), dim3(nt::kThreads), 0, s, a, (uint32_t)mt,
+                     (uint32_t)ntl, (uint32_t)p.splits, p.splits > 1 ? (S*)partial : nullptr);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const int64_t blocks = std::min<int64_t>((a.tokens * ((a.m + 3) / 4) + 255) / 256, 4096);
+  hipLaunchKernelGGL(k_join<S>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (const S*)partial, p.splits);
+  return hipGetLastError();
+}
+
+template <class T, int NT, int RW>
+hipError_t skinny_waves(const LinearArgs& a, hipStream_t s) {
+  const int64_t groups = (a.m + 16 * RW - 1) / (16 * RW);
+  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t steps = (a.n * T::kBytes + 127) / 128;
+  // enough waves to keep memory busy (8 a compute unit), each with four steps
+  // or more
+  int waves = 4;
+  while (waves < 16 && groups * waves < 2048 && steps >= 8 * waves) waves *= 2;
+  const dim3 grid((uint32_t)groups);
+  if (waves == 4)
+    hipLaunchKernelGGL((k_skinny<T, NT, RW, 4>), grid, dim3(256), 0, s, a);
+  else if (waves == 8)
+    hipLaunchKernelGGL((k_skinny<T, NT, RW, 8>), grid, dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_skinny<T, NT, RW, 16>), grid, dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t linear_for(const LinearArgs& a, const LinearPlan& p, void* partial, hipStream_t s) {
+  if (p.skinny) {
+    if (a.tokens <= 16) return skinny_waves<T, 1, 1>(a, s);
+    if (a.tokens <= 32) return a.m >= 8192 ? skinny_waves<T, 2, 2>(a, s) : skinny_waves<T, 2, 1>(a, s);
+    return a.m >= 8192 ? skinny_waves<T, 4, 2>(a, s) : skinny_waves<T, 4, 1>(a, s);
+  }
+  if (p.ti == 8 && p.tj == 8) return tiles<T, 8, 8>(a, p, partial, s);
+  if (p.ti == 4 && p.tj == 4) return tiles<T, 4, 4>(a, p, partial, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
+  if (tokens <= 64) return {true, 0, 0, 1};
+  auto count = [&](int64_t b) { return ((tokens + b - 1) / b) * ((m + b - 1) / b); };
+  if (count(256) >= 192) return {false, 8, 8, 1};
+  const int64_t t = count(128), pairs = (n * elem_bytes + nt::kPair - 1) / nt::kPair;
+  // two workgroups of 128 x 128 tiles share a compute unit; k is split until
+  // there are 512, each with eight pairs of k or more
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / t, pairs / 8, 16}));
+  return {false, 4, 4, (int)splits};
+}
+
+size_t linear_partial_bytes(const LinearPlan& p, int64_t tokens, int64_t m) {
+  return p.splits > 1 ? (size_t)p.splits * (size_t)tokens * (size_t)m * 4 : 0;
+}
+
+bool tile_rows_ok(const void* p, int64_t ld, int64_t n, int elem_bytes) {
+  return (uintptr_t)p % 16 == 0 && ld * elem_bytes % 16 == 0 && n * elem_bytes % 16 == 0 &&
+         ld * elem_bytes <= nt::kMaxRowBytes;
+}
+
+int64_t packed_ld(int64_t n, int elem_bytes) {
+  const int64_t g = nt::kPair / elem_bytes;
+  return (n + g - 1) / g * g;
+}
+
+hipError_t launch_pack_rows(const void* src, int64_t ld, int64_t rows, int64_t n, int elem_bytes, void* dst,
+                            hipStream_t s) {
+  if (rows <= 0 || n <= 0 || n * elem_bytes > nt::kMaxRowBytes || (uintptr_t)dst % 16 != 0)
+    return hipErrorInvalidValue;
+  const int64_t ldd = packed_ld(n, elem_bytes);
+  const dim3 grid((uint32_t)std::min<int64_t>((rows * (ldd * elem_bytes / 16) + 255) / 256, 8192));
+  if (elem_bytes == 1)
+    hipLaunchKernelGGL(k_pack_rows<1>, grid, dim3(256), 0, s, (const char*)src, ld, rows, n, (char*)dst, ldd);
+  else if (elem_bytes == 2)
+    hipLaunchKernelGGL(k_pack_rows<2>, grid, dim3(256), 0, s, (const char*)src, ld, rows, n, (char*)dst, ldd);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearArgs& a, const LinearPlan& p, int elem_bytes, void* partial, hipStream_t s) {
+  if (a.tokens <= 0 || a.n <= 0 || a.m <= 0 || a.n * elem_bytes > nt::kMaxRowBytes) return hipErrorInvalidValue;
+  if (p.skinny ? a.tokens > 64
+               : !tile_rows_ok(a.x, a.ldx, a.n, elem_bytes) || !tile_rows_ok(a.w, a.ldw, a.n, elem_bytes) ||
+                     p.splits < 1)
+    return hipErrorInvalidValue;
+  if (elem_bytes == 1) return linear_for<nt::I8>(a, p, partial, s);
+  if (elem_bytes == 2) return linear_for<nt::Bf16>(a, p, partial, s);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_zero(void* dst, int64_t ld, int64_t rows, int64_t cols, int elem_bytes, hipStream_t s) {
+  if (rows <= 0 || cols <= 0) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)std::min<int64_t>((rows * cols + 255) / 256, 4096));
+  if (elem_bytes == 2)
+    hipLaunchKernelGGL(k_zero<uint16_t>, grid, dim3(256), 0, s, (uint16_t*)dst, ld, rows, cols);
+  else if (elem_bytes == 4)
+    hipLaunchKernelGGL(k_zero<uint32_t>, grid, dim3(256), 0, s, (uint32_t*)dst, ld, rows, cols);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+int64_t act_grad_parts(int64_t rows) { return (rows + 63) / 64; }
+
+hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t s) {
+  const int64_t gx = (a.cols + 63) / 64, gy = (a.rows + 63) / 64;
+  if (a.rows <= 0 || a.cols <= 0 || gx > 0x7fffffff || gy > 65535 ||
+      (a.gt != nullptr && (a.ldgt % 8 != 0 || a.ldgt < a.rows || a.ldgt > gy * 64 || (uintptr_t)a.gt % 16 != 0)))
+    return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_turn<true>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_transpose(const bf16_t* src, int64_t ld, int64_t rows, int64_t cols, bf16_t* dst, int64_t ldd,
+                            hipStream_t s) {
+  ActGradArgs a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.dy = src;
+  a.lddy = ld;
+  a.gt = dst;
+  a.ldgt = ldd;
+  const int64_t gx = (cols + 63) / 64, gy = (rows + 63) / 64;
+  if (rows <= 0 || cols <= 0 || gx > 0x7fffffff || gy > 65535 || ldd % 8 != 0 || ldd < rows || ldd > gy * 64 ||
+      (uintptr_t)dst % 16 != 0)
+    return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_turn<false>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace ff
