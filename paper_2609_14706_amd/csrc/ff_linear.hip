@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "ff_layer_kernels.hpp"
 #include "ff_tile_nt.hpp"
@@ -22,27 +23,57 @@
 namespace ff {
 namespace {
 
-// z sigmoid(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi): the tanh form of gelu.
+// sigmoid(x) = 1 / (1 + 2^(-x log2 e)) by the exponential and reciprocal
+// instructions (one unit in the last place each; 0 and 1 far out).  Of the
+// argument's error, 2^-24 |x|, an activation keeps at most 2^-20.
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float sigmoid_of(float minus_x_log2e) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_x_log2e));
+}
+
+// gelu: z sigmoid(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi) (the tanh form).
 constexpr float kGelu = 1.5957691216057308f, kCube = 0.044715f;
 
-__device__ __forceinline__ float act_of(float z, int act) {
-  if (act == kActRelu) return z < 0.0f ? 0.0f : z;
-  if (act == kActSilu) return z / (1.0f + __expf(-z));
-  if (act == kActGelu) return z / (1.0f + __expf(-kGelu * (z + kCube * z * z * z)));
+__device__ __forceinline__ float gelu_gate(float z) {
+  return sigmoid_of(z * (-kGelu * kLog2e - kGelu * kLog2e * kCube * (z * z)));
+}
+__device__ __forceinline__ float silu_gate(float z) { return sigmoid_of(-kLog2e * z); }
+
+template <int ACT>
+__device__ __forceinline__ float act_as(float z) {
+  if (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
+  if (ACT == kActSilu) return z * silu_gate(z);
+  if (ACT == kActGelu) return z * gelu_gate(z);
   return z;
+}
+__device__ __forceinline__ float act_of(float z, int act) {
+  return act == kActRelu   ? act_as<kActRelu>(z)
+         : act == kActSilu ? act_as<kActSilu>(z)
+         : act == kActGelu ? act_as<kActGelu>(z)
+                           : z;
 }
 __device__ __forceinline__ float act_slope(float z, int act) {
   if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
   if (act == kActSilu) {
-    const float p = 1.0f / (1.0f + __expf(-z));
+    const float p = silu_gate(z);
     return p * (1.0f + z * (1.0f - p));
   }
   if (act == kActGelu) {
-    const float p = 1.0f / (1.0f + __expf(-kGelu * (z + kCube * z * z * z)));
+    const float p = gelu_gate(z);
     const float t = z * p * (1.0f - p);  // zero for large |z|, where z^2 may be infinite
     return t == 0.0f ? p : p + t * kGelu * (1.0f + 3.0f * kCube * z * z);
   }
   return 1.0f;
+}
+
+// f(integral_constant<0>) ... f(integral_constant<N - 1>): unrolled whatever its length.
+template <class F, int... I>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, const F& f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(const F& f) {
+  each(std::make_integer_sequence<int, N>(), f);
 }
 
 // W consecutive outputs of row t from column i on (W = 1, 2, 4 or 8), `count` of
@@ -106,6 +137,89 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t mt, uint32_t nt, ui
 template <class T> struct Scalar { typedef float type; };
 template <> struct Scalar<nt::I8> { typedef int32_t type; };
 
+// The epilogue of a tile that lies inside the matrix, straight from the
+// accumulators: a lane's TJ consecutive columns of 4 TI rows (row0 its first,
+// its rows 16 apart by i).  With one wave on a SIMD nothing hides a load, so bias, scales and the
+// rows' scales are read first and residuals three tile rows ahead; a loop that
+// loads row by row took 30 to 60 us a tile instead of 10 to 20 (256 x 256,
+// gelu, bias and residual the most).
+template <class T, int TI, int TJ>
+__device__ __forceinline__ void whole_tile(const LinearArgs& a, int64_t row0, int64_t col,
+                                           const typename nt::Tile<T, TI, TJ>::Acc& acc) {
+  constexpr int AHEAD = TI < 3 ? TI : 3;  // tile rows whose residual is on its way
+  struct Row {
+    uint32_t w[TJ / 2];
+    __device__ __forceinline__ float get(int j) const {
+      return __builtin_bit_cast(float, j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+    }
+  };
+  Row res[TI][4], bias;
+  float xs[TI][4], ws[TJ];
+  auto fetch = [&](auto i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) __builtin_memcpy(res[i][r].w, a.residual + (row0 + i * 16 + r) * a.ldr + col, sizeof(Row));
+  };
+  if (a.residual != nullptr) each<AHEAD>(fetch);
+  if (a.row_scale != nullptr) {
+    __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) __builtin_memcpy(xs[i], a.x_scale + row0 + i * 16, 16);
+  }
+  if (a.bias != nullptr) __builtin_memcpy(bias.w, a.bias + col, sizeof(Row));
+  each<TI>([&](auto i) {
+    float z[4][TJ];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) z[r][j] = (float)acc[i][j][r];
+    if (a.row_scale != nullptr) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) z[r][j] *= xs[i][r] * ws[j];
+    }
+    if (a.bias != nullptr) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) z[r][j] += bias.get(j);
+    }
+    auto store = [&](bf16_t* p, int64_t ld) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint32_t w[TJ / 2];
+#pragma unroll
+        for (int q = 0; q < TJ / 2; ++q)
+          w[q] = (uint32_t)f32_to_bf16(z[r][2 * q]) | ((uint32_t)f32_to_bf16(z[r][2 * q + 1]) << 16);
+        __builtin_memcpy(p + (row0 + i * 16 + r) * ld + col, w, sizeof w);
+      }
+    };
+    if (a.preact != nullptr) store(a.preact, a.ldz);
+    auto apply = [&](auto act) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) z[r][j] = act_as<decltype(act)::value>(z[r][j]);
+    };
+    if (a.act == kActRelu)
+      apply(std::integral_constant<int, kActRelu>());
+    else if (a.act == kActGelu)
+      apply(std::integral_constant<int, kActGelu>());
+    else if (a.act == kActSilu)
+      apply(std::integral_constant<int, kActSilu>());
+    if (a.residual != nullptr) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) z[r][j] += res[i][r].get(j);
+    }
+    store(a.y, a.ldy);
+    if constexpr (i + AHEAD < TI)
+      if (a.residual != nullptr) fetch(std::integral_constant<int, i + AHEAD>());
+    __builtin_amdgcn_sched_barrier(0);  // keeps the next rows' values out of this one's registers
+  });
+}
+
 // grid: tiles x splits.  P: null (one split), or splits x tokens x m sums.
 template <class T, int TI, int TJ>
 __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(LinearArgs a, uint32_t mt,
@@ -135,15 +249,19 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(L
         pb = B.p + k;
       },
       [&](int p) { return kbytes - p * nt::kPair; }, acc);
-  // The sums go through LDS (each lane its own 16-byte slots: no barrier, no
-  // bank conflict) so that one short loop serves all of them: unrolled, the
-  // epilogue of a 256 x 256 tile is 32 copies long.
+  const int64_t col = i0 + G::col_of();
+  if (P == nullptr && A.rows == G::BM && B.rows == G::BN) {
+    whole_tile<T, TI, TJ>(a, t0 + G::row_of(0, 0), col, acc);
+    return;
+  }
+  // Tiles at the edges and partial sums: through LDS (each lane its own
+  // 16-byte slots: no barrier, no bank conflict), so that one short loop serves
+  // every row.
   typedef typename Scalar<T>::type S;
   typedef __attribute__((ext_vector_type(4))) S S4;
   constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;  // tile rows a phase, pieces of a row
   static_assert(TJ % 4 == 0 && sizeof(S4) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
   S4* stage = reinterpret_cast<S4*>(&sm) + threadIdx.x;
-  const int64_t col = i0 + G::col_of();
   const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
