@@ -75,10 +75,11 @@ struct LinearArgs {
   int act;
 };
 // How a product is run: `skinny` for few tokens, else tiles of
-// 32 ti x 32 tj with k in `splits` parts (joined by a second kernel).
+// 32 ti x 32 tj, `slots` pairs of k in LDS, with k in `splits` parts (joined by
+// a second kernel).
 struct LinearPlan {
   bool skinny;
-  int ti, tj;
+  int ti, tj, slots;
   int splits;
 };
 LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes);

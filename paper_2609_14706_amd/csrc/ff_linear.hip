@@ -11,6 +11,10 @@
 // output rows' share of k straight from memory to the matrix cores, with no
 // LDS between, and joins the waves' sums at the end.
 #include <math.h>
+#ifdef FF_DEV
+#include <stdio.h>
+#include <stdlib.h>
+#endif
 
 #include <algorithm>
 #include <type_traits>
@@ -64,16 +68,6 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     return t == 0.0f ? p : p + t * kGelu * (1.0f + 3.0f * kCube * z * z);
   }
   return 1.0f;
-}
-
-// f(integral_constant<0>) ... f(integral_constant<N - 1>): unrolled whatever its length.
-template <class F, int... I>
-__device__ __forceinline__ void each(std::integer_sequence<int, I...>, const F& f) {
-  (f(std::integral_constant<int, I>()), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void each(const F& f) {
-  each(std::make_integer_sequence<int, N>(), f);
 }
 
 // W consecutive outputs of row t from column i on (W = 1, 2, 4 or 8), `count` of
@@ -137,96 +131,36 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t mt, uint32_t nt, ui
 template <class T> struct Scalar { typedef float type; };
 template <> struct Scalar<nt::I8> { typedef int32_t type; };
 
-// The epilogue of a tile that lies inside the matrix, straight from the
-// accumulators: a lane's TJ consecutive columns of 4 TI rows (row0 its first,
-// its rows 16 apart by i).  With one wave on a SIMD nothing hides a load, so bias, scales and the
-// rows' scales are read first and residuals three tile rows ahead; a loop that
-// loads row by row took 30 to 60 us a tile instead of 10 to 20 (256 x 256,
-// gelu, bias and residual the most).
-template <class T, int TI, int TJ>
-__device__ __forceinline__ void whole_tile(const LinearArgs& a, int64_t row0, int64_t col,
-                                           const typename nt::Tile<T, TI, TJ>::Acc& acc) {
-  constexpr int AHEAD = TI < 3 ? TI : 3;  // tile rows whose residual is on its way
-  struct Row {
-    uint32_t w[TJ / 2];
-    __device__ __forceinline__ float get(int j) const {
-      return __builtin_bit_cast(float, j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-    }
-  };
-  Row res[TI][4], bias;
-  float xs[TI][4], ws[TJ];
-  auto fetch = [&](auto i) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) __builtin_memcpy(res[i][r].w, a.residual + (row0 + i * 16 + r) * a.ldr + col, sizeof(Row));
-  };
-  if (a.residual != nullptr) each<AHEAD>(fetch);
-  if (a.row_scale != nullptr) {
-    __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
-#pragma unroll
-    for (int i = 0; i < TI; ++i) __builtin_memcpy(xs[i], a.x_scale + row0 + i * 16, 16);
+// TJ consecutive bf16 values of a row, as they lie in memory.
+template <int TJ>
+struct Piece {
+  uint32_t w[TJ / 2];
+  __device__ __forceinline__ float get(int j) const {
+    return __builtin_bit_cast(float, j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
   }
-  if (a.bias != nullptr) __builtin_memcpy(bias.w, a.bias + col, sizeof(Row));
-  each<TI>([&](auto i) {
-    float z[4][TJ];
+  __device__ __forceinline__ void set(const float (&f)[TJ]) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int j = 0; j < TJ; ++j) z[r][j] = (float)acc[i][j][r];
-    if (a.row_scale != nullptr) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) z[r][j] *= xs[i][r] * ws[j];
-    }
-    if (a.bias != nullptr) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) z[r][j] += bias.get(j);
-    }
-    auto store = [&](bf16_t* p, int64_t ld) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        uint32_t w[TJ / 2];
-#pragma unroll
-        for (int q = 0; q < TJ / 2; ++q)
-          w[q] = (uint32_t)f32_to_bf16(z[r][2 * q]) | ((uint32_t)f32_to_bf16(z[r][2 * q + 1]) << 16);
-        __builtin_memcpy(p + (row0 + i * 16 + r) * ld + col, w, sizeof w);
-      }
-    };
-    if (a.preact != nullptr) store(a.preact, a.ldz);
-    auto apply = [&](auto act) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) z[r][j] = act_as<decltype(act)::value>(z[r][j]);
-    };
-    if (a.act == kActRelu)
-      apply(std::integral_constant<int, kActRelu>());
-    else if (a.act == kActGelu)
-      apply(std::integral_constant<int, kActGelu>());
-    else if (a.act == kActSilu)
-      apply(std::integral_constant<int, kActSilu>());
-    if (a.residual != nullptr) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) z[r][j] += res[i][r].get(j);
-    }
-    store(a.y, a.ldy);
-    if constexpr (i + AHEAD < TI)
-      if (a.residual != nullptr) fetch(std::integral_constant<int, i + AHEAD>());
-    __builtin_amdgcn_sched_barrier(0);  // keeps the next rows' values out of this one's registers
-  });
-}
+    for (int q = 0; q < TJ / 2; ++q)
+      w[q] = (uint32_t)f32_to_bf16(f[2 * q]) | ((uint32_t)f32_to_bf16(f[2 * q + 1]) << 16);
+  }
+  __device__ __forceinline__ void load(const bf16_t* p) { __builtin_memcpy(w, p, sizeof w); }
+  __device__ __forceinline__ void store(bf16_t* p) const { __builtin_memcpy(p, w, sizeof w); }
+};
 
 // grid: tiles x splits.  P: null (one split), or splits x tokens x m sums.
-template <class T, int TI, int TJ>
-__global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(LinearArgs a, uint32_t mt,
-                                                                             uint32_t ntl, uint32_t splits,
-                                                                             typename Scalar<T>::type* P) {
-  typedef nt::Tile<T, TI, TJ> G;
-  __shared__ typename G::Ring sm;
+// Workgroups a compute unit: what its LDS holds.
+template <class T, int TI, int TJ, int SLOTS>
+__global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) void k_tile(
+    LinearArgs a, uint32_t mt, uint32_t ntl, uint32_t splits, typename Scalar<T>::type* P) {
+  typedef nt::Tile<T, TI, TJ, SLOTS> G;
+  // (one object: beside a second one the compiler waits for every copy before each read)
+  struct Shared {
+    typename G::Ring ring;
+    float xs[G::BM];  // the tile's row scales
+  };
+  __shared__ Shared all;
+  typename G::Ring& sm = all.ring;
+  float* xs = all.xs;
   const uint32_t tiles = mt * ntl;
   const uint32_t w = xcd_remap(blockIdx.x, gridDim.x);
   const uint32_t z = w / tiles;
@@ -241,6 +175,9 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(L
   const int p0 = (int)((int64_t)pairs * z / splits), p1 = (int)((int64_t)pairs * (z + 1) / splits);
   typename G::Acc acc;
   G::zero(acc);
+  static_assert(G::BM <= nt::kThreads, "a row a thread");
+  if (a.x_scale != nullptr && (int)threadIdx.x < G::BM)
+    xs[threadIdx.x] = (int)threadIdx.x < A.rows ? a.x_scale[t0 + threadIdx.x] : 0.0f;
   G::loop(
       sm, A, B, p0, p1,
       [&](int p, const char*& pa, const char*& pb) {
@@ -249,20 +186,34 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(L
         pb = B.p + k;
       },
       [&](int p) { return kbytes - p * nt::kPair; }, acc);
-  const int64_t col = i0 + G::col_of();
-  if (P == nullptr && A.rows == G::BM && B.rows == G::BN) {
-    whole_tile<T, TI, TJ>(a, t0 + G::row_of(0, 0), col, acc);
-    return;
-  }
-  // Tiles at the edges and partial sums: through LDS (each lane its own
-  // 16-byte slots: no barrier, no bank conflict), so that one short loop serves
-  // every row.
+  // The sums go through LDS (each lane its own 16-byte slots: no barrier, no
+  // bank conflict) so that a short loop over four rows at a time serves all of
+  // them: straight from the accumulators the epilogue of a 256 x 256 tile is 32
+  // copies long and spills.  With one wave on a SIMD nothing hides a load, so a
+  // lane's bias and scales are read once and the next rows' residual before
+  // these rows' work; reading them row by row took 30 to 60 us a tile.
   typedef typename Scalar<T>::type S;
   typedef __attribute__((ext_vector_type(4))) S S4;
   constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;  // tile rows a phase, pieces of a row
   static_assert(TJ % 4 == 0 && sizeof(S4) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
   S4* stage = reinterpret_cast<S4*>(&sm) + threadIdx.x;
+  const int64_t col = i0 + G::col_of(), row0 = t0 + G::row_of(0, 0);
   const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
+  const int rows = (int)min((int64_t)G::BM, a.tokens - row0);  // from row0 on (the lane's are 16 apart)
+  const bool vec = B.rows == G::BN || a.m % TJ == 0;           // a lane's columns are all inside or all outside
+  float ws[TJ];
+  Piece<TJ> bias, res[4], more[4];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (i * 16 + r < rows) more[r].load(a.residual + (row0 + i * 16 + r) * a.ldr + col);
+  };
+  const bool fused = vec && P == nullptr && count > 0;
+  if (fused) {
+    if (a.row_scale != nullptr) __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
+    if (a.bias != nullptr) bias.load(a.bias + col);
+    if (a.residual != nullptr) fetch(0);
+  }
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
 #pragma unroll
@@ -277,26 +228,95 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_tile(L
           stage[((i * 4 + r) * V + v) * nt::kThreads] = o;
         }
 #pragma unroll 1
-    for (int q = 0; q < HI * 4; ++q) {
-      S v[TJ];
+    for (int q = 0; q < HI; ++q) {
+      const int i = h * HI + q;
+      S s[4][TJ];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const S4 o = stage[(q * V + k) * nt::kThreads];
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * k + e] = o[e];
-      }
-      const int64_t t = t0 + G::row_of(h * HI + (q >> 2), q & 3);
-      if (t >= a.tokens) continue;
-      if (P != nullptr) {
-        S* o = P + ((int64_t)z * a.tokens + t) * a.m + col;
+        for (int v = 0; v < V; ++v) {
+          const S4 o = stage[((q * 4 + r) * V + v) * nt::kThreads];
 #pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          if (j < count) o[j] = v[j];
-      } else {
-        float f[TJ];
+          for (int e = 0; e < 4; ++e) s[r][4 * v + e] = o[e];
+        }
+      if (fused) {
+        if (a.residual != nullptr) {
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) f[j] = (float)v[j];
-        finish<TJ>(a, t, col, f, count);
+          for (int r = 0; r < 4; ++r) res[r] = more[r];
+          if (i + 1 < TI) fetch(i + 1);
+        }
+        float z[4][TJ];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) z[r][j] = (float)s[r][j];
+        if (a.row_scale != nullptr) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&xs[G::row_of(i, 0)]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) z[r][j] *= x[r] * ws[j];
+        }
+        if (a.bias != nullptr) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) z[r][j] += bias.get(j);
+        }
+        auto put = [&](bf16_t* p, int64_t ld) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            Piece<TJ> o;
+            o.set(z[r]);
+            if (i * 16 + r < rows) o.store(p + (row0 + i * 16 + r) * ld + col);
+          }
+        };
+        if (a.preact != nullptr) put(a.preact, a.ldz);
+        auto apply = [&](auto act) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) z[r][j] = act_as<decltype(act)::value>(z[r][j]);
+        };
+        if (a.act == kActRelu)
+          apply(std::integral_constant<int, kActRelu>());
+        else if (a.act == kActGelu)
+          apply(std::integral_constant<int, kActGelu>());
+        else if (a.act == kActSilu)
+          apply(std::integral_constant<int, kActSilu>());
+        if (a.residual != nullptr) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) z[r][j] += res[r].get(j);
+        }
+        put(a.y, a.ldy);
+      } else if (P != nullptr) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (i * 16 + r < rows) {
+            S* o = P + ((int64_t)z * a.tokens + row0 + i * 16 + r) * a.m + col;
+            if (count == TJ) {
+              __builtin_memcpy(o, s[r], sizeof s[r]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < TJ; ++j)
+                if (j < count) o[j] = s[r][j];
+            }
+          }
+      } else {  // columns that end inside a lane's
+#pragma unroll 1
+        for (int r = 0; r < 4; ++r)
+          if (i * 16 + r < rows) {
+            float f[TJ];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              const S4 o = stage[((q * 4 + r) * V + v) * nt::kThreads];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) f[4 * v + e] = (float)o[e];
+            }
+            finish<TJ>(a, row0 + i * 16 + r, col, f, count);
+          }
       }
     }
   }
@@ -313,9 +333,16 @@ __global__ __launch_bounds__(256) void k_join(LinearArgs a, const S* P, int spli
     S v[4] = {0, 0, 0, 0};
     for (int z = 0; z < splits; ++z) {
       const S* p = P + ((int64_t)z * a.tokens + t) * a.m + i;
+      S w[4] = {0, 0, 0, 0};
+      if (count == 4) {
+        __builtin_memcpy(w, p, sizeof w);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < count) v[k] += p[k];
+        for (int k = 0; k < 4; ++k)
+          if (k < count) w[k] = p[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += w[k];
     }
     float f[4];
 #pragma unroll
@@ -510,14 +537,14 @@ __global__ __launch_bounds__(256) void k_turn(ActGradArgs a) {
   }
 }
 
-template <class T, int TI, int TJ>
+template <class T, int TI, int TJ, int SLOTS>
 hipError_t tiles(const LinearArgs& a, const LinearPlan& p, void* partial, hipStream_t s) {
-  typedef nt::Tile<T, TI, TJ> G;
+  typedef nt::Tile<T, TI, TJ, SLOTS> G;
   const int64_t mt = (a.tokens + G::BM - 1) / G::BM, ntl = (a.m + G::BN - 1) / G::BN;
   const int64_t wgs = mt * ntl * p.splits;
   if (wgs > 0x7fffffff || (p.splits > 1 && partial == nullptr)) return hipErrorInvalidValue;
   typedef typename Scalar<T>::type S;
-  hipLaunchKernelGGL((k_tile<T, TI, TJ>), dim3((uint32_t)wgs), dim3(nt::kThreads), 0, s, a, (uint32_t)mt,
+  hipLaunchKernelGGL((k_tile<T, TI, TJ, SLOTS>), dim3((uint32_t)wgs), dim3(nt::kThreads), 0, s, a, (uint32_t)mt,
                      (uint32_t)ntl, (uint32_t)p.splits, p.splits > 1 ? (S*)partial : nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
@@ -552,22 +579,64 @@ hipError_t linear_for(const LinearArgs& a, const LinearPlan& p, void* partial, h
     if (a.tokens <= 32) return a.m >= 8192 ? skinny_waves<T, 2, 2>(a, s) : skinny_waves<T, 2, 1>(a, s);
     return a.m >= 8192 ? skinny_waves<T, 4, 2>(a, s) : skinny_waves<T, 4, 1>(a, s);
   }
-  if (p.ti == 8 && p.tj == 8) return tiles<T, 8, 8>(a, p, partial, s);
-  if (p.ti == 4 && p.tj == 4) return tiles<T, 4, 4>(a, p, partial, s);
+#define FF_TILE(I, J, S) \
+  if (p.ti == I && p.tj == J && p.slots == S) return tiles<T, I, J, S>(a, p, partial, s);
+  FF_TILE(8, 8, 2) FF_TILE(4, 4, 2) FF_TILE(4, 4, 4) FF_TILE(2, 4, 3)
+#undef FF_TILE
   return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
-  if (tokens <= 64) return {true, 0, 0, 1};
-  auto count = [&](int64_t b) { return ((tokens + b - 1) / b) * ((m + b - 1) / b); };
-  if (count(256) >= 192) return {false, 8, 8, 1};
-  const int64_t t = count(128), pairs = (n * elem_bytes + nt::kPair - 1) / nt::kPair;
-  // two workgroups of 128 x 128 tiles share a compute unit; k is split until
-  // there are 512, each with eight pairs of k or more
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / t, pairs / 8, 16}));
-  return {false, 4, 4, (int)splits};
+#ifdef FF_DEV
+  if (const char* v = getenv("FF_PLAN")) {
+    LinearPlan p{};
+    int sk;
+    if (sscanf(v, "%d,%d,%d,%d,%d", &sk, &p.ti, &p.tj, &p.slots, &p.splits) == 5) {
+      p.skinny = sk;
+      return p;
+    }
+  }
+#endif
+  // The fastest of the forms below by a model of their times (us), fitted to
+  // sweeps of both types from 1 to 4096 tokens and 300 to 28672 wide.  Per pair
+  // of k a workgroup takes `pair` (the latency of its copies, or its products)
+  // while it has a compute unit to itself and `loaded` when all are busy; where
+  // w goes by once (one row of tiles) memory's latency, 0.47, at least, and the
+  // workgroups' share of reading it at 6.6 TB/s.  `ends` is its start and
+  // epilogue.  A join of splits costs a launch and the partial sums' traffic.
+  struct Form {
+    int ti, tj, slots, wgs;
+    double pair, loaded, ends;
+  };
+  static const Form forms[] = {{8, 8, 2, 1, 1.41, 1.41, 12.0}, {4, 4, 2, 2, 0.52, 0.80, 6.0}, {4, 4, 4, 1, 0.37, 0.53, 3.0},
+                               {2, 4, 3, 2, 0.25, 0.50, 2.0}};
+  const int64_t pairs = (n * elem_bytes + nt::kPair - 1) / nt::kPair;
+  LinearPlan best{false, 8, 8, 2, 1};
+  double least = 1e300;
+  for (const Form& f : forms) {
+    const int64_t rows = (tokens + 32 * f.ti - 1) / (32 * f.ti), tiles = rows * ((m + 32 * f.tj - 1) / (32 * f.tj));
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (s > 1 && (s * 4 > pairs || tiles * s > 768 || f.ti == 8)) break;
+      const int64_t wgs = tiles * s, rounds = (wgs + 256 * f.wgs - 1) / (256 * f.wgs);
+      double pair = wgs > 256 ? f.loaded : f.pair;
+      if (rows == 1)
+        pair = std::max({pair, 0.47, (double)std::min<int64_t>(wgs, 256 * f.wgs) * (32 * f.tj * nt::kPair) / 6.6e6});
+      double us = (double)rounds * (f.ends + (double)((pairs + s - 1) / s) * pair);
+      if (s > 1) us += 5.0 + 8.0 * (double)s * (double)tokens * (double)m / 4e6;
+      if (us < least) {
+        least = us;
+        best = {false, f.ti, f.tj, f.slots, s};
+      }
+    }
+  }
+  if (tokens <= 64) {
+    // straight from memory: what 16, 32 or 64 tokens a wave leave of its rate
+    const double rate = tokens <= 16 ? 4.5e6 : tokens <= 32 ? 3.3e6 : 2.3e6;
+    if (2.0 + (double)m * (double)n * elem_bytes / rate < least) return {true, 0, 0, 0, 1};
+  }
+  return best;
 }
 
 size_t linear_partial_bytes(const LinearPlan& p, int64_t tokens, int64_t m) {

@@ -152,7 +152,7 @@ __device__ __forceinline__ void put4(uint16_t* p, const uint16_t (&v)[4]) { __bu
 
 template <int PARTS, int TI, int TJ, bool SYM>
 __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(StepArgs a) {
-  typedef nt::Tile<nt::F16, TI, TJ> G;
+  typedef nt::Tile<nt::F16, TI, TJ, 2> G;
   __shared__ typename G::Ring sm;
   const uint32_t w = xcd_remap(blockIdx.x, gridDim.x);
   uint32_t ti, tj;

@@ -7,8 +7,9 @@
 // v_mfma_i32_16x16x64_i8), so k is counted in bytes here and one loop serves
 // all: k goes in pairs of 64-byte steps, i.e. whole 128-byte lines of each
 // operand row, copied global -> LDS without registers (buffer_load ... lds,
-// 16 bytes a lane) through two slots, one pair in flight ahead of the matrix
-// cores.  The 16-byte chunk c of row r sits at position c ^ ((r >> 1) & 7) of
+// 16 bytes a lane) through SLOTS slots, all but one of them in flight ahead of the
+// matrix cores: two where the products of a pair take longer than its copies,
+// more where a tile is small or there are few of them.  The 16-byte chunk c of row r sits at position c ^ ((r >> 1) & 7) of
 // its row: a fragment read (one chunk of 16 consecutive rows per pass) then
 // covers all 64 banks.
 //
@@ -81,14 +82,16 @@ struct Rows {
   uint32_t ld;
 };
 
-template <class T, int TI, int TJ>
+template <class T, int TI, int TJ, int SLOTS>
 struct Tile {
   static constexpr int BM = 32 * TI, BN = 32 * TJ;
+  static constexpr int NL = TI + TJ;  // copies a wave issues per pair
+  static_assert(SLOTS >= 2 && (SLOTS - 1) * NL < 64, "copies in flight are counted in six bits");
   typedef typename T::acc Acc[TI][TJ];
 
   struct __align__(16) Ring {
-    u32x4 a[2][BM * kChunks];
-    u32x4 b[2][BN * kChunks];
+    u32x4 a[SLOTS][BM * kChunks];
+    u32x4 b[SLOTS][BN * kChunks];
   };
 
   // B's rows are permuted within each wave's half so that a lane's TJ tiles
@@ -160,38 +163,36 @@ struct Tile {
     f[t] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(&sm) + off);
   }
 
-  // The products of one step.  If READ, the fragments of the next step are
-  // read among the first three quarters of them; if LOADS, the copies of a
-  // later pair are spread over all of them.
-  template <bool READ, bool LOADS>
+  // The products of one step, with the next step's fragments read among the
+  // first three quarters of them.  If LOADS, the copies of a later pair are
+  // spread over all of them.
+  template <bool LOADS>
   static __device__ __forceinline__ void step(Ring& sm, const Frags& cur, Frags& nxt, int rslot, int rhalf,
                                               int lslot, const char* pa, const char* pb, const Lane& L,
                                               uint32_t cut, int wave, const FragBase& fb, Acc& acc) {
-    constexpr int NP = TI * TJ, NR = TI + TJ;
-    constexpr int RS = NP * 3 / 4 / NR > 0 ? NP * 3 / 4 / NR : 1;   // products per read
-    constexpr int RB = (NR + NP - 1) / NP;                          // reads per product (tiny tiles)
-    constexpr int LS = NP / NR > 0 ? NP / NR : 1;
+    constexpr int NP = TI * TJ;
+    constexpr int RS = NP * 3 / 4 / NL > 0 ? NP * 3 / 4 / NL : 1;  // products per read
+    constexpr int LS = NP / NL > 0 ? NP / NL : 1;                  // products per copy
+    static_assert(NP >= NL, "a read and a copy at most after each product");
 #pragma unroll
     for (int m = 0; m < NP; ++m) {
       const int i = m / TJ, j = m % TJ;
       acc[i][j] = T::mfma(cur[i], cur[TI + j], acc[i][j]);
-      if (READ) {
-        if (RB > 1) {
-#pragma unroll
-          for (int q = m * RB; q < (m + 1) * RB && q < NR; ++q) read_one(sm, rslot, rhalf, fb, nxt, q);
-        } else if (m % RS == 0 && m / RS < NR) {
-          read_one(sm, rslot, rhalf, fb, nxt, m / RS);
-        }
-      }
-      if (LOADS) {
-        if (RB > 1) {
-#pragma unroll
-          for (int q = m * RB; q < (m + 1) * RB && q < NR; ++q) issue_one(sm, lslot, pa, pb, L, cut, wave, q);
-        } else if (m % LS == 0 && m / LS < NR) {
-          issue_one(sm, lslot, pa, pb, L, cut, wave, m / LS);
-        }
-      }
+      if (m % RS == 0 && m / RS < NL) read_one(sm, rslot, rhalf, fb, nxt, m / RS);
+      if (LOADS && m % LS == 0 && m / LS < NL) issue_one(sm, lslot, pa, pb, L, cut, wave, m / LS);
       __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // 256 accumulator registers are exactly the accumulation file.  Said before
+  // and after the loop, it keeps the compiler from carrying other registers'
+  // wishes through it, at the price of 100 to 300 moves a pair.
+  static __device__ __forceinline__ void pin(Acc& acc) {
+    if (TI * TJ == 64) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) asm volatile("" : "+a"(acc[i][j]));
     }
   }
 
@@ -199,59 +200,50 @@ struct Tile {
   // pointers at pair p (row 0); left(p) the bytes of k that are left there
   // (128 or more for a whole pair).  Per pair, its first step multiplies from
   // registers while the second step's fragments are read; then the next pair
-  // has to have landed, the pair's one barrier is taken (every wave has read
-  // all of this slot and sees the next pair), and the second step reads the
-  // next pair's first fragments and copies the pair after it into the slot
-  // just freed.  Every wave takes the same number of barriers: n is uniform.
+  // has to have landed (copies return in order: at most SLOTS - 2 later pairs
+  // are still on their way), the pair's one barrier is taken (every wave has
+  // read all of this slot and sees the next pair), and the second step reads
+  // the next pair's first fragments and copies the pair SLOTS further on into
+  // the slot just freed.  Pairs beyond p1 are "copied" from outside, i.e. their
+  // slots get zeros that no product uses: one loop body for all pairs keeps
+  // the accumulators where they are (peeled ends moved hundreds of registers).
+  // Every wave takes the same number of barriers: p0 and p1 are uniform.
   template <class Addr, class Left>
   static __device__ __forceinline__ void loop(Ring& sm, const Rows& A, const Rows& B, int p0, int p1,
                                               const Addr& addr, const Left& left, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = p1 - p0;
-    if (n <= 0) return;
+    if (p1 <= p0) return;
     const Lane L = lane_of(A, B, wave, lane);
     const FragBase fb = frag_base(wave, lane);
     const char *pa, *pb;
-    auto cut = [&](int p) -> uint32_t { return 16 * L.c < left(p) ? 0u : kOutside; };
-    auto pair = [&](int p, int slot) {
-      addr(p, pa, pb);
-      const uint32_t c = cut(p);
+    auto cut = [&](int p) -> uint32_t { return p < p1 && 16 * L.c < left(p) ? 0u : kOutside; };
 #pragma unroll
-      for (int q = 0; q < TI + TJ; ++q) issue_one(sm, slot, pa, pb, L, c, wave, q);
-    };
-    pair(p0, 0);
-    if (n > 1) {
-      pair(p0 + 1, 1);
-      wait_vmem<TI + TJ>();
-    } else {
-      wait_vmem<0>();
+    for (int q = 0; q < SLOTS; ++q) {
+      addr(p0 + q, pa, pb);
+      const uint32_t c = cut(p0 + q);
+#pragma unroll
+      for (int k = 0; k < NL; ++k) issue_one(sm, q, pa, pb, L, c, wave, k);
     }
+    wait_vmem<(SLOTS - 1) * NL>();
     __builtin_amdgcn_s_barrier();
     Frags F[2];
 #pragma unroll
-    for (int q = 0; q < TI + TJ; ++q) read_one(sm, 0, 0, fb, F[0], q);
-    int j = 0;
-    for (; j + 2 < n; ++j) {
-      const int slot = j & 1;
-      step<true, false>(sm, F[0], F[1], slot, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
-      wait_vmem<0>();
+    for (int q = 0; q < NL; ++q) read_one(sm, 0, 0, fb, F[0], q);
+    int slot = 0;
+    pin(acc);
+    for (int p = p0; p < p1; ++p) {
+      step<false>(sm, F[0], F[1], slot, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
+      wait_vmem<(SLOTS - 2) * NL>();
       wait_lds();
       __builtin_amdgcn_s_barrier();
-      addr(p0 + j + 2, pa, pb);
-      step<true, true>(sm, F[1], F[0], slot ^ 1, 0, slot, pa, pb, L, cut(p0 + j + 2), wave, fb, acc);
+      addr(p + SLOTS, pa, pb);
+      const int next = slot + 1 == SLOTS ? 0 : slot + 1;
+      step<true>(sm, F[1], F[0], next, 0, slot, pa, pb, L, cut(p + SLOTS), wave, fb, acc);
+      slot = next;
     }
-    if (j + 1 < n) {
-      const int slot = j & 1;
-      step<true, false>(sm, F[0], F[1], slot, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
-      wait_vmem<0>();
-      wait_lds();
-      __builtin_amdgcn_s_barrier();
-      step<true, false>(sm, F[1], F[0], slot ^ 1, 0, 0, nullptr, nullptr, L, 0, wave, fb, acc);
-      ++j;
-    }
-    step<true, false>(sm, F[0], F[1], j & 1, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
-    step<false, false>(sm, F[1], F[0], 0, 0, 0, nullptr, nullptr, L, 0, wave, fb, acc);
+    pin(acc);
+    wait_vmem<0>();  // the copies of zeros: LDS is the caller's from here on
     __syncthreads();
   }
 
