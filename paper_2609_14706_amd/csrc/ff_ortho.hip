@@ -17,6 +17,10 @@
 // last product of a step stores both.  Symmetric products compute the tiles on
 // and above the diagonal and store them twice.
 #include <math.h>
+#ifdef FF_DEV
+#include <stdio.h>
+#include <stdlib.h>
+#endif
 
 #include <algorithm>
 
@@ -26,7 +30,7 @@
 namespace ff {
 namespace {
 
-constexpr int kNormParts = 128;  // partial sums of squares per matrix
+constexpr int kNormParts = 1024;  // partial sums of squares per matrix
 
 __device__ __forceinline__ uint16_t f16_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 __device__ __forceinline__ float f16_f32(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
@@ -128,7 +132,8 @@ __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t 
 
 // One product of a step, C = L R^T with L: rows x k, R: cols x k.
 //   out = alpha C + beta D, D (nullable) laid out as C, in parts;
-// stored by rows (o) and by columns (t), or as the result (user, E).
+// stored by rows (o) and by columns (t), or as the result (user, E), or, k in
+// `splits` parts, as partial sums (sums: splits x batch x rows x c8 fp32).
 struct StepArgs {
   int64_t rows, cols, k;  // k a multiple of 8 (the operands' zeros included)
   Parts L, R, D, o, t;
@@ -136,30 +141,87 @@ struct StepArgs {
   void* user;  // the result: element (i, j) at i si + j sj
   int64_t si, sj, su;
   int bf16;
-  int mt, ntl;  // tiles
+  int mt, ntl, tiles;  // tile rows and columns, tiles in all
+  int splits;
+  float* sums;
 };
 
-// Upper tile `idx` of a T x T grid, column by column: (0,0), (0,1), (1,1), ...
-__device__ __forceinline__ void upper_at(uint32_t idx, uint32_t& i, uint32_t& j) {
-  uint32_t c = (uint32_t)((sqrtf(8.0f * (float)idx + 1.0f) - 1.0f) * 0.5f);
-  while ((c + 1) * (c + 2) / 2 <= idx) ++c;
-  while (c * (c + 1) / 2 > idx) --c;
-  j = c;
-  i = idx - c * (c + 1) / 2;
+// N consecutive fp16 numbers of a row, as they lie in memory.
+template <int N>
+struct Halves {
+  uint32_t w[N / 2];
+  __device__ __forceinline__ float get(int j) const { return f16_f32((uint16_t)(w[j >> 1] >> (16 * (j & 1)))); }
+  __device__ __forceinline__ void load(const uint16_t* p, int count) {
+    if (count >= N) {
+      __builtin_memcpy(w, p, sizeof w);
+    } else {
+#pragma unroll
+      for (int q = 0; q < N / 2; ++q) w[q] = 0;
+#pragma unroll
+      for (int j = 0; j < N - 1; ++j)
+        if (j < count) w[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* p, int count) const {
+    if (count >= N) {
+      __builtin_memcpy(p, w, sizeof w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N - 1; ++j)
+        if (j < count) p[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+  }
+};
+// f[0] .. f[N - 1] rounded, and what the rounding left, rounded.
+template <int N>
+__device__ __forceinline__ void split_parts(const float (&f)[N], Halves<N>& hi, Halves<N>& lo) {
+#pragma unroll
+  for (int q = 0; q < N / 2; ++q) {
+    const uint16_t a = f16_bits(f[2 * q]), b = f16_bits(f[2 * q + 1]);
+    hi.w[q] = (uint32_t)a | ((uint32_t)b << 16);
+    lo.w[q] = (uint32_t)f16_bits(f[2 * q] - f16_f32(a)) | ((uint32_t)f16_bits(f[2 * q + 1] - f16_f32(b)) << 16);
+  }
 }
 
-__device__ __forceinline__ void put4(uint16_t* p, const uint16_t (&v)[4]) { __builtin_memcpy(p, v, 8); }
+// Results of four rows from `row` on, N columns from `col` on, into o by rows
+// and into t (null: not) by columns.  wide: columns that exist, the zeros up to
+// the next multiple of eight among them; rows of t hold zeros likewise.
+template <int PARTS, int N>
+__device__ __forceinline__ void store_parts(const float (&f)[4][N], int64_t row, int64_t rows, int64_t col,
+                                            int64_t cols, int wide, const Parts& o, const Parts* t, int64_t z) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (row + r < rows) {
+      Halves<N> hi, lo;
+      split_parts<N>(f[r], hi, lo);
+      const int64_t at = z * o.stride + (row + r) * o.ld + col;
+      hi.store(o.hi + at, wide);
+      if (PARTS == 2) lo.store(o.lo + at, wide);
+    }
+  if (t == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (col + j < cols) {
+      const float c[4] = {f[0][j], f[1][j], f[2][j], f[3][j]};
+      Halves<4> hi, lo;
+      split_parts<4>(c, hi, lo);
+      const int64_t at = z * t->stride + (col + j) * t->ld + row;
+      hi.store(t->hi + at, 4);
+      if (PARTS == 2) lo.store(t->lo + at, 4);
+    }
+}
 
-template <int PARTS, int TI, int TJ, bool SYM>
-__global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(StepArgs a) {
-  typedef nt::Tile<nt::F16, TI, TJ, 2> G;
+template <int PARTS, int TI, int TJ, int SLOTS, bool SYM>
+__global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) void k_step(StepArgs a) {
+  typedef nt::Tile<nt::F16, TI, TJ, SLOTS> G;
   __shared__ typename G::Ring sm;
   const uint32_t w = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t part = w / a.tiles, tile = w - part * a.tiles;
   uint32_t ti, tj;
   if (SYM) {
-    upper_at(w, ti, tj);
+    grouped_tile(tile, a.mt, ti, tj);
   } else {
-    const uint32_t strip = w / (8 * a.ntl), u = w - strip * 8 * a.ntl, r = min(8u, a.mt - strip * 8);
+    const uint32_t strip = tile / (8 * a.ntl), u = tile - strip * 8 * a.ntl, r = min(8u, a.mt - strip * 8);
     ti = strip * 8 + u % r;
     tj = u / r;
   }
@@ -168,11 +230,12 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(S
   const nt::Rows B{nullptr, (int)min((int64_t)G::BN, a.cols - j0), (uint32_t)(a.R.ld * 2)};
   const int64_t la = z * a.L.stride + i0 * a.L.ld, rb = z * a.R.stride + j0 * a.R.ld;
   const int kbytes = (int)a.k * 2, pairs = (kbytes + nt::kPair - 1) / nt::kPair;
+  const int total = PARTS == 2 ? 3 * pairs : pairs;
   typename G::Acc acc;
   G::zero(acc);
   // two parts: hi lo, lo hi, then hi hi (the largest last)
   G::loop(
-      sm, A, B, 0, PARTS == 2 ? 3 * pairs : pairs,
+      sm, A, B, (int)((int64_t)total * part / a.splits), (int)((int64_t)total * (part + 1) / a.splits),
       [&](int p, const char*& pa, const char*& pb) {
         p = __builtin_amdgcn_readfirstlane(p);
         const int seg = PARTS == 2 ? (p >= pairs) + (p >= 2 * pairs) : 2;
@@ -185,13 +248,25 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(S
         return kbytes - (p - seg * pairs) * nt::kPair;
       },
       acc);
-  // through LDS as in the linear layers: each lane its own slots
-  constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;
-  static_assert(TJ % 4 == 0 && 16 * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
-  f32x4* stage = reinterpret_cast<f32x4*>(&sm) + threadIdx.x;
-  const int64_t col = j0 + G::col_of();
+  // through LDS and four rows at a time, as in the linear layers
+  constexpr int HI = TI < 4 ? TI : TI % 4 == 0 ? 4 : 3, PC = TJ % 4 == 0 ? 4 : 2, V = TJ / PC;
+  typedef __attribute__((ext_vector_type(PC))) float Slot;
+  static_assert(TI % HI == 0 && TJ % 2 == 0 && sizeof(Slot) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
+  Slot* stage = reinterpret_cast<Slot*>(&sm) + threadIdx.x;
+  const int64_t col = j0 + G::col_of(), first = i0 + G::row_of(0, 0);
   const int64_t r8 = (a.rows + 7) / 8 * 8, c8 = (a.cols + 7) / 8 * 8;
-  const int wide = (int)min((int64_t)TJ, max((int64_t)0, c8 - col));  // columns stored (zeros among them)
+  const int wide = (int)min((int64_t)TJ, max((int64_t)0, c8 - col));
+  Halves<TJ> dh[4], dl[4];
+  const bool add = a.D.hi != nullptr && a.sums == nullptr && wide > 0;
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t at = z * a.D.stride + min(first + i * 16 + r, a.rows - 1) * a.D.ld + col;
+      dh[r].load(a.D.hi + at, wide);
+      if (PARTS == 2) dl[r].load(a.D.lo + at, wide);
+    }
+  };
+  if (add) fetch(0);
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
 #pragma unroll
@@ -199,44 +274,88 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(S
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          stage[((i * 4 + r) * V + v) * nt::kThreads] =
-              f32x4{acc[h * HI + i][4 * v][r], acc[h * HI + i][4 * v + 1][r], acc[h * HI + i][4 * v + 2][r],
-                    acc[h * HI + i][4 * v + 3][r]};
+        for (int v = 0; v < V; ++v) {
+          Slot s;
+#pragma unroll
+          for (int e = 0; e < PC; ++e) s[e] = acc[h * HI + i][PC * v + e][r];
+          stage[((i * 4 + r) * V + v) * nt::kThreads] = s;
+        }
 #pragma unroll 1
     for (int q = 0; q < HI; ++q) {
-      const int64_t row = i0 + G::row_of(h * HI + q, 0);  // four rows, TJ columns
-      if (row >= r8 || wide <= 0) continue;
+      const int i = h * HI + q;
+      const int64_t row = first + i * 16;  // four rows, TJ columns
       float f[4][TJ];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const f32x4 x = stage[((q * 4 + r) * V + v) * nt::kThreads];
+          const Slot s = stage[((q * 4 + r) * V + v) * nt::kThreads];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) f[r][4 * v + e] = a.alpha * x[e];
+          for (int e = 0; e < PC; ++e) f[r][PC * v + e] = s[e];
         }
-      if (a.D.hi != nullptr) {
+      if (a.sums != nullptr) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (row + r < a.rows) {
-            const int64_t at = z * a.D.stride + (row + r) * a.D.ld + col;
+            float* o = a.sums + (((int64_t)part * gridDim.y + z) * a.rows + row + r) * c8 + col;
             if (wide == TJ) {
-              uint16_t d[TJ], e[TJ];
-              __builtin_memcpy(d, a.D.hi + at, sizeof d);
-              if (PARTS == 2) __builtin_memcpy(e, a.D.lo + at, sizeof e);
-#pragma unroll
-              for (int j = 0; j < TJ; ++j) f[r][j] += a.beta * (f16_f32(d[j]) + (PARTS == 2 ? f16_f32(e[j]) : 0.0f));
+              __builtin_memcpy(o, f[r], sizeof f[r]);
             } else {
 #pragma unroll
-              for (int j = 0; j < TJ; ++j)
-                if (j < wide)
-                  f[r][j] += a.beta * (f16_f32(a.D.hi[at + j]) + (PARTS == 2 ? f16_f32(a.D.lo[at + j]) : 0.0f));
+              for (int j = 0; j < TJ - 1; ++j)
+                if (j < wide) o[j] = f[r][j];
             }
           }
+        continue;
       }
-      if (a.user != nullptr) {
-        const int64_t base = z * a.su;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) f[r][j] *= a.alpha;
+      if (add) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float b = row + r < a.rows ? a.beta : 0.0f;  // (rows beyond: zeros, not the last row's)
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) f[r][j] += b * (dh[r].get(j) + (PARTS == 2 ? dl[r].get(j) : 0.0f));
+        }
+        if (i + 1 < TI) fetch(i + 1);
+      }
+      if (row >= r8 || wide <= 0) continue;
+      if (a.user == nullptr) {
+        const Parts& t = SYM ? a.o : a.t;
+        store_parts<PARTS, TJ>(f, row, a.rows, col, a.cols, wide, a.o, !SYM || ti != tj ? &t : nullptr, z);
+        continue;
+      }
+      const int64_t base = z * a.su;
+      const bool inside = row + 4 <= a.rows && col + TJ <= a.cols;
+      if (inside && a.sj == 1) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (a.bf16) {
+            uint32_t o[TJ / 2];
+#pragma unroll
+            for (int j = 0; j < TJ / 2; ++j)
+              o[j] = (uint32_t)f32_to_bf16(f[r][2 * j]) | ((uint32_t)f32_to_bf16(f[r][2 * j + 1]) << 16);
+            __builtin_memcpy((bf16_t*)a.user + base + (row + r) * a.si + col, o, sizeof o);
+          } else {
+            __builtin_memcpy((float*)a.user + base + (row + r) * a.si + col, f[r], sizeof f[r]);
+          }
+        }
+      } else if (inside && a.si == 1) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+          const int64_t at = base + row + (col + j) * a.sj;
+          if (a.bf16) {
+            const uint32_t o[2] = {(uint32_t)f32_to_bf16(f[0][j]) | ((uint32_t)f32_to_bf16(f[1][j]) << 16),
+                                   (uint32_t)f32_to_bf16(f[2][j]) | ((uint32_t)f32_to_bf16(f[3][j]) << 16)};
+            __builtin_memcpy((bf16_t*)a.user + at, o, sizeof o);
+          } else {
+            const float o[4] = {f[0][j], f[1][j], f[2][j], f[3][j]};
+            __builtin_memcpy((float*)a.user + at, o, sizeof o);
+          }
+        }
+      } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -248,70 +367,129 @@ __global__ __launch_bounds__(nt::kThreads, (TI * TJ > 32 ? 1 : 2)) void k_step(S
               else
                 ((float*)a.user)[at] = f[r][j];
             }
-        continue;
-      }
-      uint16_t hi[4][TJ], lo[4][TJ];
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-          hi[r][j] = f16_bits(f[r][j]);
-          lo[r][j] = PARTS == 2 ? f16_bits(f[r][j] - f16_f32(hi[r][j])) : (uint16_t)0;
-        }
-      // by rows: TJ consecutive columns of each
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (row + r < a.rows) {
-          const int64_t at = z * a.o.stride + (row + r) * a.o.ld + col;
-          if (wide == TJ) {
-            __builtin_memcpy(a.o.hi + at, hi[r], sizeof hi[r]);
-            if (PARTS == 2) __builtin_memcpy(a.o.lo + at, lo[r], sizeof lo[r]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < TJ; ++j)
-              if (j < wide) {
-                a.o.hi[at + j] = hi[r][j];
-                if (PARTS == 2) a.o.lo[at + j] = lo[r][j];
-              }
-          }
-        }
-      // by columns: four consecutive rows of each (rows of `t` hold r8 entries)
-      if (SYM ? ti != tj : a.t.hi != nullptr) {
-        const Parts& t = SYM ? a.o : a.t;
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          if (col + j < a.cols) {
-            const int64_t at = z * t.stride + (col + j) * t.ld + row;
-            const uint16_t vh[4] = {hi[0][j], hi[1][j], hi[2][j], hi[3][j]};
-            put4(t.hi + at, vh);
-            if (PARTS == 2) {
-              const uint16_t vl[4] = {lo[0][j], lo[1][j], lo[2][j], lo[3][j]};
-              put4(t.lo + at, vl);
-            }
-          }
       }
     }
   }
 }
 
-template <int PARTS, bool SYM>
-hipError_t step_for(StepArgs a, int64_t batch, hipStream_t s) {
-  auto tiles = [&](int64_t b) {
-    const int64_t mt = (a.rows + b - 1) / b, ntl = (a.cols + b - 1) / b;
-    return SYM ? mt * (mt + 1) / 2 : mt * ntl;
-  };
-  const bool big = tiles(256) * batch >= 128;
-  const int b = big ? 256 : 128;
-  a.mt = (int)((a.rows + b - 1) / b);
-  a.ntl = (int)((a.cols + b - 1) / b);
-  const int64_t wgs = tiles(b);
-  if (wgs > 0x7fffffff || batch > 65535) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)wgs, (uint32_t)batch);
-  if (big)
-    hipLaunchKernelGGL((k_step<PARTS, 8, 8, SYM>), grid, dim3(nt::kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_step<PARTS, 4, 4, SYM>), grid, dim3(nt::kThreads), 0, s, a);
+// The symmetric product's partial sums (tiles of `edge` on and above the
+// diagonal) added in their order: four columns of a row a thread, those below
+// the diagonal's tiles read across it.
+template <int PARTS>
+__global__ __launch_bounds__(256) void k_step_join(StepArgs a, int edge) {
+  const int64_t c8 = (a.cols + 7) / 8 * 8, q4 = c8 / 4, z = blockIdx.y;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / q4, col = id % q4 * 4;
+  if (row >= a.rows) return;
+  const bool upper = row / edge <= col / edge;
+  const int64_t step = (int64_t)gridDim.y * a.rows * c8;
+  const float* p = a.sums + z * a.rows * c8;
+  float f[4] = {};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    float v[4] = {};
+    if (upper) {
+      __builtin_memcpy(v, p + s * step + row * c8 + col, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col + j < a.rows) v[j] = p[s * step + (col + j) * c8 + row];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] += v[j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] *= a.alpha;
+  Halves<4> hi, lo;
+  split_parts<4>(f, hi, lo);
+  const int64_t at = z * a.o.stride + row * a.o.ld + col;
+  hi.store(a.o.hi + at, 4);
+  if (PARTS == 2) lo.store(a.o.lo + at, 4);
+}
+
+// The fastest form of a product by a model of the forms' times (us), as for the
+// linear layers: per pair of k `pair` with a compute unit to itself, `loaded`
+// with all of them busy, `ends` for a tile's start and epilogue.
+struct StepForm {
+  int ti, tj, slots, wgs;
+  double pair, loaded, ends;
+};
+struct StepPlan {
+  int form, splits;
+};
+constexpr StepForm kSymForms[] = {{8, 8, 2, 1, 1.41, 1.41, 10.0}, {6, 6, 2, 1, 0.85, 0.85, 8.0},
+                                  {4, 4, 4, 1, 0.37, 0.53, 4.0}, {2, 2, 5, 2, 0.17, 0.30, 2.0}};
+constexpr StepForm kAnyForms[] = {{8, 8, 2, 1, 1.41, 1.41, 10.0}, {6, 6, 2, 1, 0.85, 0.85, 8.0},
+                                  {4, 4, 2, 2, 0.52, 0.80, 6.0}, {4, 4, 4, 1, 0.40, 0.62, 4.0},
+                                  {2, 4, 3, 2, 0.25, 0.50, 3.0}};
+
+StepPlan step_plan(bool sym, bool may_split, int64_t rows, int64_t cols, int64_t k, int64_t batch, int parts) {
+#ifdef FF_DEV
+  if (const char* v = getenv(sym ? may_split ? "FF_GRAM" : "FF_SQUARE" : "FF_STEP")) {
+    StepPlan p{};
+    if (sscanf(v, "%d,%d", &p.form, &p.splits) == 2) return p;
+  }
+#endif
+  const int64_t pairs = (k * 2 + nt::kPair - 1) / nt::kPair * (parts == 2 ? 3 : 1);
+  StepPlan best{0, 1};
+  double least = 1e300;
+  const int forms = sym ? 4 : 5;
+  for (int q = 0; q < forms; ++q) {
+    const StepForm& f = sym ? kSymForms[q] : kAnyForms[q];
+    const int64_t mt = (rows + 32 * f.ti - 1) / (32 * f.ti), ntl = (cols + 32 * f.tj - 1) / (32 * f.tj);
+    const int64_t tiles = (sym ? mt * (mt + 1) / 2 : mt * ntl) * batch;
+    for (int s : {1, 2, 4, 8, 16}) {
+      if (s > 1 && (!may_split || s * 4 > pairs || tiles * s > 512)) break;
+      const int64_t wgs = tiles * s, rounds = (wgs + 256 * f.wgs - 1) / (256 * f.wgs);
+      double us = (double)rounds * (f.ends + (double)((pairs + s - 1) / s) * (wgs > 256 ? f.loaded : f.pair));
+      if (s > 1) us += 6.0 + 8.0 * (double)s * (double)(batch * rows * rows) / 4e6;
+      if (us < least) {
+        least = us;
+        best = {q, s};
+      }
+    }
+  }
+  return best;
+}
+
+template <int PARTS, int TI, int TJ, int SLOTS, bool SYM>
+hipError_t step_tiles(StepArgs a, int64_t batch, hipStream_t s) {
+  constexpr int BM = 32 * TI, BN = 32 * TJ;
+  a.mt = (int)((a.rows + BM - 1) / BM);
+  a.ntl = (int)((a.cols + BN - 1) / BN);
+  const int64_t tiles = SYM ? (int64_t)a.mt * (a.mt + 1) / 2 : (int64_t)a.mt * a.ntl;
+  if (tiles * a.splits > 0x7fffffff || batch > 65535) return hipErrorInvalidValue;
+  a.tiles = (int)tiles;
+  hipLaunchKernelGGL((k_step<PARTS, TI, TJ, SLOTS, SYM>), dim3((uint32_t)(tiles * a.splits), (uint32_t)batch),
+                     dim3(nt::kThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t threads = a.rows * ((a.cols + 7) / 8 * 2);
+  hipLaunchKernelGGL(k_step_join<PARTS>, dim3((uint32_t)((threads + 255) / 256), (uint32_t)batch), dim3(256), 0, s, a,
+                     BM);
   return hipGetLastError();
+}
+
+template <int PARTS>
+hipError_t sym_step(StepArgs a, const StepPlan& p, float* sums, int64_t batch, hipStream_t s) {
+  a.splits = p.splits;
+  a.sums = p.splits > 1 ? sums : nullptr;
+  switch (p.form) {
+    case 0: return step_tiles<PARTS, 8, 8, 2, true>(a, batch, s);
+    case 1: return step_tiles<PARTS, 6, 6, 2, true>(a, batch, s);
+    case 2: return step_tiles<PARTS, 4, 4, 4, true>(a, batch, s);
+    default: return step_tiles<PARTS, 2, 2, 5, true>(a, batch, s);
+  }
+}
+template <int PARTS>
+hipError_t any_step(StepArgs a, const StepPlan& p, int64_t batch, hipStream_t s) {
+  a.splits = 1;
+  switch (p.form) {
+    case 0: return step_tiles<PARTS, 8, 8, 2, false>(a, batch, s);
+    case 1: return step_tiles<PARTS, 6, 6, 2, false>(a, batch, s);
+    case 2: return step_tiles<PARTS, 4, 4, 2, false>(a, batch, s);
+    case 3: return step_tiles<PARTS, 4, 4, 4, false>(a, batch, s);
+    default: return step_tiles<PARTS, 2, 4, 3, false>(a, batch, s);
+  }
 }
 
 // Largest |b u + c u^2| for u in [0, top].
@@ -360,6 +538,7 @@ float scale_for(double bound) {
 
 struct Buffers {
   double* part;
+  float* sums;  // partial sums of the first product
   Parts x[2], t[2], gram, poly;
   size_t bytes;
 };
@@ -388,19 +567,280 @@ Buffers layout(int64_t batch, int64_t m, int64_t n, int parts, char* base) {
     b.x[k] = operand(r, ldc);
     b.t[k] = operand(c, ldr);
   }
+  const int splits = step_plan(true, true, r, r, (c + 7) / 8 * 8, batch, parts).splits;
+  if (splits > 1) b.sums = (float*)take((size_t)splits * (size_t)(batch * r * ((r + 7) / 8 * 8)) * sizeof(float));
   b.gram = operand(r, ldr);
   b.poly = operand(r, ldr);
   b.bytes = off;
   return b;
 }
 
+// ------------------------------------------------------------ small matrices
+// All steps of one matrix in one workgroup of 16 waves, everything in LDS: X by
+// rows and by columns and one r x r matrix (A, then b A + c A A in its place),
+// each in PARTS fp16 parts with rows of whole 64-byte steps of k plus 16 bytes
+// (16 consecutive rows at one k then start in different banks).  A wave takes
+// whole 16 x 16 tiles; what it computes replaces an operand of the others, so
+// it stays in registers until all of them are done (LIMIT tiles a wave).  The matrices are symmetric:
+// a lane's four consecutive rows of one column are stored as four consecutive
+// columns of one row.
+constexpr int kSmallThreads = 1024;
+constexpr int small_tiles(int parts) { return parts == 2 ? 4 : 8; }  // a wave, what LDS holds
+constexpr size_t kSmallLds = 160 * 1024 - 256;
+
+struct SmallLayout {
+  int rp, cp;        // rows of X and X^T: multiples of 16
+  int ldx, ldr;      // elements
+  size_t x, t, a, bytes;  // parts of X, X^T and A: offsets of the first, bytes of one
+};
+__host__ __device__ inline SmallLayout small_layout(int r, int c, int parts) {
+  SmallLayout s{};
+  s.rp = (r + 15) / 16 * 16;
+  s.cp = (c + 15) / 16 * 16;
+  s.ldx = (c + 31) / 32 * 32 + 8;
+  s.ldr = (r + 31) / 32 * 32 + 8;
+  s.x = (size_t)s.rp * s.ldx * 2;
+  s.t = (size_t)s.cp * s.ldr * 2;
+  s.a = (size_t)s.rp * s.ldr * 2;
+  s.bytes = (s.x + s.t + s.a) * (size_t)parts;
+  return s;
+}
+bool small_fits(int64_t m, int64_t n, int parts) {
+  const int64_t r = std::min(m, n), c = std::max(m, n);
+  if (c > 4096) return false;
+  const SmallLayout s = small_layout((int)r, (int)c, parts);
+  return s.bytes <= kSmallLds && (s.rp / 16) * (s.cp / 16) <= small_tiles(parts) * (kSmallThreads / 64);
+}
+
+// Parts with which a matrix is taken here, 0: not at all.  Two where they fit,
+// for bf16 too: few directions average few roundings, and a near-singular
+// small matrix with one part was off by 5e-3 instead of the 1.7e-3 of its
+// own rounding.
+int small_parts(int64_t m, int64_t n, bool bf16) { return small_fits(m, n, 2) ? 2 : bf16 && small_fits(m, n, 1) ? 1 : 0; }
+
+struct SmallArgs {
+  int r, c, steps, tall, bf16;
+  const void* g;
+  int64_t ldg, sg;
+  void* out;
+  int64_t ldo, so;
+  float a, b, c5, scale, sx, sa, sb;  // coefficients, the result's scale, the operands' scales
+  double eps;
+};
+
+template <class E, int PARTS>
+__global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
+  extern __shared__ char lds[];
+  __shared__ double share[kSmallThreads / 64];
+  const SmallLayout S = small_layout(a.r, a.c, PARTS);
+  char* const X = lds;
+  char* const T = X + S.x * PARTS;
+  char* const A = T + S.t * PARTS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int W = kSmallThreads / 64, LIMIT = small_tiles(PARTS);
+  const E* g = (const E*)a.g + blockIdx.x * a.sg;
+  const int m = a.tall ? a.c : a.r, n = a.tall ? a.r : a.c;
+  for (size_t o = (size_t)tid * 16; o < S.bytes; o += kSmallThreads * 16) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0, 0, 0, 0};
+  // f(row, column, value) of this thread's elements of G, eight loads at a time
+  auto elements = [&](auto f) {
+    int i[8], j[8];
+    i[0] = tid / n;
+    j[0] = tid - i[0] * n;
+    const int di = kSmallThreads / n, dj = kSmallThreads - di * n;
+    for (int id = tid; id < m * n; id += 8 * kSmallThreads) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k > 0) {
+          i[k] = i[k - 1] + di;
+          j[k] = j[k - 1] + dj;
+          if (j[k] >= n) {
+            j[k] -= n;
+            ++i[k];
+          }
+        }
+        v[k] = i[k] < m ? Elem<E>::to_f32(g[(int64_t)i[k] * a.ldg + j[k]]) : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (i[k] < m) f(i[k], j[k], v[k]);
+      i[0] = i[7] + di;
+      j[0] = j[7] + dj;
+      if (j[0] >= n) {
+        j[0] -= n;
+        ++i[0];
+      }
+    }
+  };
+  double ss = 0.0;
+  elements([&](int, int, float v) { ss += (double)v * (double)v; });
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) ss += __shfl_xor(ss, d);
+  if (lane == 0) share[wave] = ss;
+  __syncthreads();
+  ss = 0.0;
+  for (int k = 0; k < W; ++k) ss += share[k];
+  const double inv = 1.0 / (sqrt(ss) + a.eps);
+  // part q of element (i, j) of a matrix whose parts are `size` bytes apart
+  auto at = [](char* M, size_t size, int ld, int q, int i, int j) {
+    return reinterpret_cast<uint16_t*>(M + q * size) + i * ld + j;
+  };
+  elements([&](int gi, int gj, float x) {
+    const int i = a.tall ? gj : gi, j = a.tall ? gi : gj;
+    const float v = (float)((double)x * inv) * a.sx;
+    const uint16_t hi = f16_bits(v), lo = f16_bits(v - f16_f32(hi));
+    *at(X, S.x, S.ldx, 0, i, j) = *at(T, S.t, S.ldr, 0, j, i) = hi;
+    if (PARTS == 2) *at(X, S.x, S.ldx, 1, i, j) = *at(T, S.t, S.ldr, 1, j, i) = lo;
+  });
+  __syncthreads();
+  // a 16 x 16 tile of P Q^T, rows p0.. of P and q0.. of Q, k elements
+  auto product = [&](char* P, size_t ps, int ldp, int p0, char* Q, size_t qs, int ldq, int q0, int k) {
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, low = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int kc = 8 * (lane >> 4);
+    auto frag = [&](char* M, size_t size, int ld, int row, int q, int kk) {
+      return *reinterpret_cast<const u32x4*>(at(M, size, ld, q, row + (lane & 15), kk + kc));
+    };
+    for (int kk = 0; kk < k; kk += 32) {
+      const u32x4 ph = frag(P, ps, ldp, p0, 0, kk), qh = frag(Q, qs, ldq, q0, 0, kk);
+      if (PARTS == 2) {
+        const u32x4 pl = frag(P, ps, ldp, p0, 1, kk), ql = frag(Q, qs, ldq, q0, 1, kk);
+        low = nt::F16::mfma(ph, ql, low);
+        low = nt::F16::mfma(pl, qh, low);
+      }
+      acc = nt::F16::mfma(ph, qh, acc);
+    }
+    return acc + low;
+  };
+  auto put4 = [&](char* M, size_t size, int ld, int i, int j, const float (&f)[4]) {
+    Halves<4> hi, lo;
+    split_parts<4>(f, hi, lo);
+    hi.store(at(M, size, ld, 0, i, j), 4);
+    if (PARTS == 2) lo.store(at(M, size, ld, 1, i, j), 4);
+  };
+  auto get4 = [&](char* M, size_t size, int ld, int i, int j, float (&f)[4]) {
+    Halves<4> hi, lo;
+    hi.load(at(M, size, ld, 0, i, j), 4);
+    if (PARTS == 2) lo.load(at(M, size, ld, 1, i, j), 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = hi.get(e) + (PARTS == 2 ? lo.get(e) : 0.0f);
+  };
+  // (opaque, or every tile's addresses are computed ahead and held)
+  auto tile_of = [&](int u) {
+    int q = wave + u * W;
+    asm volatile("" : "+s"(q));
+    return q;
+  };
+  const int rt = S.rp / 16, ct = S.cp / 16, kr = S.ldr - 8, kc = S.ldx - 8;
+  const int lr = 4 * (lane >> 4), lc = lane & 15;  // a lane's first row and its column in a tile
+  for (int step = 0; step < a.steps; ++step) {
+    for (int q = wave; q < rt * rt; q += W) {
+      const int i0 = q / rt * 16, j0 = q % rt * 16;
+      const f32x4 s = product(X, S.x, S.ldx, i0, X, S.x, S.ldx, j0, kc);
+      const float al = a.sa / (a.sx * a.sx), f[4] = {al * s[0], al * s[1], al * s[2], al * s[3]};
+      put4(A, S.a, S.ldr, j0 + lc, i0 + lr, f);
+    }
+    __syncthreads();
+    float keep[LIMIT][4];
+#pragma unroll
+    for (int u = 0; u < LIMIT; ++u) {
+      const int q = tile_of(u);
+      if (q < rt * rt) {
+        const int i0 = q / rt * 16, j0 = q % rt * 16;
+        const f32x4 s = product(A, S.a, S.ldr, i0, A, S.a, S.ldr, j0, kr);
+        float d[4];
+        get4(A, S.a, S.ldr, j0 + lc, i0 + lr, d);
+        const float al = a.c5 * a.sb / (a.sa * a.sa), be = a.b * a.sb / a.sa;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[u][e] = al * s[e] + be * d[e];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < LIMIT; ++u) {
+      const int q = tile_of(u);
+      if (q < rt * rt) put4(A, S.a, S.ldr, q % rt * 16 + lc, q / rt * 16 + lr, keep[u]);
+    }
+    __syncthreads();
+    const bool last = step + 1 == a.steps;
+#pragma unroll
+    for (int u = 0; u < LIMIT; ++u) {
+      const int q = tile_of(u);
+      if (q < rt * ct) {
+        const int i0 = q / ct * 16, j0 = q % ct * 16;
+        const f32x4 s = product(A, S.a, S.ldr, i0, T, S.t, S.ldr, j0, kr);
+        float d[4];
+        get4(T, S.t, S.ldr, j0 + lc, i0 + lr, d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[u][e] = s[e] * (1.0f / a.sb) + a.a * d[e];
+        if (last) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = i0 + lr + e, j = j0 + lc;
+            if (i < a.r && j < a.c) {
+              const int64_t o = blockIdx.x * a.so + (a.tall ? (int64_t)j * a.ldo + i : (int64_t)i * a.ldo + j);
+              ((E*)a.out)[o] = Elem<E>::from_f32(keep[u][e] * (a.scale / a.sx));
+            }
+          }
+        }
+      }
+    }
+    if (last) break;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < LIMIT; ++u) {
+      const int q = tile_of(u);
+      if (q < rt * ct) {
+        const int i = q / ct * 16 + lr, j = q % ct * 16 + lc;
+        put4(T, S.t, S.ldr, j, i, keep[u]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint16_t hi = f16_bits(keep[u][e]);
+          *at(X, S.x, S.ldx, 0, i + e, j) = hi;
+          if (PARTS == 2) *at(X, S.x, S.ldx, 1, i + e, j) = f16_bits(keep[u][e] - f16_f32(hi));
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int PARTS, class E>
+hipError_t run_small(const OrthoArgs& a, float sx, float sa, float sb, hipStream_t s) {
+  SmallArgs q{};
+  q.tall = a.m > a.n;
+  q.r = (int)std::min(a.m, a.n);
+  q.c = (int)std::max(a.m, a.n);
+  q.steps = a.steps;
+  q.g = a.g;
+  q.ldg = a.ldg;
+  q.sg = a.sg;
+  q.out = a.out;
+  q.ldo = a.ldo;
+  q.so = a.so;
+  q.a = a.a;
+  q.b = a.b;
+  q.c5 = a.c;
+  q.scale = a.scale;
+  q.sx = sx;
+  q.sa = sa;
+  q.sb = sb;
+  q.eps = (double)a.eps;
+  hipLaunchKernelGGL((k_small<E, PARTS>), dim3((uint32_t)a.batch), dim3(kSmallThreads),
+                     (uint32_t)small_layout(q.r, q.c, PARTS).bytes, s, q);
+  return hipGetLastError();
+}
+
 template <int PARTS, class E>
 hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
+  const double most = iterates_bound(a.steps, a.a, a.b, a.c);
+  const float sx = scale_for(most), sa = scale_for(most * most), sb = scale_for(quad_bound(a.b, a.c, most * most));
+  const int small = small_parts(a.m, a.n, a.bf16);
+  if (small == 2) return run_small<2, E>(a, sx, sa, sb, s);
+  if constexpr (PARTS == 1)
+    if (small == 1) return run_small<1, E>(a, sx, sa, sb, s);
   const bool tall = a.m > a.n;
   const int64_t r = std::min(a.m, a.n), c = std::max(a.m, a.n);
   Buffers w = layout(a.batch, a.m, a.n, PARTS, (char*)workspace);
-  const double most = iterates_bound(a.steps, a.a, a.b, a.c);
-  const float sx = scale_for(most), sa = scale_for(most * most), sb = scale_for(quad_bound(a.b, a.c, most * most));
   const int parts = (int)std::min<int64_t>(kNormParts, (a.m * ((a.n + 7) / 8) + 255) / 256);
   hipLaunchKernelGGL(k_square_sums<E>, dim3((uint32_t)parts, (uint32_t)a.batch), dim3(256), 0, s, (const E*)a.g,
                      a.ldg, a.sg, a.m, a.n, w.part);
@@ -412,6 +852,9 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
                      tall ? w.t[0] : w.x[0], tall ? w.x[0] : w.t[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t r8 = (r + 7) / 8 * 8, c8 = (c + 7) / 8 * 8;
+  const StepPlan gram = step_plan(true, true, r, r, c8, a.batch, PARTS);
+  const StepPlan square = step_plan(true, false, r, r, r8, a.batch, PARTS);
+  const StepPlan apply = step_plan(false, false, r, c, r8, a.batch, PARTS);
   for (int k = 0; k < a.steps; ++k) {
     const int cur = k & 1, nxt = cur ^ 1;
     StepArgs q{};
@@ -420,13 +863,13 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
     q.L = q.R = w.x[cur];
     q.o = w.gram;
     q.alpha = sa / (sx * sx);
-    if ((e = step_for<PARTS, true>(q, a.batch, s)) != hipSuccess) return e;
+    if ((e = sym_step<PARTS>(q, gram, w.sums, a.batch, s)) != hipSuccess) return e;
     q.k = r8;
     q.L = q.R = q.D = w.gram;
     q.o = w.poly;
     q.alpha = a.c * sb / (sa * sa);
     q.beta = a.b * sb / sa;
-    if ((e = step_for<PARTS, true>(q, a.batch, s)) != hipSuccess) return e;
+    if ((e = sym_step<PARTS>(q, square, nullptr, a.batch, s)) != hipSuccess) return e;
     q.cols = c;
     q.L = w.poly;
     q.R = w.t[cur];
@@ -444,7 +887,7 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
       q.su = a.so;
       q.bf16 = a.bf16;
     }
-    if ((e = step_for<PARTS, false>(q, a.batch, s)) != hipSuccess) return e;
+    if ((e = any_step<PARTS>(q, apply, a.batch, s)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -454,13 +897,14 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
 bool ortho_bounded(int steps, double a, double b, double c) { return iterates_bound(steps, a, b, c) < 16.0; }
 
 size_t ortho_workspace(int64_t batch, int64_t m, int64_t n, bool bf16) {
+  if (small_parts(m, n, bf16) != 0) return 0;
   return layout(batch, m, n, bf16 ? 1 : 2, nullptr).bytes;
 }
 
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t s) {
   // 2^20: the operands' rows stay within nt::kMaxRowBytes, the grid within its limits
   if (a.batch <= 0 || a.batch > 65535 || a.m <= 0 || a.n <= 0 || std::max(a.m, a.n) > (1 << 20) || a.steps <= 0 ||
-      workspace == nullptr || (uintptr_t)workspace % 256 != 0 || !ortho_bounded(a.steps, a.a, a.b, a.c))
+      (workspace == nullptr && small_parts(a.m, a.n, a.bf16) == 0) || (uintptr_t)workspace % 256 != 0 || !ortho_bounded(a.steps, a.a, a.b, a.c))
     return hipErrorInvalidValue;
   return a.bf16 ? run<1, bf16_t>(a, workspace, s) : run<2, float>(a, workspace, s);
 }

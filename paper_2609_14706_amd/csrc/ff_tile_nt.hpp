@@ -184,11 +184,11 @@ struct Tile {
     }
   }
 
-  // 256 accumulator registers are exactly the accumulation file.  Said before
+  // The accumulators of a large tile belong in the accumulation file.  Said before
   // and after the loop, it keeps the compiler from carrying other registers'
   // wishes through it, at the price of 100 to 300 moves a pair.
   static __device__ __forceinline__ void pin(Acc& acc) {
-    if (TI * TJ == 64) {
+    if (TI * TJ >= 36) {
 #pragma unroll
       for (int i = 0; i < TI; ++i)
 #pragma unroll

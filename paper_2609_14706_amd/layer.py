@@ -89,7 +89,7 @@ def _library():
 _ELEM = {torch.float32: 0, torch.bfloat16: 1}   # ff_dtype
 
 
-def _rows(t, name, dtype, device, cols=None, rows=None):
+def _rows(t, name, dtype, device, cols=None):
     """(pointer, leading dimension, rows, columns) of a tensor's rows."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
@@ -97,22 +97,24 @@ def _rows(t, name, dtype, device, cols=None, rows=None):
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, not on {t.device}")
-    d = t.dim()
-    if d == 0:
+    shape = t.shape
+    if not shape:
         raise ValueError(f"{name} must have at least one dimension")
-    c = t.shape[-1]
-    if t.is_contiguous():
-        r, ld = (t.numel() // c if c else t.shape[:-1].numel()), c
-    elif d == 2 and (c == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= c):
-        r = t.shape[0]
-        ld = t.stride(0) if r > 1 else c
-    else:
-        raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows that do not overlap")
+    c = shape[-1]
     if cols is not None and c != cols:
         raise ValueError(f"{name} must have rows of {cols} elements, not {c}")
-    if rows is not None and r != rows:
-        raise ValueError(f"{name} must have {rows} rows, not {r}")
-    return t.data_ptr(), ld, r, c
+    if t.is_contiguous():
+        return t.data_ptr(), c, (t.numel() // c if c else shape[:-1].numel()), c
+    if len(shape) != 2 or (c != 1 and t.stride(1) != 1) or (shape[0] != 1 and t.stride(0) < c):
+        raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows that do not overlap")
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else c), shape[0], c
+
+
+def _like(t, dtype):
+    """A new contiguous tensor of t's shape."""
+    if t.is_contiguous():
+        return torch.empty_like(t, dtype=dtype)
+    return torch.empty(t.shape, dtype=dtype, device=t.device)
 
 
 def _vector(t, name, dtype, device, count):
@@ -204,17 +206,17 @@ def _norm(x, weight, residual, eps, col_scale, q8, normalise):
             raise ValueError(f"residual must have x's shape {tuple(x.shape)}")
         a.residual, a.ldr, _, _ = _rows(residual, "residual", x.dtype, dev, c)
         if normalise:
-            s = torch.empty(x.shape, dtype=x.dtype, device=dev)
+            s = _like(x, x.dtype)
             a.sum, a.ldsum = s.data_ptr(), c
     a.weight = _vector(weight, "weight", x.dtype, dev, c)
     a.eps, a.normalise = eps, normalise
     if q8:
-        y = torch.empty(x.shape, dtype=torch.int8, device=dev)
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+        y = _like(x, torch.int8)
+        scale = torch.empty((r,) if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=dev)
         a.col_scale = _vector(col_scale, "col_scale", torch.float32, dev, c)
         a.q, a.ldq, a.q_scale = y.data_ptr(), c, scale.data_ptr()
     else:
-        y, scale = torch.empty(x.shape, dtype=x.dtype, device=dev), None
+        y, scale = _like(x, x.dtype), None
         a.y, a.ldy = y.data_ptr(), c
     if r:
         _launch("ff_rms_norm", a, dev)
@@ -267,11 +269,11 @@ def rms_norm_backward(dy, s, weight=None, *, eps: float = 1e-6, dsum=None, works
         a.dsum, a.lddsum, _, _ = _rows(dsum, "dsum", s.dtype, dev, c)
     a.weight = _vector(weight, "weight", s.dtype, dev, c)
     a.eps = eps
-    ds = torch.empty(s.shape, dtype=s.dtype, device=dev)
+    ds = _like(s, s.dtype)
     a.ds, a.ldds = ds.data_ptr(), c
     dw = None
     if weight is not None:
-        dw = torch.empty(weight.shape, dtype=s.dtype, device=dev)
+        dw = torch.empty_like(weight)
         a.dweight = dw.data_ptr()
     keep = _workspace(a, _bytes("ff_rms_norm_backward_workspace_size", a), workspace, dev)
     _launch("ff_rms_norm_backward", a, dev)
@@ -294,7 +296,7 @@ def _linear(name, x, weight, dtype, x_scale, row_scale, bias, residual, activati
         a.row_scale = _vector(row_scale, "row_scale", torch.float32, dev, m)
     if bias is not None:
         a.bias = _vector(bias, "bias", bf16, dev, m)
-    shape = x.shape[:-1] + (m,)
+    shape = (T, m) if x.dim() == 2 else x.shape[:-1] + (m,)
     if residual is not None:
         if residual.shape != shape:
             raise ValueError(f"residual must have the output's shape {tuple(shape)}")
@@ -304,7 +306,7 @@ def _linear(name, x, weight, dtype, x_scale, row_scale, bias, residual, activati
     a.y, a.ldy = y.data_ptr(), m
     z = None
     if keep_preact:
-        z = torch.empty(shape, dtype=bf16, device=dev)
+        z = torch.empty_like(y)
         a.preact, a.ldz = z.data_ptr(), m
     keep = _workspace(a, _bytes("ff_linear_workspace_size", a, int(x_scale is not None)), workspace, dev)
     if T:
@@ -358,7 +360,7 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError("weight must be a 2-D tensor (m, n)")
     pw, ldw, m, _ = _rows(weight, "weight", bf16, dev, n)
-    shape = x.shape[:-1] + (m,)
+    shape = (T, m) if x.dim() == 2 else x.shape[:-1] + (m,)
     if dy.shape != shape:
         raise ValueError(f"dy must have the output's shape {tuple(shape)}")
     pdy, lddy, _, _ = _rows(dy, "dy", bf16, dev, m)
@@ -369,14 +371,14 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
         if preact is None or preact.shape != shape:
             raise ValueError(f"preact of shape {tuple(shape)} is needed with an activation")
         a.preact, a.ldz, _, _ = _rows(preact, "preact", bf16, dev, m)
-        g = torch.empty(shape, dtype=bf16, device=dev)
+        g = _like(dy, bf16)
         a.g, a.ldg = g.data_ptr(), m
     dx = dw = db = None
     if need_input:
-        dx = torch.empty(x.shape, dtype=bf16, device=dev)
+        dx = _like(x, bf16)
         a.dx, a.lddx = dx.data_ptr(), n
     if need_weight:
-        dw = torch.empty((m, n), dtype=bf16, device=dev)
+        dw = _like(weight, bf16)
         a.dw, a.lddw = dw.data_ptr(), n
     if need_bias:
         db = torch.empty(m, dtype=bf16, device=dev)
@@ -411,7 +413,7 @@ def orthogonalize(G, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), 
     if G.dim() == 3 and batch > 1 and G.stride(0) < 0:
         raise ValueError("the matrices of G must follow each other")
     a_, b_, c_ = (float(v) for v in coefficients)
-    out = torch.empty(G.shape, dtype=G.dtype, device=dev)
+    out = _like(G, G.dtype)
     a = ff_ortho_args(batch, m, n, dt, G.data_ptr(), G.stride(-2) if m > 1 else n,
                       G.stride(0) if G.dim() == 3 else m * n, out.data_ptr(), n, m * n, steps, a_, b_, c_, eps, scale)
     keep = _workspace(a, _bytes("ff_orthogonalize_workspace_size", a), workspace, dev)
