@@ -173,6 +173,23 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
                    (uint32_t)(a.ldw * T::kBytes)};
   const int kbytes = (int)(a.n * T::kBytes), pairs = (kbytes + nt::kPair - 1) / nt::kPair;
   const int p0 = (int)((int64_t)pairs * z / splits), p1 = (int)((int64_t)pairs * (z + 1) / splits);
+  const int64_t col = i0 + G::col_of(), row0 = t0 + G::row_of(0, 0);
+  const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
+  const int rows = (int)min((int64_t)G::BM, a.tokens - row0);  // from row0 on (the lane's are 16 apart)
+  const bool vec = B.rows == G::BN || a.m % TJ == 0;           // a lane's columns are all inside or all outside
+  float ws[TJ];
+  Piece<TJ> bias, res[4], more[4];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (i * 16 + r < rows) more[r].load(a.residual + (row0 + i * 16 + r) * a.ldr + col);
+  };
+  const bool fused = vec && P == nullptr && count > 0;
+  if (fused) {
+    if (a.row_scale != nullptr) __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
+    if (a.bias != nullptr) bias.load(a.bias + col);
+    if (a.residual != nullptr) fetch(0);  // (all of these land during the loop)
+  }
   typename G::Acc acc;
   G::zero(acc);
   static_assert(G::BM <= nt::kThreads, "a row a thread");
@@ -197,23 +214,6 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;  // tile rows a phase, pieces of a row
   static_assert(TJ % 4 == 0 && sizeof(S4) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
   S4* stage = reinterpret_cast<S4*>(&sm) + threadIdx.x;
-  const int64_t col = i0 + G::col_of(), row0 = t0 + G::row_of(0, 0);
-  const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
-  const int rows = (int)min((int64_t)G::BM, a.tokens - row0);  // from row0 on (the lane's are 16 apart)
-  const bool vec = B.rows == G::BN || a.m % TJ == 0;           // a lane's columns are all inside or all outside
-  float ws[TJ];
-  Piece<TJ> bias, res[4], more[4];
-  auto fetch = [&](int i) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (i * 16 + r < rows) more[r].load(a.residual + (row0 + i * 16 + r) * a.ldr + col);
-  };
-  const bool fused = vec && P == nullptr && count > 0;
-  if (fused) {
-    if (a.row_scale != nullptr) __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
-    if (a.bias != nullptr) bias.load(a.bias + col);
-    if (a.residual != nullptr) fetch(0);
-  }
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
 #pragma unroll

@@ -231,6 +231,20 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   const int64_t la = z * a.L.stride + i0 * a.L.ld, rb = z * a.R.stride + j0 * a.R.ld;
   const int kbytes = (int)a.k * 2, pairs = (kbytes + nt::kPair - 1) / nt::kPair;
   const int total = PARTS == 2 ? 3 * pairs : pairs;
+  const int64_t col = j0 + G::col_of(), first = i0 + G::row_of(0, 0);
+  const int64_t r8 = (a.rows + 7) / 8 * 8, c8 = (a.cols + 7) / 8 * 8;
+  const int wide = (int)min((int64_t)TJ, max((int64_t)0, c8 - col));
+  Halves<TJ> dh[4], dl[4];
+  const bool add = a.D.hi != nullptr && a.sums == nullptr && wide > 0;
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t at = z * a.D.stride + min(first + i * 16 + r, a.rows - 1) * a.D.ld + col;
+      dh[r].load(a.D.hi + at, wide);
+      if (PARTS == 2) dl[r].load(a.D.lo + at, wide);
+    }
+  };
+  if (add) fetch(0);  // (lands during the loop)
   typename G::Acc acc;
   G::zero(acc);
   // two parts: hi lo, lo hi, then hi hi (the largest last)
@@ -253,20 +267,6 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   typedef __attribute__((ext_vector_type(PC))) float Slot;
   static_assert(TI % HI == 0 && TJ % 2 == 0 && sizeof(Slot) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
   Slot* stage = reinterpret_cast<Slot*>(&sm) + threadIdx.x;
-  const int64_t col = j0 + G::col_of(), first = i0 + G::row_of(0, 0);
-  const int64_t r8 = (a.rows + 7) / 8 * 8, c8 = (a.cols + 7) / 8 * 8;
-  const int wide = (int)min((int64_t)TJ, max((int64_t)0, c8 - col));
-  Halves<TJ> dh[4], dl[4];
-  const bool add = a.D.hi != nullptr && a.sums == nullptr && wide > 0;
-  auto fetch = [&](int i) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t at = z * a.D.stride + min(first + i * 16 + r, a.rows - 1) * a.D.ld + col;
-      dh[r].load(a.D.hi + at, wide);
-      if (PARTS == 2) dl[r].load(a.D.lo + at, wide);
-    }
-  };
-  if (add) fetch(0);
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
 #pragma unroll

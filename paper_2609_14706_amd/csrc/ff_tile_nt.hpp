@@ -184,16 +184,19 @@ struct Tile {
     }
   }
 
-  // The accumulators of a large tile belong in the accumulation file.  Said before
-  // and after the loop, it keeps the compiler from carrying other registers'
-  // wishes through it, at the price of 100 to 300 moves a pair.
+  // Said before and after the loop, this keeps the compiler from carrying other
+  // registers' wishes through it, at the price of 100 to 300 moves a pair: the
+  // accumulators of a large tile in the accumulation file, others not.
   static __device__ __forceinline__ void pin(Acc& acc) {
-    if (TI * TJ >= 36) {
 #pragma unroll
-      for (int i = 0; i < TI; ++i)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) asm volatile("" : "+a"(acc[i][j]));
-    }
+      for (int j = 0; j < TJ; ++j) {
+        if (TI * TJ >= 36)
+          asm volatile("" : "+a"(acc[i][j]));
+        else
+          asm volatile("" : "+v"(acc[i][j]));
+      }
   }
 
   // acc += sum over pairs [p0, p1).  addr(p, pa, pb) yields the operands'
