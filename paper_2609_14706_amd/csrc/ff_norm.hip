@@ -7,10 +7,12 @@
 //             dw_j = sum_t dy_tj s_tj i_t
 //
 // Both are bound by memory: every row is read once, held in registers (fp32)
-// through its reductions and written once.  A row takes one wave (up to 4
-// vectors of 16 bytes a lane) or a workgroup of 256 to 1024 threads; waves run
-// through many rows with the columns' weights in registers.  Rows too long for
-// registers are read again for each pass (k_norm_long, k_norm_grad_long).
+// through its reductions and written once.  A row takes one wave (up to two
+// vectors of 16 bytes a lane) or a workgroup of 128 to 1024 threads; rows too
+// long for registers (above 32768 bf16, 16384 fp32) are read again for each
+// pass (k_norm_long, k_norm_grad_long).  8192 x 8192 bf16 with residual to 8
+// bits: 99 us, 4.7 TB/s where a large copy reaches 5.1; gradient of 8191 x 4096:
+// 57 us (4.7 TB/s) and 5 us for the sums of dw.
 // All sums are fp32, in an order fixed by the sizes.
 #include <math.h>
 
@@ -90,11 +92,13 @@ __device__ __forceinline__ void store_codes(int8_t* p, const float (&h)[N], floa
   }
 }
 
-// THR threads a row (64: four rows a workgroup), VPT vectors a thread.
-// Q8: codes and scales; otherwise y.
+// Threads of a workgroup of rows that take THR each: a row, or four of a wave.
+constexpr int block_of(int thr) { return thr == 64 ? 256 : thr; }
+
+// THR threads a row, VPT vectors a thread.  Q8: codes and scales; otherwise y.
 template <class E, int THR, int VPT, bool Q8>
-__global__ __launch_bounds__(THR < 256 ? 256 : THR) void k_norm(NormArgs a) {
-  constexpr int N = Vec<E>::N, RPB = THR < 256 ? 256 / THR : 1;
+__global__ __launch_bounds__(block_of(THR)) void k_norm(NormArgs a) {
+  constexpr int N = Vec<E>::N, RPB = block_of(THR) / THR;
   __shared__ float red[16];
   const int t = threadIdx.x % THR;
   for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / THR; row < a.rows;
@@ -238,8 +242,8 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
 // Gradient: as k_norm, with the columns' share of dw summed over the
 // workgroup's rows and left in part[workgroup][column].
 template <class E, int THR, int VPT>
-__global__ __launch_bounds__(THR < 256 ? 256 : THR) void k_norm_grad(NormGradArgs a) {
-  constexpr int N = Vec<E>::N, RPB = THR < 256 ? 256 / THR : 1;
+__global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
+  constexpr int N = Vec<E>::N, RPB = block_of(THR) / THR;
   __shared__ float red[32];
   __shared__ float share[RPB > 1 ? RPB * 64 * VPT * N : 1];
   const int t = threadIdx.x % THR;
@@ -372,40 +376,38 @@ __global__ __launch_bounds__(1024) void k_col_sums(const float* part, int64_t ro
   }
 }
 
-// Threads and vectors a thread for rows of `cols`: a wave up to 4 vectors a
-// lane, then 256, 512 and 1024 threads.  Few rows (under 512: not one a
-// compute unit twice over) go to 1024 threads, which hold a row in one vector
-// each: latency is what counts there.
+// Threads and vectors a thread for rows of `cols`: one or two vectors a thread
+// up to 1024 vectors (8192 x 8192 to 8 bits: 512 x 2 99 us, 256 x 4 108 us), four beyond.
+// Few rows (under 512: not one a compute unit twice over) go to 1024 threads,
+// which hold a row in one vector each: latency is what counts there.
 struct Shape {
   int thr, vpt;
 };
-Shape norm_shape(int64_t rows, int64_t cols, int elems, int most) {
+Shape norm_shape(int64_t rows, int64_t cols, int elems) {
   const int64_t nv = (cols + elems - 1) / elems;
   if (nv <= 64) return {64, 1};
   if (rows < 512 && nv <= 1024 && nv > 128) return {1024, 1};
   if (nv <= 128) return {64, 2};
-  if (most >= 4 && nv <= 256) return {64, 4};
+  if (nv <= 256) return {128, 2};
   if (nv <= 512) return {256, 2};
-  if (most >= 4 && nv <= 1024) return {256, 4};
   if (nv <= 1024) return {512, 2};
-  if (most >= 4 && nv <= 2048) return {512, 4};
-  if (nv <= 2048) return {1024, 2};
+  if (nv <= 2048) return {512, 4};
   if (nv <= 4096) return {1024, 4};
   return {0, 0};
 }
 
 template <class E, bool Q8>
 hipError_t norm_for(const NormArgs& a, hipStream_t s) {
-  const Shape sh = norm_shape(a.rows, a.cols, Vec<E>::N, 4);
+  const Shape sh = norm_shape(a.rows, a.cols, Vec<E>::N);
   const int rpb = sh.thr == 64 ? 4 : 1;
-  const int64_t blocks = std::min<int64_t>((a.rows + rpb - 1) / rpb, 256 * (sh.thr <= 256 ? 8 : 2048 / sh.thr));
+  const int64_t blocks = std::min<int64_t>((a.rows + rpb - 1) / rpb, 4096);
   const dim3 grid((uint32_t)blocks);
 #define FF_CASE(T, V)                                                                          \
   if (sh.thr == T && sh.vpt == V) {                                                            \
-    hipLaunchKernelGGL((k_norm<E, T, V, Q8>), grid, dim3(T < 256 ? 256 : T), 0, s, a);         \
+    hipLaunchKernelGGL((k_norm<E, T, V, Q8>), grid, dim3(block_of(T)), 0, s, a);               \
     return hipGetLastError();                                                                  \
   }
-  FF_CASE(64, 1) FF_CASE(64, 2) FF_CASE(64, 4) FF_CASE(256, 2) FF_CASE(256, 4) FF_CASE(512, 4)
+  FF_CASE(64, 1) FF_CASE(64, 2) FF_CASE(128, 2) FF_CASE(256, 2) FF_CASE(512, 2) FF_CASE(512, 4)
   FF_CASE(1024, 1) FF_CASE(1024, 4)
 #undef FF_CASE
   hipLaunchKernelGGL((k_norm_long<E, Q8>), dim3((uint32_t)std::min<int64_t>(a.rows, 512)), dim3(1024), 0, s, a);
@@ -414,14 +416,14 @@ hipError_t norm_for(const NormArgs& a, hipStream_t s) {
 
 template <class E>
 hipError_t grad_for(const NormGradArgs& a, hipStream_t s) {
-  const Shape sh = norm_shape(a.rows, a.cols, Vec<E>::N, 2);
+  const Shape sh = norm_shape(a.rows, a.cols, Vec<E>::N);
   const dim3 grid((uint32_t)norm_grad_parts(a.rows));
 #define FF_CASE(T, V)                                                                          \
   if (sh.thr == T && sh.vpt == V) {                                                            \
-    hipLaunchKernelGGL((k_norm_grad<E, T, V>), grid, dim3(T < 256 ? 256 : T), 0, s, a);        \
+    hipLaunchKernelGGL((k_norm_grad<E, T, V>), grid, dim3(block_of(T)), 0, s, a);              \
   } else
-  FF_CASE(64, 1) FF_CASE(64, 2) FF_CASE(256, 2) FF_CASE(512, 2) FF_CASE(1024, 1) FF_CASE(1024, 2)
-  FF_CASE(1024, 4)
+  FF_CASE(64, 1) FF_CASE(64, 2) FF_CASE(128, 2) FF_CASE(256, 2) FF_CASE(512, 2) FF_CASE(512, 4)
+  FF_CASE(1024, 1) FF_CASE(1024, 4)
 #undef FF_CASE
   hipLaunchKernelGGL((k_norm_grad_long<E>), grid, dim3(1024), 0, s, a);
   return hipGetLastError();
@@ -429,8 +431,10 @@ hipError_t grad_for(const NormGradArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups of the gradient, each with a row of partial sums of dw.
-int64_t norm_grad_parts(int64_t rows) { return std::min<int64_t>(rows, 512); }
+// Workgroups of the gradient, each with a row of partial sums of dw: two a
+// compute unit; few rows take one, their partial sums weigh as much as they do
+// (2048 x 16384 bf16: 82 us with 512, 67 us with 256; 8191 x 4096: 60 and 84).
+int64_t norm_grad_parts(int64_t rows) { return std::min<int64_t>(rows, rows < 4096 ? 256 : 512); }
 
 hipError_t launch_norm(const NormArgs& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0 || a.cols <= 0) return hipErrorInvalidValue;
