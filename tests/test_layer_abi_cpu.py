@@ -1,0 +1,175 @@
+"""Host-side checks of the layer operators' C ABI (no GPU needed): bad arguments
+are refused before a device is touched, workspaces are sized, and the rule that
+chooses a product's form keeps to what its kernels take."""
+import ctypes
+import os
+import random
+
+import pytest
+
+import paper_2609_14706_amd as ff
+
+P = 1 << 40    # an aligned address that is never read
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(ff.LIB_PATH):
+        from paper_2609_14706_amd.build import build
+        build()
+    return ff.load_library()
+
+
+def _refused(lib, name, args):
+    code = getattr(lib, name)(ctypes.byref(args))
+    return code, ff.ff_last_error()
+
+
+def norm(**kw):
+    a = ff.ff_norm_args(8, 64, 1, P, 64)
+    a.eps, a.normalise, a.y, a.ldy = 1e-6, 1, 2 * P, 64
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=-1), dict(cols=0), dict(cols=(1 << 24) + 1), dict(dtype=2), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(eps=float("inf")), dict(y=None), dict(q=3 * P, ldq=64, q_scale=4 * P), dict(x=None), dict(x=P + 1), dict(ldx=63),
+    dict(ldy=63), dict(normalise=2), dict(residual=3 * P, ldr=8), dict(sum=3 * P, ldsum=0), dict(weight=P + 1),
+    dict(col_scale=4 * P), dict(y=None, q=3 * P, ldq=64), dict(y=None, q=3 * P, ldq=8, q_scale=4 * P),
+    dict(y=P + 2), dict(sum=2 * P, ldsum=64), dict(y=None, q=P, ldq=64, q_scale=4 * P)])
+def test_norm_refusals(lib, kw):
+    code, msg = _refused(lib, "ff_rms_norm", norm(**kw))
+    assert code == ff.FF_ERR_INVALID_ARG and msg
+    assert _refused(lib, "ff_rms_norm", norm(rows=0))[0] == ff.FF_OK    # (nothing to do)
+
+
+def grad(**kw):
+    a = ff.ff_norm_grad_args(8, 64, 1, P, 64, 2 * P, 64)
+    a.eps, a.ds, a.ldds = 1e-6, 3 * P, 64
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(cols=0), 1), (dict(ds=None), 1), (dict(lds=1), 1), (dict(dsum=4 * P, lddsum=63), 1), (dict(ds=P + 2), 1),
+    (dict(dweight=5 * P + 1), 1), (dict(dweight=5 * P), 3), (dict(dweight=5 * P, workspace=6 * P, workspace_bytes=8), 3),
+    (dict(dweight=5 * P, workspace=6 * P + 16, workspace_bytes=1 << 30), 3)])
+def test_norm_gradient_refusals(lib, kw, code):
+    assert _refused(lib, "ff_rms_norm_backward", grad(**kw))[0] == code
+
+
+def linear(q8=False, **kw):
+    a = ff.ff_linear_args(8, 64, 32, P, 64, 2 * P, 64)
+    a.y, a.ldy = 3 * P, 32
+    if q8:
+        a.x_scale, a.row_scale = 4 * P, 5 * P
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("q8,kw", [
+    (0, dict(tokens=-1)), (0, dict(n=0)), (0, dict(m=0)), (0, dict(n=(1 << 20) + 1)), (1, dict(n=131073, ldx=131073, ldw=131073)),
+    (0, dict(x=None)), (0, dict(x=P + 1)), (0, dict(ldx=63)), (0, dict(ldw=63)), (0, dict(y=None)), (0, dict(ldy=31)),
+    (0, dict(residual=6 * P, ldr=31)), (0, dict(preact=6 * P, ldz=0)), (0, dict(bias=P + 1)), (0, dict(activation=4)),
+    (0, dict(activation=-1)), (0, dict(x_scale=4 * P)), (1, dict(x_scale=None)), (1, dict(row_scale=5 * P + 2)),
+    (0, dict(y=P)), (0, dict(y=2 * P)), (0, dict(preact=3 * P, ldz=32)), (0, dict(residual=3 * P + 64, ldr=32)),
+    (0, dict(preact=6 * P, ldz=32, residual=6 * P, ldr=32))])
+def test_linear_refusals(lib, q8, kw):
+    code, msg = _refused(lib, "ff_linear_q8" if q8 else "ff_linear", linear(q8, **kw))
+    assert code == ff.FF_ERR_INVALID_ARG and msg
+
+
+def test_linear_workspaces(lib):
+    size = ctypes.c_size_t(7)
+    # few tokens: none, whatever the alignment
+    assert lib.ff_linear_workspace_size(ctypes.byref(linear(x=P + 2, ldx=65)), 0, ctypes.byref(size)) == 0
+    assert size.value == 0
+    # many: rows that no 16-byte piece divides are copied
+    big = dict(tokens=4096, n=1001, m=1024, ldx=1001, ldw=1001, ldy=1024)
+    a = linear(**big)
+    assert lib.ff_linear_workspace_size(ctypes.byref(a), 0, ctypes.byref(size)) == 0
+    assert size.value == (4096 + 1024) * 1024 * 2
+    assert _refused(lib, "ff_linear", a)[0] == ff.FF_ERR_WORKSPACE
+    a = linear(**dict(big, n=1024, ldx=1024, ldw=1024))
+    assert lib.ff_linear_workspace_size(ctypes.byref(a), 0, ctypes.byref(size)) == 0 and size.value == 0
+    assert lib.ff_linear_workspace_size(ctypes.byref(a), 0, None) == ff.FF_ERR_INVALID_ARG
+    assert lib.ff_linear_workspace_size(None, 0, ctypes.byref(size)) == ff.FF_ERR_INVALID_ARG
+
+
+def linear_grad(**kw):
+    a = ff.ff_linear_grad_args(8, 64, 32, P, 32, 2 * P, 64, 3 * P, 64)
+    a.dx, a.lddx, a.dw, a.lddw, a.db = 4 * P, 64, 5 * P, 64, 6 * P
+    a.workspace, a.workspace_bytes = 8 * P, 1 << 30
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(tokens=(1 << 21) + 1), 1), (dict(activation=1), 1), (dict(activation=1, preact=7 * P, ldz=3), 1),
+    (dict(dy=None), 1), (dict(x=None), 1), (dict(w=None), 1), (dict(lddw=63), 1), (dict(lddx=63), 1), (dict(db=6 * P + 1), 1),
+    (dict(dx=2 * P), 1), (dict(dw=4 * P), 1), (dict(g=P, ldg=32), 1), (dict(g=7 * P, ldg=31), 1), (dict(db=5 * P), 1),
+    (dict(workspace=None), 3), (dict(workspace_bytes=100), 3)])
+def test_linear_gradient_refusals(lib, kw, code):
+    assert _refused(lib, "ff_linear_backward", linear_grad(**kw))[0] == code
+
+
+def test_column_blocks_of_one_buffer_do_not_overlap(lib):
+    # y and the residual side by side in rows of 96: refused for the workspace alone
+    a = linear(tokens=4096, n=1001, m=32, ldx=1001, ldw=1001, y=3 * P, ldy=96, residual=3 * P + 64, ldr=96)
+    assert _refused(lib, "ff_linear", a)[0] == ff.FF_ERR_WORKSPACE
+    a.residual = 3 * P + 62
+    assert _refused(lib, "ff_linear", a)[0] == ff.FF_ERR_INVALID_ARG
+
+
+def ortho(**kw):
+    a = ff.ff_ortho_args(2, 64, 700, 0, P, 700, 64 * 700, 2 * P, 700, 64 * 700, 5, 3.4445, -4.775, 2.0315, 1e-7, 1.0,
+                         3 * P, 1 << 30)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=-1), 1), (dict(batch=65536), 1), (dict(m=0), 1), (dict(n=(1 << 20) + 1), 1), (dict(dtype=3), 1),
+    (dict(steps=0), 1), (dict(steps=65), 1), (dict(a=float("nan")), 1), (dict(eps=-1.0), 1), (dict(scale=float("inf")), 1),
+    (dict(a=8.0), 1), (dict(c=40.0), 1), (dict(G=None), 1), (dict(ldg=699), 1), (dict(ldo=1), 1), (dict(stride_o=699), 1),
+    (dict(out=P), 1), (dict(workspace=None), 3), (dict(workspace_bytes=64), 3)])
+def test_orthogonalize_refusals(lib, kw, code):
+    assert _refused(lib, "ff_orthogonalize", ortho(**kw))[0] == code
+
+
+def test_small_updates_need_no_workspace(lib):
+    size = ctypes.c_size_t(7)
+    assert lib.ff_orthogonalize_workspace_size(ctypes.byref(ortho(m=64, n=128, batch=9)), ctypes.byref(size)) == 0
+    assert size.value == 0
+    assert lib.ff_orthogonalize_workspace_size(ctypes.byref(ortho()), ctypes.byref(size)) == 0
+    assert size.value > 2 * 4 * 2 * 2 * 64 * 700    # X and its transpose, twice, in two parts, both matrices
+
+
+class Plan(ctypes.Structure):
+    _fields_ = [("skinny", ctypes.c_bool), ("ti", ctypes.c_int), ("tj", ctypes.c_int), ("slots", ctypes.c_int),
+                ("splits", ctypes.c_int)]
+
+
+def test_forms_of_linear_products(lib):
+    fn = lib["_ZN2ff11linear_planEllli"]
+    fn.argtypes, fn.restype = [ctypes.c_int64] * 3 + [ctypes.c_int], Plan
+    rng = random.Random(1)
+    for _ in range(500):
+        T, n, m = (int(2 ** rng.uniform(0, b)) for b in (14, 15, 15))
+        eb = rng.choice([1, 2])
+        p = fn(T, n, m, eb)
+        pairs = -(-n * eb // 128)
+        if p.skinny:
+            assert T <= 64 and p.splits == 1
+        else:
+            assert (p.ti, p.tj, p.slots) in {(8, 8, 2), (4, 4, 2), (4, 4, 4), (2, 4, 3)}
+            assert p.splits >= 1 and (p.splits == 1 or p.splits * 4 <= pairs)
+    # the ends of the range: one token by reading w, a prompt by the largest tiles
+    assert fn(1, 4096, 4096, 2).skinny
+    assert (fn(8192, 4096, 11008, 2).ti, fn(8192, 4096, 11008, 2).splits) == (8, 1)
