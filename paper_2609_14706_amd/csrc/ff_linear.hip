@@ -143,8 +143,27 @@ struct Piece {
     for (int q = 0; q < TJ / 2; ++q)
       w[q] = (uint32_t)f32_to_bf16(f[2 * q]) | ((uint32_t)f32_to_bf16(f[2 * q + 1]) << 16);
   }
-  __device__ __forceinline__ void load(const bf16_t* p) { __builtin_memcpy(w, p, sizeof w); }
-  __device__ __forceinline__ void store(bf16_t* p) const { __builtin_memcpy(p, w, sizeof w); }
+  // `count` of them exist (zeros beyond)
+  __device__ __forceinline__ void load(const bf16_t* p, int count) {
+    if (count >= TJ) {
+      __builtin_memcpy(w, p, sizeof w);
+    } else {
+#pragma unroll
+      for (int q = 0; q < TJ / 2; ++q) w[q] = 0;
+#pragma unroll
+      for (int j = 0; j < TJ - 1; ++j)
+        if (j < count) w[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    }
+  }
+  __device__ __forceinline__ void store(bf16_t* p, int count) const {
+    if (count >= TJ) {
+      __builtin_memcpy(p, w, sizeof w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < TJ - 1; ++j)
+        if (j < count) p[j] = (bf16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+  }
 };
 
 // grid: tiles x splits.  P: null (one split), or splits x tokens x m sums.
@@ -176,18 +195,20 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   const int64_t col = i0 + G::col_of(), row0 = t0 + G::row_of(0, 0);
   const int count = (int)min((int64_t)TJ, max((int64_t)0, a.m - col));
   const int rows = (int)min((int64_t)G::BM, a.tokens - row0);  // from row0 on (the lane's are 16 apart)
-  const bool vec = B.rows == G::BN || a.m % TJ == 0;           // a lane's columns are all inside or all outside
   float ws[TJ];
   Piece<TJ> bias, res[4], more[4];
   auto fetch = [&](int i) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (i * 16 + r < rows) more[r].load(a.residual + (row0 + i * 16 + r) * a.ldr + col);
+      if (i * 16 + r < rows) more[r].load(a.residual + (row0 + i * 16 + r) * a.ldr + col, count);
   };
-  const bool fused = vec && P == nullptr && count > 0;
+  const bool fused = P == nullptr && count > 0;
   if (fused) {
-    if (a.row_scale != nullptr) __builtin_memcpy(ws, a.row_scale + col, sizeof ws);
-    if (a.bias != nullptr) bias.load(a.bias + col);
+    if (a.row_scale != nullptr) {
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) ws[j] = a.row_scale[min(col + j, a.m - 1)];
+    }
+    if (a.bias != nullptr) bias.load(a.bias + col, count);
     if (a.residual != nullptr) fetch(0);  // (all of these land during the loop)
   }
   typename G::Acc acc;
@@ -268,7 +289,7 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
           for (int r = 0; r < 4; ++r) {
             Piece<TJ> o;
             o.set(z[r]);
-            if (i * 16 + r < rows) o.store(p + (row0 + i * 16 + r) * ld + col);
+            if (i * 16 + r < rows) o.store(p + (row0 + i * 16 + r) * ld + col, count);
           }
         };
         if (a.preact != nullptr) put(a.preact, a.ldz);
@@ -303,19 +324,6 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
               for (int j = 0; j < TJ; ++j)
                 if (j < count) o[j] = s[r][j];
             }
-          }
-      } else {  // columns that end inside a lane's
-#pragma unroll 1
-        for (int r = 0; r < 4; ++r)
-          if (i * 16 + r < rows) {
-            float f[TJ];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-              const S4 o = stage[((q * 4 + r) * V + v) * nt::kThreads];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) f[4 * v + e] = (float)o[e];
-            }
-            finish<TJ>(a, row0 + i * 16 + r, col, f, count);
           }
       }
     }
