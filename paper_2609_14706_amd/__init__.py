@@ -20,8 +20,20 @@ from .binding import (FF_APPLY, FF_APPLY_INV, FF_BF16, FF_ERR_HIP, FF_ERR_INVALI
                       ff_quantize_workspace_size, ff_set_timing, ff_status_string,
                       ff_whiten_split_state,
                       ff_workspace_size, header_functions, load_library, LIB_PATH)
-from .layer import (ACTIVATIONS, ff_linear_args, ff_linear_grad_args, ff_norm_args, ff_norm_grad_args,
-                    ff_ortho_args, linear, linear_backward, linear_q8, orthogonalize, quantize_rows,
-                    rms_norm, rms_norm_backward, rms_norm_q8)
 
-__all__ = [n for n in dir() if not n.startswith("_")]
+# The layer operators are torch functions: imported with the first use of one,
+# so that the rest of the package does not need torch to be imported.
+_LAYER = ("ACTIVATIONS", "ff_linear_args", "ff_linear_grad_args", "ff_norm_args", "ff_norm_grad_args",
+          "ff_ortho_args", "linear", "linear_backward", "linear_q8", "orthogonalize", "quantize_rows",
+          "rms_norm", "rms_norm_backward", "rms_norm_q8")
+
+
+def __getattr__(name):
+    if name not in _LAYER:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import layer
+    globals().update({n: getattr(layer, n) for n in _LAYER})
+    return globals()[name]
+
+
+__all__ = [n for n in dir() if not n.startswith("_")] + list(_LAYER)

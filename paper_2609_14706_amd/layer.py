@@ -89,14 +89,19 @@ def _library():
 _ELEM = {torch.float32: 0, torch.bfloat16: 1}   # ff_dtype
 
 
-def _rows(t, name, dtype, device, cols=None):
-    """(pointer, leading dimension, rows, columns) of a tensor's rows."""
+def _refuse(t, name, dtype, device):
+    """Why t is not a tensor of that type on that device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, not on {t.device}")
+    raise ValueError(f"{name} must be on {device}, not on {t.device}")
+
+
+def _rows(t, name, dtype, device, cols=None):
+    """(pointer, leading dimension, rows, columns) of a tensor's rows."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
+        _refuse(t, name, dtype, device)
     shape = t.shape
     if not shape:
         raise ValueError(f"{name} must have at least one dimension")
@@ -104,7 +109,7 @@ def _rows(t, name, dtype, device, cols=None):
     if cols is not None and c != cols:
         raise ValueError(f"{name} must have rows of {cols} elements, not {c}")
     if t.is_contiguous():
-        return t.data_ptr(), c, (t.numel() // c if c else shape[:-1].numel()), c
+        return t.data_ptr(), c, shape[0] if len(shape) == 2 else shape[:-1].numel(), c
     if len(shape) != 2 or (c != 1 and t.stride(1) != 1) or (shape[0] != 1 and t.stride(0) < c):
         raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows that do not overlap")
     return t.data_ptr(), (t.stride(0) if shape[0] > 1 else c), shape[0], c
@@ -120,12 +125,10 @@ def _like(t, dtype):
 def _vector(t, name, dtype, device, count):
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.device != device or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor of {count} elements on {device}")
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
+        _refuse(t, name, dtype, device)
+    if t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {count} elements")
     return t.data_ptr()
 
 
@@ -172,11 +175,14 @@ def _workspace(args, nbytes, workspace, device):
     return workspace
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _launch(name, args, device):
     """Call the library on the device's current stream."""
     index = device.index
-    args.stream = torch._C._cuda_getCurrentRawStream(index)
-    if torch._C._cuda_getDevice() == index:
+    args.stream = _raw_stream(index)
+    if _current_device() == index:
         code = _FN[name](args)
     else:
         with torch.cuda.device(index):
@@ -195,29 +201,30 @@ def _bytes(name, args, *more):
 
 # ----------------------------------------------------------------------- norm
 def _norm(x, weight, residual, eps, col_scale, q8, normalise):
-    _library()
+    """(y or codes, their scales or None, the sum or None)."""
+    if not _FN:
+        _library()
     dev = _first(x, "x")
-    dt = _elem(x, "x")
-    px, ldx, r, c = _rows(x, "x", x.dtype, dev)
-    a = ff_norm_args(r, c, dt, px, ldx)
-    s = None
+    dtype = x.dtype
+    px, ldx, r, c = _rows(x, "x", dtype, dev)
+    pr = ldr = ps = 0
+    s = scale = None
     if residual is not None:
         if residual.shape != x.shape:
             raise ValueError(f"residual must have x's shape {tuple(x.shape)}")
-        a.residual, a.ldr, _, _ = _rows(residual, "residual", x.dtype, dev, c)
+        pr, ldr, _, _ = _rows(residual, "residual", dtype, dev, c)
         if normalise:
-            s = _like(x, x.dtype)
-            a.sum, a.ldsum = s.data_ptr(), c
-    a.weight = _vector(weight, "weight", x.dtype, dev, c)
-    a.eps, a.normalise = eps, normalise
+            s = _like(x, dtype)
+            ps = s.data_ptr()
+    pw = None if weight is None else _vector(weight, "weight", dtype, dev, c)
     if q8:
         y = _like(x, torch.int8)
         scale = torch.empty((r,) if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=dev)
-        a.col_scale = _vector(col_scale, "col_scale", torch.float32, dev, c)
-        a.q, a.ldq, a.q_scale = y.data_ptr(), c, scale.data_ptr()
+        a = ff_norm_args(r, c, _elem(x, "x"), px, ldx, pr, ldr, pw, eps, normalise, ps, c, None, 0,
+                         _vector(col_scale, "col_scale", torch.float32, dev, c), y.data_ptr(), c, scale.data_ptr())
     else:
-        y, scale = _like(x, x.dtype), None
-        a.y, a.ldy = y.data_ptr(), c
+        y = _like(x, dtype)
+        a = ff_norm_args(r, c, _elem(x, "x"), px, ldx, pr, ldr, pw, eps, normalise, ps, c, y.data_ptr(), c)
     if r:
         _launch("ff_rms_norm", a, dev)
     return y, scale, s
@@ -283,32 +290,34 @@ def rms_norm_backward(dy, s, weight=None, *, eps: float = 1e-6, dsum=None, works
 
 # --------------------------------------------------------------------- linear
 def _linear(name, x, weight, dtype, x_scale, row_scale, bias, residual, activation, keep_preact, workspace):
-    _library()
+    if not _FN:
+        _library()
     dev = _first(x, "x")
     px, ldx, T, n = _rows(x, "x", dtype, dev)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError("weight must be a 2-D tensor (m, n)")
     pw, ldw, m, _ = _rows(weight, "weight", dtype, dev, n)
-    a = ff_linear_args(T, n, m, px, ldx, pw, ldw)
     bf16 = torch.bfloat16
-    if x_scale is not None:
-        a.x_scale = _vector(x_scale, "x_scale", torch.float32, dev, T)
-        a.row_scale = _vector(row_scale, "row_scale", torch.float32, dev, m)
+    q8 = x_scale is not None
+    ps = pb = pr = pm = pz = None
+    ldr = 0
+    if q8:
+        ps = _vector(x_scale, "x_scale", torch.float32, dev, T)
+        pm = _vector(row_scale, "row_scale", torch.float32, dev, m)
     if bias is not None:
-        a.bias = _vector(bias, "bias", bf16, dev, m)
+        pb = _vector(bias, "bias", bf16, dev, m)
     shape = (T, m) if x.dim() == 2 else x.shape[:-1] + (m,)
     if residual is not None:
         if residual.shape != shape:
             raise ValueError(f"residual must have the output's shape {tuple(shape)}")
-        a.residual, a.ldr, _, _ = _rows(residual, "residual", bf16, dev, m)
-    a.activation = _act(activation)
+        pr, ldr, _, _ = _rows(residual, "residual", bf16, dev, m)
     y = torch.empty(shape, dtype=bf16, device=dev)
-    a.y, a.ldy = y.data_ptr(), m
     z = None
     if keep_preact:
         z = torch.empty_like(y)
-        a.preact, a.ldz = z.data_ptr(), m
-    keep = _workspace(a, _bytes("ff_linear_workspace_size", a, int(x_scale is not None)), workspace, dev)
+        pz = z.data_ptr()
+    a = ff_linear_args(T, n, m, px, ldx, pw, ldw, ps, pm, pb, pr, ldr, _act(activation), y.data_ptr(), m, pz, m)
+    keep = _workspace(a, _bytes("ff_linear_workspace_size", a, int(q8)), workspace, dev)
     if T:
         _launch(name, a, dev)
     del keep
