@@ -693,17 +693,19 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     if (PARTS == 2) *at(X, S.x, S.ldx, 1, i, j) = *at(T, S.t, S.ldr, 1, j, i) = lo;
   });
   __syncthreads();
-  // a 16 x 16 tile of P Q^T, rows p0.. of P and q0.. of Q, k elements
-  auto product = [&](char* P, size_t ps, int ldp, int p0, char* Q, size_t qs, int ldq, int q0, int k) {
+  // Everything below addresses bytes: a lane's place in a tile plus the tile's
+  // (uniform) place in its matrix.
+  const int rt = S.rp / 16, ct = S.cp / 16, kr = S.ldr - 8, kc = S.ldx - 8;
+  const int lr = 4 * (lane >> 4), lc = lane & 15;  // a lane's first row and its column in a result
+  const uint32_t frag_x = (uint32_t)(lc * S.ldx + 2 * lr) * 2, frag_r = (uint32_t)(lc * S.ldr + 2 * lr) * 2;
+  const uint32_t four_r = (uint32_t)(lc * S.ldr + lr) * 2, one_x = (uint32_t)(lr * S.ldx + lc) * 2;
+  // a 16 x 16 tile of P Q^T from the operands' fragments at p and q, k elements
+  auto product = [&](const char* p, size_t ps, const char* q, size_t qs, int k) {
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, low = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int kc = 8 * (lane >> 4);
-    auto frag = [&](char* M, size_t size, int ld, int row, int q, int kk) {
-      return *reinterpret_cast<const u32x4*>(at(M, size, ld, q, row + (lane & 15), kk + kc));
-    };
-    for (int kk = 0; kk < k; kk += 32) {
-      const u32x4 ph = frag(P, ps, ldp, p0, 0, kk), qh = frag(Q, qs, ldq, q0, 0, kk);
+    for (int kk = 0; kk < k; kk += 32, p += 64, q += 64) {
+      const u32x4 ph = *reinterpret_cast<const u32x4*>(p), qh = *reinterpret_cast<const u32x4*>(q);
       if (PARTS == 2) {
-        const u32x4 pl = frag(P, ps, ldp, p0, 1, kk), ql = frag(Q, qs, ldq, q0, 1, kk);
+        const u32x4 pl = *reinterpret_cast<const u32x4*>(p + ps), ql = *reinterpret_cast<const u32x4*>(q + qs);
         low = nt::F16::mfma(ph, ql, low);
         low = nt::F16::mfma(pl, qh, low);
       }
@@ -711,16 +713,16 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     }
     return acc + low;
   };
-  auto put4 = [&](char* M, size_t size, int ld, int i, int j, const float (&f)[4]) {
+  auto put4 = [&](char* p, size_t size, const float (&f)[4]) {
     Halves<4> hi, lo;
     split_parts<4>(f, hi, lo);
-    hi.store(at(M, size, ld, 0, i, j), 4);
-    if (PARTS == 2) lo.store(at(M, size, ld, 1, i, j), 4);
+    __builtin_memcpy(p, hi.w, 8);
+    if (PARTS == 2) __builtin_memcpy(p + size, lo.w, 8);
   };
-  auto get4 = [&](char* M, size_t size, int ld, int i, int j, float (&f)[4]) {
+  auto get4 = [&](const char* p, size_t size, float (&f)[4]) {
     Halves<4> hi, lo;
-    hi.load(at(M, size, ld, 0, i, j), 4);
-    if (PARTS == 2) lo.load(at(M, size, ld, 1, i, j), 4);
+    __builtin_memcpy(hi.w, p, 8);
+    if (PARTS == 2) __builtin_memcpy(lo.w, p + size, 8);
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = hi.get(e) + (PARTS == 2 ? lo.get(e) : 0.0f);
   };
@@ -730,14 +732,22 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     asm volatile("" : "+s"(q));
     return q;
   };
-  const int rt = S.rp / 16, ct = S.cp / 16, kr = S.ldr - 8, kc = S.ldx - 8;
-  const int lr = 4 * (lane >> 4), lc = lane & 15;  // a lane's first row and its column in a tile
+  // q / n and q % n for q < 256 by n's reciprocal in 16 bits
+  const uint32_t inv_rt = (65535u + (uint32_t)rt) / (uint32_t)rt, inv_ct = (65535u + (uint32_t)ct) / (uint32_t)ct;
+  auto place = [](int q, int n, uint32_t inv, int& i, int& j) {
+    i = (int)(((uint32_t)q * inv) >> 16);
+    j = q - i * n;
+  };
+  const int row_x = 16 * S.ldx * 2, row_r = 16 * S.ldr * 2;  // bytes of sixteen rows
+  const float gram = a.sa / (a.sx * a.sx), square = a.c5 * a.sb / (a.sa * a.sa), keep_a = a.b * a.sb / a.sa,
+              back = 1.0f / a.sb;
   for (int step = 0; step < a.steps; ++step) {
     for (int q = wave; q < rt * rt; q += W) {
-      const int i0 = q / rt * 16, j0 = q % rt * 16;
-      const f32x4 s = product(X, S.x, S.ldx, i0, X, S.x, S.ldx, j0, kc);
-      const float al = a.sa / (a.sx * a.sx), f[4] = {al * s[0], al * s[1], al * s[2], al * s[3]};
-      put4(A, S.a, S.ldr, j0 + lc, i0 + lr, f);
+      int i, j;
+      place(q, rt, inv_rt, i, j);
+      const f32x4 s = product(X + i * row_x + frag_x, S.x, X + j * row_x + frag_x, S.x, kc);
+      const float f[4] = {gram * s[0], gram * s[1], gram * s[2], gram * s[3]};
+      put4(A + j * row_r + i * 32 + four_r, S.a, f);
     }
     __syncthreads();
     float keep[LIMIT][4];
@@ -745,20 +755,24 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     for (int u = 0; u < LIMIT; ++u) {
       const int q = tile_of(u);
       if (q < rt * rt) {
-        const int i0 = q / rt * 16, j0 = q % rt * 16;
-        const f32x4 s = product(A, S.a, S.ldr, i0, A, S.a, S.ldr, j0, kr);
+        int i, j;
+        place(q, rt, inv_rt, i, j);
+        const f32x4 s = product(A + i * row_r + frag_r, S.a, A + j * row_r + frag_r, S.a, kr);
         float d[4];
-        get4(A, S.a, S.ldr, j0 + lc, i0 + lr, d);
-        const float al = a.c5 * a.sb / (a.sa * a.sa), be = a.b * a.sb / a.sa;
+        get4(A + j * row_r + i * 32 + four_r, S.a, d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) keep[u][e] = al * s[e] + be * d[e];
+        for (int e = 0; e < 4; ++e) keep[u][e] = square * s[e] + keep_a * d[e];
       }
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < LIMIT; ++u) {
       const int q = tile_of(u);
-      if (q < rt * rt) put4(A, S.a, S.ldr, q % rt * 16 + lc, q / rt * 16 + lr, keep[u]);
+      if (q < rt * rt) {
+        int i, j;
+        place(q, rt, inv_rt, i, j);
+        put4(A + j * row_r + i * 32 + four_r, S.a, keep[u]);
+      }
     }
     __syncthreads();
     const bool last = step + 1 == a.steps;
@@ -766,21 +780,22 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     for (int u = 0; u < LIMIT; ++u) {
       const int q = tile_of(u);
       if (q < rt * ct) {
-        const int i0 = q / ct * 16, j0 = q % ct * 16;
-        const f32x4 s = product(A, S.a, S.ldr, i0, T, S.t, S.ldr, j0, kr);
+        int i, j;
+        place(q, ct, inv_ct, i, j);
+        const f32x4 s = product(A + i * row_r + frag_r, S.a, T + j * row_r + frag_r, S.t, kr);
         float d[4];
-        get4(T, S.t, S.ldr, j0 + lc, i0 + lr, d);
+        get4(T + j * row_r + i * 32 + four_r, S.t, d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) keep[u][e] = s[e] * (1.0f / a.sb) + a.a * d[e];
+        for (int e = 0; e < 4; ++e) keep[u][e] = back * s[e] + a.a * d[e];
         if (last) {
+          const int gi = i * 16 + lr, gj = j * 16 + lc;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = i0 + lr + e, j = j0 + lc;
-            if (i < a.r && j < a.c) {
-              const int64_t o = blockIdx.x * a.so + (a.tall ? (int64_t)j * a.ldo + i : (int64_t)i * a.ldo + j);
+          for (int e = 0; e < 4; ++e)
+            if (gi + e < a.r && gj < a.c) {
+              const int64_t o =
+                  blockIdx.x * a.so + (a.tall ? (int64_t)gj * a.ldo + gi + e : (int64_t)(gi + e) * a.ldo + gj);
               ((E*)a.out)[o] = Elem<E>::from_f32(keep[u][e] * (a.scale / a.sx));
             }
-          }
         }
       }
     }
@@ -790,13 +805,19 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     for (int u = 0; u < LIMIT; ++u) {
       const int q = tile_of(u);
       if (q < rt * ct) {
-        const int i = q / ct * 16 + lr, j = q % ct * 16 + lc;
-        put4(T, S.t, S.ldr, j, i, keep[u]);
+        int i, j;
+        place(q, ct, inv_ct, i, j);
+        Halves<4> hi, lo;
+        split_parts<4>(keep[u], hi, lo);
+        char* t = T + j * row_r + i * 32 + four_r;
+        char* x = X + i * row_x + j * 32 + one_x;
+        __builtin_memcpy(t, hi.w, 8);
+        if (PARTS == 2) __builtin_memcpy(t + S.t, lo.w, 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint16_t hi = f16_bits(keep[u][e]);
-          *at(X, S.x, S.ldx, 0, i + e, j) = hi;
-          if (PARTS == 2) *at(X, S.x, S.ldx, 1, i + e, j) = f16_bits(keep[u][e] - f16_f32(hi));
+          *reinterpret_cast<uint16_t*>(x + e * S.ldx * 2) = (uint16_t)(hi.w[e >> 1] >> (16 * (e & 1)));
+          if (PARTS == 2)
+            *reinterpret_cast<uint16_t*>(x + S.x + e * S.ldx * 2) = (uint16_t)(lo.w[e >> 1] >> (16 * (e & 1)));
         }
       }
     }
