@@ -409,15 +409,28 @@ ff_status ff_linear_backward(const ff_linear_grad_args* a) {
   k.gt = a->dw != nullptr ? (bf16_t*)(ws + w.off_gt) : nullptr;
   k.ldgt = w.ldt;
   k.part = a->db != nullptr ? (float*)(ws + w.off_part) : nullptr;
-  if (k.g != nullptr || k.gt != nullptr || k.part != nullptr)
-    if ((rc = hip(launch_act_grad(k, s), "pre-activation gradient")) != FF_OK) return rc;
+  // one launch for what the products read: g by rows and columns, W^T and x^T
+  ActGradArgs jobs[3];
+  int count = 0;
+  if (k.g != nullptr || k.gt != nullptr || k.part != nullptr) jobs[count++] = k;
+  auto turn = [&](const void* src, int64_t ld, int64_t rows, int64_t cols, size_t off, int64_t ldt) {
+    ActGradArgs j{};
+    j.rows = rows;
+    j.cols = cols;
+    j.dy = (const bf16_t*)src;
+    j.lddy = ld;
+    j.gt = (bf16_t*)(ws + off);
+    j.ldgt = ldt;
+    jobs[count++] = j;
+    return j.gt;
+  };
+  const bf16_t* wt = a->dx != nullptr ? turn(a->w, a->ldw, a->m, a->n, w.off_wt, w.ldm) : nullptr;
+  const bf16_t* xt = a->dw != nullptr ? turn(a->x, a->ldx, T, a->n, w.off_xt, w.ldt) : nullptr;
+  if (count > 0 && (rc = hip(launch_act_grad(jobs, count, s), "operands of the gradient")) != FF_OK) return rc;
   if (a->db != nullptr &&
       (rc = hip(launch_col_sums(k.part, act_grad_parts(T), a->m, a->db, true, s), "bias gradient")) != FF_OK)
     return rc;
   if (a->dx != nullptr) {
-    bf16_t* wt = (bf16_t*)(ws + w.off_wt);
-    if ((rc = hip(launch_transpose((const bf16_t*)a->w, a->ldw, a->m, a->n, wt, w.ldm, s), "transposing W")) != FF_OK)
-      return rc;
     LinearArgs p{};
     p.tokens = T;
     p.n = a->m;
@@ -431,9 +444,6 @@ ff_status ff_linear_backward(const ff_linear_grad_args* a) {
     if ((rc = run_linear(p, 2, ws + w.off_lin, s, true)) != FF_OK) return rc;
   }
   if (a->dw != nullptr) {
-    bf16_t* xt = (bf16_t*)(ws + w.off_xt);
-    if ((rc = hip(launch_transpose((const bf16_t*)a->x, a->ldx, T, a->n, xt, w.ldt, s), "transposing x")) != FF_OK)
-      return rc;
     LinearArgs p{};
     p.tokens = a->m;
     p.n = w.ldt;  // (zeros beyond the tokens)

@@ -98,17 +98,15 @@ hipError_t launch_linear(const LinearArgs& a, const LinearPlan& p, int elem_byte
 // dst (rows x cols elements, ld apart) = 0.
 hipError_t launch_zero(void* dst, int64_t ld, int64_t rows, int64_t cols, int elem_bytes, hipStream_t s);
 
-// dst (cols x ldd, zeros beyond rows) = src^T for src rows x cols, bf16.
-hipError_t launch_transpose(const bf16_t* src, int64_t ld, int64_t rows, int64_t cols, bf16_t* dst, int64_t ldd,
-                            hipStream_t s);
 // g = dy act'(z) (rows x cols; null: not stored), its transpose gt (cols x
-// ldgt, zeros beyond rows) and, with part, column sums of every 64 rows
-// (act_grad_parts(rows) x cols).
+// ldgt, zeros beyond rows; null: not stored) and, with part, column sums of
+// every 64 rows (act_grad_parts(rows) x cols).  z null: g = dy, so that with
+// gt alone a job is a transposition.  One to three jobs in one launch.
 struct ActGradArgs {
   int64_t rows, cols;
   const bf16_t* dy;
   int64_t lddy;
-  const bf16_t* z;  // null: g = dy
+  const bf16_t* z;
   int64_t ldz;
   bf16_t* g;
   int64_t ldg;
@@ -118,7 +116,7 @@ struct ActGradArgs {
   int act;
 };
 int64_t act_grad_parts(int64_t rows);
-hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t s);
+hipError_t launch_act_grad(const ActGradArgs* jobs, int count, hipStream_t s);
 
 // ---------------------------------------------------------- orthogonalisation
 // X <- a X + (b A + c A^2) X, A = X X^T, `steps` times from G / (||G||_F + eps)

@@ -497,11 +497,19 @@ struct __align__(16) Turn {
   bf16_t e[64][66];
 };
 
-template <bool GRAD>
-__global__ __launch_bounds__(256) void k_turn(ActGradArgs a) {
+// Up to three jobs in one launch, each a range of workgroups.
+struct TurnJobs {
+  ActGradArgs job[3];
+  uint32_t end[3], gx[3];  // first workgroup after the job, its 64-column blocks
+};
+
+__global__ __launch_bounds__(256) void k_turn(TurnJobs jobs) {
   __shared__ Turn sm;
   __shared__ float sums[4][64];
-  const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+  const int which = (blockIdx.x >= jobs.end[0]) + (blockIdx.x >= jobs.end[1]);
+  const ActGradArgs& a = jobs.job[which];
+  const uint32_t w = blockIdx.x - (which > 0 ? jobs.end[which - 1] : 0), by = w / jobs.gx[which];
+  const int64_t r0 = (int64_t)by * 64, c0 = (int64_t)(w - by * jobs.gx[which]) * 64;
   const int tid = threadIdx.x;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -511,19 +519,19 @@ __global__ __launch_bounds__(256) void k_turn(ActGradArgs a) {
     Vec<bf16_t> v;
     v.w = u32x4{0, 0, 0, 0};
     if (count > 0) v = load_row(a.dy + row * a.lddy + col, count);
-    if (GRAD && a.z != nullptr && count > 0) {
+    if (a.z != nullptr && count > 0) {
       const Vec<bf16_t> z = load_row(a.z + row * a.ldz + col, count);
       float f[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) f[k] = v.get(k) * act_slope(z.get(k), a.act);
       v.set(f);
     }
-    if (GRAD && a.g != nullptr && count > 0) store_row(a.g + row * a.ldg + col, v, count);
+    if (a.g != nullptr && count > 0) store_row(a.g + row * a.ldg + col, v, count);
 #pragma unroll
     for (int k = 0; k < 8; ++k) sm.e[r][c + k] = k < count ? v.bits(k) : (bf16_t)0;
   }
   __syncthreads();
-  if (GRAD && a.part != nullptr) {
+  if (a.part != nullptr) {
     const int c = tid & 63, g = tid >> 6;
     float s = 0.0f;
 #pragma unroll
@@ -531,7 +539,7 @@ __global__ __launch_bounds__(256) void k_turn(ActGradArgs a) {
     sums[g][c] = s;
     __syncthreads();
     if (g == 0 && c0 + c < a.cols)
-      a.part[(int64_t)blockIdx.y * a.cols + c0 + c] = s + sums[1][c] + sums[2][c] + sums[3][c];
+      a.part[(int64_t)by * a.cols + c0 + c] = s + sums[1][c] + sums[2][c] + sums[3][c];
   }
   if (a.gt == nullptr) return;
 #pragma unroll
@@ -701,29 +709,24 @@ hipError_t launch_zero(void* dst, int64_t ld, int64_t rows, int64_t cols, int el
 
 int64_t act_grad_parts(int64_t rows) { return (rows + 63) / 64; }
 
-hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t s) {
-  const int64_t gx = (a.cols + 63) / 64, gy = (a.rows + 63) / 64;
-  if (a.rows <= 0 || a.cols <= 0 || gx > 0x7fffffff || gy > 65535 ||
-      (a.gt != nullptr && (a.ldgt % 8 != 0 || a.ldgt < a.rows || a.ldgt > gy * 64 || (uintptr_t)a.gt % 16 != 0)))
-    return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_turn<true>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_transpose(const bf16_t* src, int64_t ld, int64_t rows, int64_t cols, bf16_t* dst, int64_t ldd,
-                            hipStream_t s) {
-  ActGradArgs a{};
-  a.rows = rows;
-  a.cols = cols;
-  a.dy = src;
-  a.lddy = ld;
-  a.gt = dst;
-  a.ldgt = ldd;
-  const int64_t gx = (cols + 63) / 64, gy = (rows + 63) / 64;
-  if (rows <= 0 || cols <= 0 || gx > 0x7fffffff || gy > 65535 || ldd % 8 != 0 || ldd < rows || ldd > gy * 64 ||
-      (uintptr_t)dst % 16 != 0)
-    return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_turn<false>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, a);
+hipError_t launch_act_grad(const ActGradArgs* jobs, int count, hipStream_t s) {
+  if (count < 1 || count > 3) return hipErrorInvalidValue;
+  TurnJobs q{};
+  int64_t total = 0;
+  for (int k = 0; k < count; ++k) {
+    const ActGradArgs& a = jobs[k];
+    const int64_t gx = (a.cols + 63) / 64, gy = (a.rows + 63) / 64;
+    if (a.rows <= 0 || a.cols <= 0 || gx * gy > 0x7fffffff ||
+        (a.gt != nullptr && (a.ldgt % 8 != 0 || a.ldgt < a.rows || a.ldgt > gy * 64 || (uintptr_t)a.gt % 16 != 0)))
+      return hipErrorInvalidValue;
+    total += gx * gy;
+    if (total > 0x7fffffff) return hipErrorInvalidValue;
+    q.job[k] = a;
+    q.gx[k] = (uint32_t)gx;
+    q.end[k] = (uint32_t)total;
+  }
+  for (int k = count; k < 3; ++k) q.end[k] = (uint32_t)total;
+  hipLaunchKernelGGL(k_turn, dim3((uint32_t)total), dim3(256), 0, s, q);
   return hipGetLastError();
 }
 
