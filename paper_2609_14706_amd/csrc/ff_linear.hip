@@ -231,10 +231,11 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   // lane's bias and scales are read once and the next rows' residual before
   // these rows' work; reading them row by row took 30 to 60 us a tile.
   typedef typename Scalar<T>::type S;
-  typedef __attribute__((ext_vector_type(4))) S S4;
-  constexpr int HI = TI < 4 ? TI : 4, V = TJ / 4;  // tile rows a phase, pieces of a row
-  static_assert(TJ % 4 == 0 && sizeof(S4) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
-  S4* stage = reinterpret_cast<S4*>(&sm) + threadIdx.x;
+  // tile rows a phase, numbers of a piece of a row, pieces of a row
+  constexpr int HI = TI < 4 ? TI : TI % 4 == 0 ? 4 : 3, PC = TJ % 4 == 0 ? 4 : 2, V = TJ / PC;
+  typedef __attribute__((ext_vector_type(PC))) S Slot;
+  static_assert(TI % HI == 0 && TJ % 2 == 0 && sizeof(Slot) * HI * 4 * V * nt::kThreads <= sizeof(sm), "stage");
+  Slot* stage = reinterpret_cast<Slot*>(&sm) + threadIdx.x;
 #pragma unroll
   for (int h = 0; h < TI / HI; ++h) {
 #pragma unroll
@@ -243,9 +244,9 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          S4 o;
+          Slot o;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = acc[h * HI + i][4 * v + e][r];
+          for (int e = 0; e < PC; ++e) o[e] = acc[h * HI + i][PC * v + e][r];
           stage[((i * 4 + r) * V + v) * nt::kThreads] = o;
         }
 #pragma unroll 1
@@ -256,9 +257,9 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const S4 o = stage[((q * 4 + r) * V + v) * nt::kThreads];
+          const Slot o = stage[((q * 4 + r) * V + v) * nt::kThreads];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[r][4 * v + e] = o[e];
+          for (int e = 0; e < PC; ++e) s[r][PC * v + e] = o[e];
         }
       if (fused) {
         if (a.residual != nullptr) {
@@ -597,7 +598,7 @@ hipError_t linear_for(const LinearArgs& a, const LinearPlan& p, void* partial, h
   }
 #define FF_TILE(I, J, S) \
   if (p.ti == I && p.tj == J && p.slots == S) return tiles<T, I, J, S>(a, p, partial, s);
-  FF_TILE(8, 8, 2) FF_TILE(4, 4, 2) FF_TILE(4, 4, 4) FF_TILE(2, 4, 3)
+  FF_TILE(8, 8, 2) FF_TILE(6, 8, 2) FF_TILE(4, 8, 3) FF_TILE(4, 6, 3) FF_TILE(4, 4, 2) FF_TILE(4, 4, 4) FF_TILE(2, 4, 3)
 #undef FF_TILE
   return hipErrorInvalidValue;
 }
@@ -626,15 +627,16 @@ LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
     int ti, tj, slots, wgs;
     double pair, loaded, ends;
   };
-  static const Form forms[] = {{8, 8, 2, 1, 1.41, 1.41, 12.0}, {4, 4, 2, 2, 0.52, 0.80, 6.0}, {4, 4, 4, 1, 0.37, 0.53, 3.0},
-                               {2, 4, 3, 2, 0.25, 0.50, 2.0}};
+  static const Form forms[] = {{8, 8, 2, 1, 1.36, 1.36, 13.0}, {6, 8, 2, 1, 1.09, 1.09, 10.0}, {4, 8, 3, 1, 0.79, 0.79, 8.0},
+                               {4, 6, 3, 1, 0.61, 0.61, 7.0},  {4, 4, 2, 2, 0.53, 0.85, 6.5},  {4, 4, 4, 1, 0.42, 0.53, 5.0},
+                               {2, 4, 3, 2, 0.27, 0.53, 3.0}};
   const int64_t pairs = (n * elem_bytes + nt::kPair - 1) / nt::kPair;
   LinearPlan best{false, 8, 8, 2, 1};
   double least = 1e300;
   for (const Form& f : forms) {
     const int64_t rows = (tokens + 32 * f.ti - 1) / (32 * f.ti), tiles = rows * ((m + 32 * f.tj - 1) / (32 * f.tj));
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      if (s > 1 && (s * 4 > pairs || tiles * s > 768 || f.ti == 8)) break;
+      if (s > 1 && (s * 4 > pairs || tiles * s > 768 || f.ti * f.tj > 16)) break;
       const int64_t wgs = tiles * s, rounds = (wgs + 256 * f.wgs - 1) / (256 * f.wgs);
       double pair = wgs > 256 ? f.loaded : f.pair;
       if (rows == 1)

@@ -416,10 +416,12 @@ struct StepForm {
 struct StepPlan {
   int form, splits;
 };
-constexpr StepForm kSymForms[] = {{8, 8, 2, 1, 1.41, 1.41, 10.0}, {6, 6, 2, 1, 0.85, 0.85, 8.0},
-                                  {4, 4, 4, 1, 0.37, 0.53, 4.0}, {2, 2, 5, 2, 0.17, 0.30, 2.0}};
-constexpr StepForm kAnyForms[] = {{8, 8, 2, 1, 1.41, 1.41, 10.0}, {6, 6, 2, 1, 0.85, 0.85, 8.0},
-                                  {4, 4, 2, 2, 0.52, 0.80, 6.0}, {4, 4, 4, 1, 0.40, 0.62, 4.0},
+constexpr StepForm kSymForms[] = {{8, 8, 2, 1, 1.36, 1.36, 12.0}, {6, 6, 2, 1, 0.85, 0.85, 8.0},
+                                  {4, 4, 2, 2, 0.53, 0.85, 6.5},  {4, 4, 4, 1, 0.40, 0.53, 5.0},
+                                  {2, 2, 5, 2, 0.17, 0.30, 2.0}};
+constexpr StepForm kAnyForms[] = {{8, 8, 2, 1, 1.36, 1.36, 12.0}, {6, 8, 2, 1, 1.09, 1.09, 10.0},
+                                  {4, 8, 3, 1, 0.79, 0.79, 8.0},  {4, 6, 3, 1, 0.61, 0.61, 7.0},
+                                  {4, 4, 2, 2, 0.53, 0.85, 6.5},  {4, 4, 4, 1, 0.40, 0.55, 5.0},
                                   {2, 4, 3, 2, 0.25, 0.50, 3.0}};
 
 StepPlan step_plan(bool sym, bool may_split, int64_t rows, int64_t cols, int64_t k, int64_t batch, int parts) {
@@ -432,7 +434,7 @@ StepPlan step_plan(bool sym, bool may_split, int64_t rows, int64_t cols, int64_t
   const int64_t pairs = (k * 2 + nt::kPair - 1) / nt::kPair * (parts == 2 ? 3 : 1);
   StepPlan best{0, 1};
   double least = 1e300;
-  const int forms = sym ? 4 : 5;
+  const int forms = sym ? 5 : 7;
   for (int q = 0; q < forms; ++q) {
     const StepForm& f = sym ? kSymForms[q] : kAnyForms[q];
     const int64_t mt = (rows + 32 * f.ti - 1) / (32 * f.ti), ntl = (cols + 32 * f.tj - 1) / (32 * f.tj);
@@ -476,7 +478,8 @@ hipError_t sym_step(StepArgs a, const StepPlan& p, float* sums, int64_t batch, h
   switch (p.form) {
     case 0: return step_tiles<PARTS, 8, 8, 2, true>(a, batch, s);
     case 1: return step_tiles<PARTS, 6, 6, 2, true>(a, batch, s);
-    case 2: return step_tiles<PARTS, 4, 4, 4, true>(a, batch, s);
+    case 2: return step_tiles<PARTS, 4, 4, 2, true>(a, batch, s);
+    case 3: return step_tiles<PARTS, 4, 4, 4, true>(a, batch, s);
     default: return step_tiles<PARTS, 2, 2, 5, true>(a, batch, s);
   }
 }
@@ -485,9 +488,11 @@ hipError_t any_step(StepArgs a, const StepPlan& p, int64_t batch, hipStream_t s)
   a.splits = 1;
   switch (p.form) {
     case 0: return step_tiles<PARTS, 8, 8, 2, false>(a, batch, s);
-    case 1: return step_tiles<PARTS, 6, 6, 2, false>(a, batch, s);
-    case 2: return step_tiles<PARTS, 4, 4, 2, false>(a, batch, s);
-    case 3: return step_tiles<PARTS, 4, 4, 4, false>(a, batch, s);
+    case 1: return step_tiles<PARTS, 6, 8, 2, false>(a, batch, s);
+    case 2: return step_tiles<PARTS, 4, 8, 3, false>(a, batch, s);
+    case 3: return step_tiles<PARTS, 4, 6, 3, false>(a, batch, s);
+    case 4: return step_tiles<PARTS, 4, 4, 2, false>(a, batch, s);
+    case 5: return step_tiles<PARTS, 4, 4, 4, false>(a, batch, s);
     default: return step_tiles<PARTS, 2, 4, 3, false>(a, batch, s);
   }
 }

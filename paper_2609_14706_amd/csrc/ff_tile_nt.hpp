@@ -192,7 +192,7 @@ struct Tile {
     for (int i = 0; i < TI; ++i)
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
-        if (TI * TJ >= 36)
+        if (TI * TJ >= 24)
           asm volatile("" : "+a"(acc[i][j]));
         else
           asm volatile("" : "+v"(acc[i][j]));

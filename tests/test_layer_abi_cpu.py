@@ -168,7 +168,7 @@ def test_forms_of_linear_products(lib):
         if p.skinny:
             assert T <= 64 and p.splits == 1
         else:
-            assert (p.ti, p.tj, p.slots) in {(8, 8, 2), (4, 4, 2), (4, 4, 4), (2, 4, 3)}
+            assert (p.ti, p.tj, p.slots) in {(8, 8, 2), (6, 8, 2), (4, 8, 3), (4, 6, 3), (4, 4, 2), (4, 4, 4), (2, 4, 3)}
             assert p.splits >= 1 and (p.splits == 1 or p.splits * 4 <= pairs)
     # the ends of the range: one token by reading w, a prompt by the largest tiles
     assert fn(1, 4096, 4096, 2).skinny
