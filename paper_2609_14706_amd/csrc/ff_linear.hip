@@ -216,14 +216,8 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   static_assert(G::BM <= nt::kThreads, "a row a thread");
   if (a.x_scale != nullptr && (int)threadIdx.x < G::BM)
     xs[threadIdx.x] = (int)threadIdx.x < A.rows ? a.x_scale[t0 + threadIdx.x] : 0.0f;
-  G::loop(
-      sm, A, B, p0, p1,
-      [&](int p, const char*& pa, const char*& pb) {
-        const int k = __builtin_amdgcn_readfirstlane(p) * nt::kPair;
-        pa = A.p + k;
-        pb = B.p + k;
-      },
-      [&](int p) { return kbytes - p * nt::kPair; }, acc);
+  nt::Straight walk{A.p + p0 * nt::kPair, B.p + p0 * nt::kPair, kbytes - p0 * nt::kPair};
+  G::loop(sm, A, B, p1 - p0, walk, acc);
   // The sums go through LDS (each lane its own 16-byte slots: no barrier, no
   // bank conflict) so that a short loop over four rows at a time serves all of
   // them: straight from the accumulators the epilogue of a 256 x 256 tile is 32

@@ -211,6 +211,37 @@ __device__ __forceinline__ void store_parts(const float (&f)[4][N], int64_t row,
     }
 }
 
+// k three times over, for operands in two parts: hi lo, lo hi, then hi hi (the
+// largest last).
+struct Thrice {
+  const char *lh, *rh;  // the larger parts at k = 0
+  const char* next;     // L's part of the next round
+  int bytes;            // of k
+  const char *pa, *pb;
+  int left;
+  // at pair p of 3 `pairs`
+  __device__ __forceinline__ Thrice(const char* lh, const char* ll, const char* rh, const char* rl, int bytes,
+                                    int p, int pairs)
+      : lh(lh), rh(rh), bytes(bytes) {
+    const int round = (p >= pairs) + (p >= 2 * pairs), k = (p - round * pairs) * nt::kPair;
+    next = round == 0 ? ll : lh;
+    pa = (round == 1 ? ll : lh) + k;
+    pb = (round == 0 ? rl : rh) + k;
+    left = bytes - k;
+  }
+  __device__ __forceinline__ int operator()(const char*& a, const char*& b) {
+    a = pa;
+    b = pb;
+    const int l = left;
+    const bool end = l <= nt::kPair;
+    pa = end ? next : pa + nt::kPair;
+    pb = end ? rh : pb + nt::kPair;
+    left = end ? bytes : l - nt::kPair;
+    next = end ? lh : next;
+    return l;
+  }
+};
+
 template <int PARTS, int TI, int TJ, int SLOTS, bool SYM>
 __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) void k_step(StepArgs a) {
   typedef nt::Tile<nt::F16, TI, TJ, SLOTS> G;
@@ -247,21 +278,16 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   if (add) fetch(0);  // (lands during the loop)
   typename G::Acc acc;
   G::zero(acc);
-  // two parts: hi lo, lo hi, then hi hi (the largest last)
-  G::loop(
-      sm, A, B, (int)((int64_t)total * part / a.splits), (int)((int64_t)total * (part + 1) / a.splits),
-      [&](int p, const char*& pa, const char*& pb) {
-        p = __builtin_amdgcn_readfirstlane(p);
-        const int seg = PARTS == 2 ? (p >= pairs) + (p >= 2 * pairs) : 2;
-        const int k = (PARTS == 2 ? p - seg * pairs : p) * nt::kPair;
-        pa = (const char*)((PARTS == 2 && seg == 1 ? a.L.lo : a.L.hi) + la) + k;
-        pb = (const char*)((PARTS == 2 && seg == 0 ? a.R.lo : a.R.hi) + rb) + k;
-      },
-      [&](int p) {
-        const int seg = PARTS == 2 ? (p >= pairs) + (p >= 2 * pairs) : 0;
-        return kbytes - (p - seg * pairs) * nt::kPair;
-      },
-      acc);
+  const int p0 = (int)((int64_t)total * part / a.splits), p1 = (int)((int64_t)total * (part + 1) / a.splits);
+  if (PARTS == 1) {
+    nt::Straight walk{(const char*)(a.L.hi + la) + p0 * nt::kPair, (const char*)(a.R.hi + rb) + p0 * nt::kPair,
+                      kbytes - p0 * nt::kPair};
+    G::loop(sm, A, B, p1 - p0, walk, acc);
+  } else {
+    Thrice walk{(const char*)(a.L.hi + la), (const char*)(a.L.lo + la), (const char*)(a.R.hi + rb),
+                (const char*)(a.R.lo + rb), kbytes, p0, pairs};
+    G::loop(sm, A, B, p1 - p0, walk, acc);
+  }
   // through LDS and four rows at a time, as in the linear layers
   constexpr int HI = TI < 4 ? TI : TI % 4 == 0 ? 4 : 3, PC = TJ % 4 == 0 ? 4 : 2, V = TJ / PC;
   typedef __attribute__((ext_vector_type(PC))) float Slot;

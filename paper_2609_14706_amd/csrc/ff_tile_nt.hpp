@@ -74,6 +74,22 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const char* p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, (int)0x7fffffff, 0x00020000);
 }
 
+// k without interruption, from pair 0 at pa and pb on.
+struct Straight {
+  const char* pa;
+  const char* pb;
+  int left;
+  __device__ __forceinline__ int operator()(const char*& a, const char*& b) {
+    a = pa;
+    b = pb;
+    pa += kPair;
+    pb += kPair;
+    const int l = left;
+    left -= kPair;
+    return l;
+  }
+};
+
 // One operand of a tile: its first row, the rows from there on that exist and
 // the bytes from row to row.
 struct Rows {
@@ -199,50 +215,111 @@ struct Tile {
       }
   }
 
-  // acc += sum over pairs [p0, p1).  addr(p, pa, pb) yields the operands'
-  // pointers at pair p (row 0); left(p) the bytes of k that are left there
-  // (128 or more for a whole pair).  Per pair, its first step multiplies from
+  // acc += sum over `count` pairs.  walk(pa, pb) yields the operands' pointers
+  // (row 0) at the next pair, in order, and returns the bytes of k that are left
+  // there (128 or more for a whole pair).  Per pair, its first step multiplies from
   // registers while the second step's fragments are read; then the next pair
   // has to have landed (copies return in order: at most SLOTS - 2 later pairs
   // are still on their way), the pair's one barrier is taken (every wave has
   // read all of this slot and sees the next pair), and the second step reads
   // the next pair's first fragments and copies the pair SLOTS further on into
-  // the slot just freed.  Pairs beyond p1 are "copied" from outside, i.e. their
+  // the slot just freed.  Pairs beyond the last are "copied" from outside, i.e. their
   // slots get zeros that no product uses: one loop body for all pairs keeps
   // the accumulators where they are (peeled ends moved hundreds of registers).
-  // Every wave takes the same number of barriers: p0 and p1 are uniform.
-  template <class Addr, class Left>
-  static __device__ __forceinline__ void loop(Ring& sm, const Rows& A, const Rows& B, int p0, int p1,
-                                              const Addr& addr, const Left& left, Acc& acc) {
+  // Every wave takes the same number of barriers: count is uniform.
+  //
+  // Small tiles (up to eight products a step) would wait for the fragments' LDS
+  // latency at every step: they take whole pairs, the next pair's fragments
+  // read among this one's products, two pairs a turn so that no fragment changes
+  // registers, and the last pair waits for nothing.
+  template <class Walk>
+  static __device__ __forceinline__ void loop(Ring& sm, const Rows& A, const Rows& B, int count, Walk& walk,
+                                              Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (p1 <= p0) return;
+    if (count <= 0) return;
     const Lane L = lane_of(A, B, wave, lane);
     const FragBase fb = frag_base(wave, lane);
     const char *pa, *pb;
-    auto cut = [&](int p) -> uint32_t { return p < p1 && 16 * L.c < left(p) ? 0u : kOutside; };
+    const int chunk = 16 * L.c;
+    auto advance = [&](int p) -> uint32_t {  // to pair p, the next one
+      const int left = walk(pa, pb);
+      return chunk < (p < count ? left : 0) ? 0u : kOutside;
+    };
 #pragma unroll
     for (int q = 0; q < SLOTS; ++q) {
-      addr(p0 + q, pa, pb);
-      const uint32_t c = cut(p0 + q);
+      const uint32_t c = advance(q);
 #pragma unroll
       for (int k = 0; k < NL; ++k) issue_one(sm, q, pa, pb, L, c, wave, k);
     }
     wait_vmem<(SLOTS - 1) * NL>();
     __builtin_amdgcn_s_barrier();
+    int slot = 0;
+    if constexpr (TI * TJ <= 8) {
+      Frags F[2][2];
+#pragma unroll
+      for (int q = 0; q < 2 * NL; ++q) read_one(sm, 0, q / NL, fb, F[0][q / NL], q % NL);
+      pin(acc);
+      auto whole = [&](const Frags(&cur)[2], Frags(&nxt)[2], int p) {
+        wait_vmem<(SLOTS - 2) * NL>();
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
+        const uint32_t c = advance(p + SLOTS);
+        const int next = slot + 1 == SLOTS ? 0 : slot + 1;
+        constexpr int NP = TI * TJ;
+        static_assert(2 * NP >= 2 * NL, "reads and copies after products");
+#pragma unroll
+        for (int m = 0; m < 2 * NP; ++m) {
+          const int h = m / NP, i = m % NP / TJ, j = m % TJ;
+          acc[i][j] = T::mfma(cur[h][i], cur[h][TI + j], acc[i][j]);
+          if (m < NL) {
+            read_one(sm, next, 0, fb, nxt[0], m);
+            read_one(sm, next, 1, fb, nxt[1], m);
+          } else if (m < 2 * NL) {
+            issue_one(sm, slot, pa, pb, L, c, wave, m - NL);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = next;
+      };
+      auto last = [&](const Frags(&cur)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = T::mfma(cur[h][i], cur[h][TI + j], acc[i][j]);
+      };
+      int p = 0;
+      for (; p + 2 < count; p += 2) {
+        whole(F[0], F[1], p);
+        whole(F[1], F[0], p + 1);
+      }
+      wait_lds();
+      if (p + 2 == count) {
+        whole(F[0], F[1], p);
+        wait_lds();
+        last(F[1]);
+      } else {
+        last(F[0]);
+      }
+      pin(acc);
+      wait_vmem<0>();
+      __syncthreads();
+      return;
+    }
     Frags F[2];
 #pragma unroll
     for (int q = 0; q < NL; ++q) read_one(sm, 0, 0, fb, F[0], q);
-    int slot = 0;
     pin(acc);
-    for (int p = p0; p < p1; ++p) {
+    for (int p = 0; p < count; ++p) {
       step<false>(sm, F[0], F[1], slot, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
       wait_vmem<(SLOTS - 2) * NL>();
       wait_lds();
       __builtin_amdgcn_s_barrier();
-      addr(p + SLOTS, pa, pb);
+      const uint32_t c = advance(p + SLOTS);
       const int next = slot + 1 == SLOTS ? 0 : slot + 1;
-      step<true>(sm, F[1], F[0], next, 0, slot, pa, pb, L, cut(p + SLOTS), wave, fb, acc);
+      step<true>(sm, F[1], F[0], next, 0, slot, pa, pb, L, c, wave, fb, acc);
       slot = next;
     }
     pin(acc);
