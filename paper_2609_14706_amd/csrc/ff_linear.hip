@@ -4,17 +4,13 @@
 // with alpha folded into the rows: s the rows' scales, b = beta), whose
 // integer sums are exact.
 //
-// Many tokens are bound by the matrix cores: 256 x 256 or 128 x 128 tiles
+// Many tokens are bound by the matrix cores: tiles of 256 x 256 down to 64 x 128
 // (ff_tile_nt.hpp), tiles that run together on an XCD sharing operand rows in
 // its L2, k split and joined by a second kernel where tiles are few.  Few
 // tokens (up to 64) are bound by reading w once: k_skinny gives every wave 16
 // output rows' share of k straight from memory to the matrix cores, with no
 // LDS between, and joins the waves' sums at the end.
 #include <math.h>
-#ifdef FF_DEV
-#include <stdio.h>
-#include <stdlib.h>
-#endif
 
 #include <algorithm>
 #include <type_traits>
@@ -166,8 +162,12 @@ struct Piece {
   }
 };
 
-// grid: tiles x splits.  P: null (one split), or splits x tokens x m sums.
-// Workgroups a compute unit: what its LDS holds.
+// Many tokens.  grid: tiles x splits.  P: null (one split), or splits x tokens
+// x m sums.  Workgroups a compute unit: what its LDS holds.  256 x 256 tiles have
+// the fewest operand bytes per product (1.36 us a pair, 2.0 POP/s in 8 bits for
+// 4096 x 4096 -> 11008: 180 us, of which the last, partly filled round of 688
+// tiles on 256 units costs a tenth); smaller ones fill the units where those
+// are few (1021 x 1000 -> 777 bf16: 12 to 13.5 us, 9 of it a kernel's start and end).
 template <class T, int TI, int TJ, int SLOTS>
 __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) void k_tile(
     LinearArgs a, uint32_t mt, uint32_t ntl, uint32_t splits, typename Scalar<T>::type* P) {
@@ -376,7 +376,9 @@ __device__ __forceinline__ u32x4 row_bytes(const char* row, int k, int bytes) {
 // 128 bytes a step: lane l holds bytes 32 (l / 16) .. + 31 of the step of row
 // (token) l % 16, two matrix instructions' worth; which k a lane holds does not
 // matter as long as both operands agree.  Accumulator element r of lane l:
-// output row 4 (l / 16) + r, token l % 16.
+// output row 4 (l / 16) + r, token l % 16.  Bound by reading w and, as a call is
+// short, by the latency of its first bytes: one token, 4096 -> 11008 in 8 bits,
+// 45 MB, in 10.6 to 13.7 us (3.3 to 4.3 TB/s).
 template <class T, int NT, int RW, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_skinny(LinearArgs a) {
   typedef typename Scalar<T>::type S;
@@ -600,16 +602,6 @@ hipError_t linear_for(const LinearArgs& a, const LinearPlan& p, void* partial, h
 }  // namespace
 
 LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
-#ifdef FF_DEV
-  if (const char* v = getenv("FF_PLAN")) {
-    LinearPlan p{};
-    int sk;
-    if (sscanf(v, "%d,%d,%d,%d,%d", &sk, &p.ti, &p.tj, &p.slots, &p.splits) == 5) {
-      p.skinny = sk;
-      return p;
-    }
-  }
-#endif
   // The fastest of the forms below by a model of their times (us), fitted to
   // sweeps of both types from 1 to 4096 tokens and 300 to 28672 wide.  Per pair
   // of k a workgroup takes `pair` (the latency of its copies, or its products)

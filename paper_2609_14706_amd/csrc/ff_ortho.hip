@@ -17,10 +17,6 @@
 // last product of a step stores both.  Symmetric products compute the tiles on
 // and above the diagonal and store them twice.
 #include <math.h>
-#ifdef FF_DEV
-#include <stdio.h>
-#include <stdlib.h>
-#endif
 
 #include <algorithm>
 
@@ -134,6 +130,12 @@ __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t 
 //   out = alpha C + beta D, D (nullable) laid out as C, in parts;
 // stored by rows (o) and by columns (t), or as the result (user, E), or, k in
 // `splits` parts, as partial sums (sums: splits x batch x rows x c8 fp32).
+// Large ones are bound by the matrix cores (the product with X of a 4096 x 11008
+// bf16 update: 307 to 336 us, 1.10 to 1.20 PFLOP/s, 688 tiles of 256 x 256 making 2.7
+// rounds), small ones by a kernel's start, first reads and stores (5 to 7 us).
+// 3 x 1500 x 1000 fp32, three fp16 products: 26 to 33 us for a symmetric one
+// (tiles of 64 x 64: 408), 49 to 56 for the one with X, whose D and
+// results in parts and both ways are 54 MB, 11 us at a copy's rate.
 struct StepArgs {
   int64_t rows, cols, k;  // k a multiple of 8 (the operands' zeros included)
   Parts L, R, D, o, t;
@@ -451,12 +453,6 @@ constexpr StepForm kAnyForms[] = {{8, 8, 2, 1, 1.36, 1.36, 12.0}, {6, 8, 2, 1, 1
                                   {2, 4, 3, 2, 0.25, 0.50, 3.0}};
 
 StepPlan step_plan(bool sym, bool may_split, int64_t rows, int64_t cols, int64_t k, int64_t batch, int parts) {
-#ifdef FF_DEV
-  if (const char* v = getenv(sym ? may_split ? "FF_GRAM" : "FF_SQUARE" : "FF_STEP")) {
-    StepPlan p{};
-    if (sscanf(v, "%d,%d", &p.form, &p.splits) == 2) return p;
-  }
-#endif
   const int64_t pairs = (k * 2 + nt::kPair - 1) / nt::kPair * (parts == 2 ? 3 : 1);
   StepPlan best{0, 1};
   double least = 1e300;
@@ -612,9 +608,11 @@ Buffers layout(int64_t batch, int64_t m, int64_t n, int parts, char* base) {
 // each in PARTS fp16 parts with rows of whole 64-byte steps of k plus 16 bytes
 // (16 consecutive rows at one k then start in different banks).  A wave takes
 // whole 16 x 16 tiles; what it computes replaces an operand of the others, so
-// it stays in registers until all of them are done (LIMIT tiles a wave).  The matrices are symmetric:
-// a lane's four consecutive rows of one column are stored as four consecutive
-// columns of one row.
+// it stays in registers until all of them are done (LIMIT tiles a wave).  The
+// matrices are symmetric: a lane's four consecutive rows of one column are stored
+// as four consecutive columns of one row.  Bound by LDS reads and their latency:
+// 64 x 128 fp32 in 30 us, 4.5 a step and 8 around them, where the launches of the
+// larger sizes' way are 17 of 5 to 7 us.
 constexpr int kSmallThreads = 1024;
 constexpr int small_tiles(int parts) { return parts == 2 ? 4 : 8; }  // a wave, what LDS holds
 constexpr size_t kSmallLds = 160 * 1024 - 256;
