@@ -96,6 +96,18 @@ def test_q8_longest_sums(gpu):
                       torch.zeros(5, n + 16, dtype=torch.int8, device=gpu), one)
 
 
+@pytest.mark.parametrize("pairs", range(1, 10))
+@pytest.mark.parametrize("T,m", [(70, 100), (200, 130), (300, 500)])
+def test_lengths_of_k(gpu, T, m, pairs):
+    # every number of 128-byte pieces up to more than are ever in flight, whole
+    # and with a last one that is cut
+    for n in (64 * pairs, 64 * pairs - 8, 64 * pairs - 56):
+        x, W = _rand(gpu, T, n, seed=n), _rand(gpu, m, n, seed=n + 1, scale=2 / math.sqrt(n))
+        x64, W64 = x.double(), W.double()
+        want = x64 @ W64.T
+        _close(ffe.linear(x, W)[0], want, n * 2.0 ** -24 * (x64.abs() @ W64.abs().T) + HALF * 1.01 * want.abs() + 1e-30)
+
+
 @pytest.mark.parametrize("T", [3, 40, 200])
 def test_strides_alignment_and_higher_rank(gpu, T):
     n, m = 250, 130
