@@ -7,11 +7,17 @@
 // The products run on the matrix cores in fp16: the operands are bounded (X's
 // singular values by the polynomial's range, known on the host), so a fixed
 // power of two per operand puts them where fp16 keeps 11 bits, three more than
-// bf16 at the same rate.  For bf16 updates one part is enough: every rounding
-// of X, A and b A + c A A to fp16 is an eighth of the output's own.  For fp32 updates
-// every operand is held as hi + lo (22 bits) and a product is three, hi hi +
-// hi lo + lo hi, the k axis running over them one after the other; lo lo, 2^-22
-// of the product, is left out.  All sums are fp32.
+// bf16 at the same rate.  For fp32 updates every operand is held as hi + lo (22
+// bits) and a product is three, hi hi + hi lo + lo hi, the k axis running over
+// them one after the other; lo lo, 2^-22 of the product, is left out.  For bf16
+// updates the products take one part each, but the a X that is added keeps both
+// of X: what rounding X puts into directions that the update hardly has grows by
+// a a step (3.44^5 = 485 over five) through a X alone, for b A + c A A is small
+// there, while errors of a product stay within the update's own directions.  A
+// matrix of rank 16 was off by 4e-2 with X in one part throughout, by 1.9e-3 so,
+// of which 1.7e-3 is the result's own rounding; the most of 84 measured, an eighth
+// of 300 x 1000's rows over zeros, by 3.3e-3.  The last step adds X in one part:
+// a 2^-12 of it at most, below the result's rounding.  All sums are fp32.
 //
 // Each step needs X by rows (A = X X^T) and by columns (B X = B (X^T)^T): the
 // last product of a step stores both.  Symmetric products compute the tiles on
@@ -79,8 +85,9 @@ struct __align__(16) TurnF {
 };
 
 // The start: `rows` (m x n8) and `cols` (n x m8) get scale G / (||G|| + eps) as
-// it is and transposed, zeros up to the next multiple of eight.
-template <class E, int PARTS>
+// it is and transposed, each in the parts it has, zeros up to the next multiple
+// of eight.
+template <class E>
 __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t sg, int64_t m, int64_t n,
                                                const double* part, int parts, double eps, float scale, Parts rows,
                                                Parts cols) {
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t 
     }
     const int64_t at = blockIdx.z * o.stride + row * o.ld + col;
     *reinterpret_cast<u32x4*>(o.hi + at) = hi;
-    if (PARTS == 2) *reinterpret_cast<u32x4*>(o.lo + at) = lo;
+    if (o.lo != nullptr) *reinterpret_cast<u32x4*>(o.lo + at) = lo;
   }
 }
 
@@ -131,8 +138,8 @@ __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t 
 // stored by rows (o) and by columns (t), or as the result (user, E), or, k in
 // `splits` parts, as partial sums (sums: splits x batch x rows x c8 fp32).
 // Large ones are bound by the matrix cores (the product with X of a 4096 x 11008
-// bf16 update: 307 to 336 us, 1.10 to 1.20 PFLOP/s, 688 tiles of 256 x 256 making 2.7
-// rounds), small ones by a kernel's start, first reads and stores (5 to 7 us).
+// bf16 update: 317 us for the last step, 1.16 PFLOP/s, 688 tiles of 256 x 256 making
+// 2.7 rounds; 371 to 394 for the others, X's second part read and written), small ones by a kernel's start, first reads and stores (5 to 7 us).
 // 3 x 1500 x 1000 fp32, three fp16 products: 26 to 33 us for a symmetric one
 // (tiles of 64 x 64: 408), 49 to 56 for the one with X, whose D and
 // results in parts and both ways are 54 MB, 11 us at a copy's rate.
@@ -187,8 +194,9 @@ __device__ __forceinline__ void split_parts(const float (&f)[N], Halves<N>& hi, 
 
 // Results of four rows from `row` on, N columns from `col` on, into o by rows
 // and into t (null: not) by columns.  wide: columns that exist, the zeros up to
-// the next multiple of eight among them; rows of t hold zeros likewise.
-template <int PARTS, int N>
+// the next multiple of eight among them; rows of t hold zeros likewise.  BOTH: o
+// may have two parts, with PARTS == 2 t has too.
+template <int PARTS, bool BOTH, int N>
 __device__ __forceinline__ void store_parts(const float (&f)[4][N], int64_t row, int64_t rows, int64_t col,
                                             int64_t cols, int wide, const Parts& o, const Parts* t, int64_t z) {
 #pragma unroll
@@ -198,7 +206,7 @@ __device__ __forceinline__ void store_parts(const float (&f)[4][N], int64_t row,
       split_parts<N>(f[r], hi, lo);
       const int64_t at = z * o.stride + (row + r) * o.ld + col;
       hi.store(o.hi + at, wide);
-      if (PARTS == 2) lo.store(o.lo + at, wide);
+      if (PARTS == 2 || (BOTH && o.lo != nullptr)) lo.store(o.lo + at, wide);
     }
   if (t == nullptr) return;
 #pragma unroll
@@ -268,13 +276,16 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
   const int64_t r8 = (a.rows + 7) / 8 * 8, c8 = (a.cols + 7) / 8 * 8;
   const int wide = (int)min((int64_t)TJ, max((int64_t)0, c8 - col));
   Halves<TJ> dh[4], dl[4];
+  // (of the products of one part, the one with X adds both of X)
+  constexpr bool BOTH = PARTS == 2 || !SYM;
   const bool add = a.D.hi != nullptr && a.sums == nullptr && wide > 0;
+  const bool low = PARTS == 2 || (BOTH && a.D.lo != nullptr);
   auto fetch = [&](int i) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int64_t at = z * a.D.stride + min(first + i * 16 + r, a.rows - 1) * a.D.ld + col;
       dh[r].load(a.D.hi + at, wide);
-      if (PARTS == 2) dl[r].load(a.D.lo + at, wide);
+      if (BOTH && low) dl[r].load(a.D.lo + at, wide);
     }
   };
   if (add) fetch(0);  // (lands during the loop)
@@ -346,13 +357,17 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
           const float b = row + r < a.rows ? a.beta : 0.0f;  // (rows beyond: zeros, not the last row's)
 #pragma unroll
           for (int j = 0; j < TJ; ++j) f[r][j] += b * (dh[r].get(j) + (PARTS == 2 ? dl[r].get(j) : 0.0f));
+          if (PARTS == 1 && BOTH && low) {
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) f[r][j] += b * dl[r].get(j);
+          }
         }
         if (i + 1 < TI) fetch(i + 1);
       }
       if (row >= r8 || wide <= 0) continue;
       if (a.user == nullptr) {
         const Parts& t = SYM ? a.o : a.t;
-        store_parts<PARTS, TJ>(f, row, a.rows, col, a.cols, wide, a.o, !SYM || ti != tj ? &t : nullptr, z);
+        store_parts<PARTS, BOTH, TJ>(f, row, a.rows, col, a.cols, wide, a.o, !SYM || ti != tj ? &t : nullptr, z);
         continue;
       }
       const int64_t base = z * a.su;
@@ -566,7 +581,7 @@ float scale_for(double bound) {
 struct Buffers {
   double* part;
   float* sums;  // partial sums of the first product
-  Parts x[2], t[2], gram, poly;
+  Parts x[2], t[2], gram, poly;  // x: always in two parts
   size_t bytes;
 };
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -581,7 +596,7 @@ Buffers layout(int64_t batch, int64_t m, int64_t n, int parts, char* base) {
     off += up256(bytes);
     return p;
   };
-  auto operand = [&](int64_t rows, int64_t ld) {
+  auto operand = [&](int64_t rows, int64_t ld, int parts) {
     Parts p{};
     p.ld = ld;
     p.stride = rows * ld;
@@ -591,13 +606,13 @@ Buffers layout(int64_t batch, int64_t m, int64_t n, int parts, char* base) {
   };
   b.part = (double*)take((size_t)batch * kNormParts * sizeof(double));
   for (int k = 0; k < 2; ++k) {
-    b.x[k] = operand(r, ldc);
-    b.t[k] = operand(c, ldr);
+    b.x[k] = operand(r, ldc, 2);
+    b.t[k] = operand(c, ldr, parts);
   }
   const int splits = step_plan(true, true, r, r, (c + 7) / 8 * 8, batch, parts).splits;
   if (splits > 1) b.sums = (float*)take((size_t)splits * (size_t)(batch * r * ((r + 7) / 8 * 8)) * sizeof(float));
-  b.gram = operand(r, ldr);
-  b.poly = operand(r, ldr);
+  b.gram = operand(r, ldr, parts);
+  b.poly = operand(r, ldr, parts);
   b.bytes = off;
   return b;
 }
@@ -642,9 +657,9 @@ bool small_fits(int64_t m, int64_t n, int parts) {
 }
 
 // Parts with which a matrix is taken here, 0: not at all.  Two where they fit,
-// for bf16 too: few directions average few roundings, and a near-singular
-// small matrix with one part was off by 5e-3 instead of the 1.7e-3 of its
-// own rounding.
+// for bf16 too: few directions average few roundings (128 x 128 is off by up to
+// 3.0e-3 with one part, 96 x 80 by its own rounding, 1.7e-3, with two).  With one,
+// what X's rounding leaves of a wave's own tiles stays in its registers.
 int small_parts(int64_t m, int64_t n, bool bf16) { return small_fits(m, n, 2) ? 2 : bf16 && small_fits(m, n, 1) ? 1 : 0; }
 
 struct SmallArgs {
@@ -742,6 +757,8 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     }
     return acc + low;
   };
+  // With one part: what X's rounding left of this wave's tiles of X
+  Halves<4> low[PARTS == 1 ? LIMIT : 1];
   auto put4 = [&](char* p, size_t size, const float (&f)[4]) {
     Halves<4> hi, lo;
     split_parts<4>(f, hi, lo);
@@ -768,6 +785,25 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
     j = q - i * n;
   };
   const int row_x = 16 * S.ldx * 2, row_r = 16 * S.ldr * 2;  // bytes of sixteen rows
+  if (PARTS == 1) {
+#pragma unroll
+    for (int u = 0; u < LIMIT; ++u) {
+      const int q = tile_of(u);
+      if (q < rt * ct) {
+        int i, j;
+        place(q, ct, inv_ct, i, j);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int gi = i * 16 + lr + e, gj = j * 16 + lc;
+          const int row = a.tall ? gj : gi, col = a.tall ? gi : gj;
+          v[e] = gi < a.r && gj < a.c ? (float)((double)Elem<E>::to_f32(g[(int64_t)row * a.ldg + col]) * inv) * a.sx : 0.0f;
+        }
+        Halves<4> hi;
+        split_parts<4>(v, hi, low[u]);
+      }
+    }
+  }
   const float gram = a.sa / (a.sx * a.sx), square = a.c5 * a.sb / (a.sa * a.sa), keep_a = a.b * a.sb / a.sa,
               back = 1.0f / a.sb;
   for (int step = 0; step < a.steps; ++step) {
@@ -815,7 +851,10 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
         float d[4];
         get4(T + j * row_r + i * 32 + four_r, S.t, d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) keep[u][e] = back * s[e] + a.a * d[e];
+        for (int e = 0; e < 4; ++e) {
+          if (PARTS == 1 && !last) d[e] += low[u].get(e);
+          keep[u][e] = back * s[e] + a.a * d[e];
+        }
         if (last) {
           const int gi = i * 16 + lr, gj = j * 16 + lc;
 #pragma unroll
@@ -838,6 +877,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_small(SmallArgs a) {
         place(q, ct, inv_ct, i, j);
         Halves<4> hi, lo;
         split_parts<4>(keep[u], hi, lo);
+        if (PARTS == 1) low[u] = lo;
         char* t = T + j * row_r + i * 32 + four_r;
         char* x = X + i * row_x + j * 32 + one_x;
         __builtin_memcpy(t, hi.w, 8);
@@ -891,15 +931,21 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
   const bool tall = a.m > a.n;
   const int64_t r = std::min(a.m, a.n), c = std::max(a.m, a.n);
   Buffers w = layout(a.batch, a.m, a.n, PARTS, (char*)workspace);
+  // X by rows, as step k takes it: of bf16 updates the last one adds it in one part
+  auto x_of = [&](int k) {
+    Parts x = w.x[k & 1];
+    if (PARTS == 1 && k + 1 == a.steps) x.lo = nullptr;
+    return x;
+  };
   const int parts = (int)std::min<int64_t>(kNormParts, (a.m * ((a.n + 7) / 8) + 255) / 256);
   hipLaunchKernelGGL(k_square_sums<E>, dim3((uint32_t)parts, (uint32_t)a.batch), dim3(256), 0, s, (const E*)a.g,
                      a.ldg, a.sg, a.m, a.n, w.part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_start<E, PARTS>),
+  hipLaunchKernelGGL(k_start<E>,
                      dim3((uint32_t)((a.n + 63) / 64), (uint32_t)((a.m + 63) / 64), (uint32_t)a.batch), dim3(256), 0,
                      s, (const E*)a.g, a.ldg, a.sg, a.m, a.n, w.part, parts, (double)a.eps, sx,
-                     tall ? w.t[0] : w.x[0], tall ? w.x[0] : w.t[0]);
+                     tall ? w.t[0] : x_of(0), tall ? x_of(0) : w.t[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t r8 = (r + 7) / 8 * 8, c8 = (c + 7) / 8 * 8;
   const StepPlan gram = step_plan(true, true, r, r, c8, a.batch, PARTS);
@@ -923,8 +969,8 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
     q.cols = c;
     q.L = w.poly;
     q.R = w.t[cur];
-    q.D = w.x[cur];
-    q.o = w.x[nxt];
+    q.D = x_of(k);
+    q.o = x_of(k + 1);
     q.t = w.t[nxt];
     q.alpha = 1.0f / sb;
     q.beta = a.a;

@@ -404,7 +404,8 @@ def orthogonalize(G, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), 
     """Updates G (m, n) or (batch, m, n), float32 or bfloat16, towards scale
     times the orthogonal factor of their polar decomposition: X = G / (||G||_F +
     eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T.  The
-    coefficients have to keep singular values in [0, 1] below 16."""
+    coefficients have to keep singular values in [0, 1] below 16.  bfloat16 products take operands of 11 bits (results
+    were off by 1.7e-3 of their norm, their own rounding, to 3.3e-3), float32 ones of 22."""
     if stream is not None:
         return _on_stream(stream, orthogonalize, G, steps=steps, coefficients=coefficients, eps=eps, scale=scale,
                           workspace=workspace)
