@@ -450,7 +450,8 @@ typedef enum { FF_ACT_NONE = 0, FF_ACT_RELU = 1, FF_ACT_GELU = 2, FF_ACT_SILU = 
  *     z = x W^T + bias,  y = act(z) + residual            (ff_linear)
  *     z_ti = x_scale_t row_scale_i sum_j x_tj W_ij + bias_i   (ff_linear_q8)
  * ff_linear: x, W, bias, residual, y and preact are bf16.  ff_linear_q8: x and
- * W are int8 (rows of ff_rms_norm, codes Z that fit 8 bits), the rest bf16.
+ * W are int8 (rows of ff_rms_norm, codes Z that fit 8 bits; -128 is taken in both),
+ * the rest bf16.
  * y may be the residual itself (the same rows and ld). */
 typedef struct {
   int64_t tokens, n, m;     /* n, m <= 2^20, n <= 131072 for ff_linear_q8 */

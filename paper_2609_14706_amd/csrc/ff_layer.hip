@@ -120,7 +120,7 @@ ff_status linear_checks(const ff_linear_args* a, bool q8) {
   if (a == nullptr) return bad("args is NULL");
   ff_status rc = linear_sizes(a->tokens, a->n, a->m);
   if (rc != FF_OK) return rc;
-  // 127^2 n stays below 2^31
+  // 128^2 n reaches 2^31 at most, which the kernels still tell apart
   if (q8 && a->n > 131072) return bad("n must be <= 131072 for 8-bit products");
   if (a->tokens > (int64_t(1) << 31)) return bad("tokens must be <= 2^31");
   return FF_OK;

@@ -127,6 +127,15 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t mt, uint32_t nt, ui
 template <class T> struct Scalar { typedef float type; };
 template <> struct Scalar<nt::I8> { typedef int32_t type; };
 
+// Sums of 8-bit products lie in -127 128 n .. 128^2 n, n <= 2^17: the one that 32
+// bits do not hold, 2^31 of (-128)^2 alone at n = 2^17, comes out as -2^31, which is
+// none of them.
+constexpr int64_t kWrapN = int64_t(1) << 17;
+__device__ __forceinline__ float sum_f32(int32_t v) { return v == INT32_MIN ? 0x1p31f : (float)v; }
+__device__ __forceinline__ float sum_f32(float v) { return v; }
+__device__ __forceinline__ int32_t add(int32_t a, int32_t b) { return (int32_t)((uint32_t)a + (uint32_t)b); }
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
 // TJ consecutive bf16 values of a row, as they lie in memory.
 template <int TJ>
 struct Piece {
@@ -266,6 +275,12 @@ __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) vo
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int j = 0; j < TJ; ++j) z[r][j] = (float)s[r][j];
+        if (std::is_same<T, nt::I8>::value && a.n == kWrapN) {  // (for any n it took 3 % of a prompt's time)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) z[r][j] = sum_f32(s[r][j]);
+        }
         if (a.row_scale != nullptr) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(&xs[G::row_of(i, 0)]);
 #pragma unroll
@@ -345,11 +360,11 @@ __global__ __launch_bounds__(256) void k_join(LinearArgs a, const S* P, int spli
           if (k < count) w[k] = p[k];
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] += w[k];
+      for (int k = 0; k < 4; ++k) v[k] = add(v[k], w[k]);
     }
     float f[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = (float)v[k];
+    for (int k = 0; k < 4; ++k) f[k] = sum_f32(v[k]);
     finish<4>(a, t, i, f, count);
   }
 }
@@ -464,8 +479,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_skinny(LinearArgs a) {
     if (t >= a.tokens || i >= a.m) continue;
     S v = sh[0][o];
 #pragma unroll
-    for (int k = 1; k < WAVES; ++k) v += sh[k][o];
-    const float f = (float)v;
+    for (int k = 1; k < WAVES; ++k) v = add(v, sh[k][o]);
+    const float f = sum_f32(v);
     finish<1>(a, t, i, &f, 1);
   }
 }
