@@ -65,6 +65,7 @@ _FN = {}
 def _library():
     """The library's layer functions with their signatures, by name."""
     if not _FN:
+        found = {}
         lib = load_library()
         ref = ctypes.POINTER
         size = ref(_size)
@@ -81,7 +82,8 @@ def _library():
                 "ff_orthogonalize_workspace_size": [ref(ff_ortho_args), size]}.items():
             f = getattr(lib, name)
             f.restype, f.argtypes = _int, args
-            _FN[name] = f
+            found[name] = f
+        _FN.update(found)   # all at once: other threads see none or all of them
     return _FN
 
 
