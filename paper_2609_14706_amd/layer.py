@@ -4,8 +4,8 @@ orthogonalisation of an update of its weights.
 
 Each is one call of the HIP library (include/ff.h) on torch tensors: no state,
 no autograd, results as new tensors on the inputs' device.  Work goes to the
-device's current stream, or to `stream` (ordered by the caller after what made
-the inputs); nothing waits.  Rows are the last dimension, contiguous; a 2-D
+device's current stream, or to `stream`, one of that device (ordered by the
+caller after what made the inputs); nothing waits.  Rows are the last dimension, contiguous; a 2-D
 tensor's rows may lie any distance apart, other shapes have to be contiguous.
 Workspaces are taken from torch unless `workspace` (a uint8 tensor) is given.
 """
@@ -155,11 +155,17 @@ def _elem(t, name):
 
 def _on_stream(stream, fn, *args, **kw):
     """fn on `stream`: its allocations and the inputs' lives are ordered there."""
+    device = getattr(stream, "device", None)
+    if device is None:
+        raise TypeError("stream must be a torch.cuda.Stream")
+    inputs = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor) and t.is_cuda]
+    for t in inputs:
+        if t.device != device:
+            raise ValueError(f"stream is of {device}, the tensors are on {t.device}")
     with torch.cuda.stream(stream):
         out = fn(*args, **kw)
-    for t in (*args, *kw.values()):
-        if isinstance(t, torch.Tensor) and t.is_cuda:
-            t.record_stream(stream)
+    for t in inputs:
+        t.record_stream(stream)
     return out
 
 

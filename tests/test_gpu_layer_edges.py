@@ -1,4 +1,6 @@
 """The layer operators at the ends of what they take."""
+import types
+
 import pytest
 import torch
 
@@ -25,3 +27,24 @@ def test_q8_sums_of_two_to_the_31(gpu, T, m):
     want = rows[:, None] * cols * n
     want[T - 1] += cols
     assert torch.equal(y.cpu(), want.to(BF16))
+
+
+def _calls(gpu):
+    """One call of each function that takes a stream."""
+    x, W, G = torch.ones(40, 64, dtype=BF16, device=gpu), torch.ones(48, 64, dtype=BF16, device=gpu), torch.eye(20, device=gpu)
+    w, dy = torch.ones(64, dtype=BF16, device=gpu), torch.ones(40, 48, dtype=BF16, device=gpu)
+    q, Z = torch.ones(40, 64, dtype=torch.int8, device=gpu), torch.ones(48, 64, dtype=torch.int8, device=gpu)
+    one, beta = torch.ones(40, device=gpu), torch.ones(48, device=gpu)
+    return [lambda **k: ffe.rms_norm(x, w, **k), lambda **k: ffe.rms_norm_q8(x, w, **k), lambda **k: ffe.quantize_rows(x, **k),
+            lambda **k: ffe.rms_norm_backward(x, x, w, **k), lambda **k: ffe.linear(x, W, **k),
+            lambda **k: ffe.linear_q8(q, one, Z, beta, **k), lambda **k: ffe.linear_backward(dy, x, W, **k),
+            lambda **k: ffe.orthogonalize(G, **k)]
+
+
+@pytest.mark.parametrize("which", range(8))
+def test_a_stream_of_another_device(gpu, which):
+    call = _calls(gpu)[which]
+    with pytest.raises(ValueError, match="stream"):
+        call(stream=types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0))
+    with pytest.raises(TypeError, match="stream"):
+        call(stream=7)
