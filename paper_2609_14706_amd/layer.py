@@ -154,7 +154,8 @@ def _elem(t, name):
 
 
 def _on_stream(stream, fn, *args, **kw):
-    """fn on `stream`: its allocations and the inputs' lives are ordered there."""
+    """fn on `stream`: its allocations and the inputs' lives are ordered there,
+    the results' also on the caller's stream, which is to use them."""
     device = getattr(stream, "device", None)
     if device is None:
         raise TypeError("stream must be a torch.cuda.Stream")
@@ -166,6 +167,10 @@ def _on_stream(stream, fn, *args, **kw):
         out = fn(*args, **kw)
     for t in inputs:
         t.record_stream(stream)
+    caller = torch.cuda.current_stream(device)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(caller)
     return out
 
 

@@ -48,3 +48,21 @@ def test_a_stream_of_another_device(gpu, which):
         call(stream=types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0))
     with pytest.raises(TypeError, match="stream"):
         call(stream=7)
+
+
+def test_results_outlive_their_use_on_the_callers_stream(gpu):
+    """A result of another stream that the caller's stream still reads is not
+    handed to the next call on that other stream."""
+    x, W = torch.ones(1536, 512, dtype=BF16, device=gpu), torch.ones(1408, 512, dtype=BF16, device=gpu)
+    s = torch.cuda.Stream(gpu)
+    s.wait_stream(torch.cuda.current_stream(gpu))
+    y, _ = ffe.linear(x, W, stream=s)
+    torch.cuda.current_stream(gpu).wait_stream(s)
+    torch.cuda._sleep(100_000_000)    # some 50 ms
+    copy = y.clone()                  # behind it
+    taken = y.data_ptr()
+    del y
+    again, _ = ffe.linear(x, W, stream=s)
+    assert again.data_ptr() != taken
+    torch.cuda.synchronize()
+    assert torch.equal(copy, again)
