@@ -387,7 +387,8 @@ ff_status ff_kernel_timing(ff_handle h, int kernel, int64_t* launches, double* t
  *     h_j = y_j col_scale_j,  scale = max_j |h_j| / 127,  q_j = rint(h_j / scale).
  * A row of h that is not finite gets a NaN scale and zero codes; one whose largest
  * magnitude is below 2^-118 a zero scale and zero codes.  normalise = 0 leaves the division
- * by the root mean square out (codes of any rows; eps is not used).  sum may be
+ * by the root mean square out (codes of any rows; eps is not used).  The squares
+ * and eps need not fit fp32: rows where they do not are scaled first.  sum may be
  * x or residual themselves (the same rows and ld), and so may y. */
 typedef struct {
   int64_t rows, cols;       /* cols <= 2^24 */

@@ -275,7 +275,7 @@ ff_status ff_rms_norm(const ff_norm_args* a) {
   k.q = a->q;
   k.ldq = a->ldq;
   k.q_scale = a->q_scale;
-  k.eps = (float)a->eps;
+  k.eps = eps_of(a->eps);
   k.normalise = a->normalise;
   return hip(launch_norm(k, a->dtype == FF_BF16, (hipStream_t)a->stream), "norm");
 }
@@ -323,7 +323,7 @@ ff_status ff_rms_norm_backward(const ff_norm_grad_args* a) {
   k.dx = a->ds;
   k.lddx = a->ldds;
   k.part = a->dweight != nullptr ? (float*)a->workspace : nullptr;
-  k.eps = (float)a->eps;
+  k.eps = eps_of(a->eps);
   if ((rc = hip(launch_norm_grad(k, bf16, s), "norm gradient")) != FF_OK || a->dweight == nullptr) return rc;
   return hip(launch_col_sums(k.part, norm_grad_parts(a->rows), a->cols, a->dweight, bf16, s), "norm gradient's sums");
 }

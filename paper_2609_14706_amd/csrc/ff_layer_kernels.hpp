@@ -12,6 +12,11 @@ namespace ff {
 typedef uint16_t bf16_t;
 
 // --------------------------------------------------------------------- norm
+// eps as it is added to mean s^2, and for s scaled up or down by the kernels' factors
+struct Eps {
+  float plain, up, down;
+};
+Eps eps_of(double eps);
 // Rows of `cols` elements (bf16 or fp32), leading dimensions in elements.
 struct NormArgs {
   int64_t rows, cols;
@@ -28,7 +33,7 @@ struct NormArgs {
   int8_t* q;  // codes, or null (then y)
   int64_t ldq;
   float* q_scale;  // rows
-  float eps;
+  Eps eps;
   int normalise;  // 0: codes of x (+ residual) itself
 };
 hipError_t launch_norm(const NormArgs& a, bool bf16, hipStream_t s);
@@ -45,7 +50,7 @@ struct NormGradArgs {
   void* dx;
   int64_t lddx;
   float* part;  // norm_grad_parts(rows) x cols partial sums of dw, or null
-  float eps;
+  Eps eps;
 };
 int64_t norm_grad_parts(int64_t rows);
 hipError_t launch_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t s);

@@ -13,10 +13,13 @@
 // pass (k_norm_long, k_norm_grad_long).  8192 x 8192 bf16 with residual to 8
 // bits: 99 us, 4.7 TB/s where a large copy reaches 5.1; gradient of 8191 x 4096:
 // 57 us (4.7 TB/s) and 5 us for the sums of dw.
-// All sums are fp32, in an order fixed by the sizes.
+// All sums are fp32, in an order fixed by the sizes.  A row whose squares leave
+// fp32's range (mean s^2 + eps not in 2^-100 .. 2^128) is summed again with s and
+// eps scaled by a power of two.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ff_layer_kernels.hpp"
 #include "ff_vec.hpp"
@@ -47,6 +50,19 @@ __device__ __forceinline__ float row_reduce(float v, float* red, Op op) {
 struct Add {
   __device__ float operator()(float a, float b) const { return a + b; }
 };
+// Whether fp32 holds m = mean s^2 + eps and the squares that matter in it; if
+// not, the factor of s with which it does, kUp or kDown (a row of NaN or infinities
+// gets one too, to no effect), and eps with it.  s from 2^-149 on to 2^-43 becomes
+// 2^-49 .. 2^57, from 2^57 on 2^-23 .. 2^48.
+constexpr float kUp = 0x1p100f, kDown = 0x1p-80f;
+__device__ __forceinline__ bool in_range(float m) { return m >= 0x1p-100f && m < INFINITY; }
+struct One {};
+__device__ __forceinline__ float operator*(float v, One) { return v; }
+// A value that every lane of the wave holds, as one for all of them.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
 // Largest bit pattern: of magnitudes the largest, and a NaN above them all.
 struct MaxBits {
   __device__ float operator()(float a, float b) const {
@@ -141,13 +157,24 @@ __global__ __launch_bounds__(block_of(THR)) void k_norm(NormArgs a) {
     }
     float inv_rms = 1.0f;
     if (a.normalise) {
-      float ss = 0.0f;
+      float eps = a.eps.plain;
+#pragma unroll 1
+      for (int pass = 0;; ++pass) {  // (every thread of a row takes the same passes)
+        float ss = 0.0f;
 #pragma unroll
-      for (int k = 0; k < VPT; ++k)
+        for (int k = 0; k < VPT; ++k)
 #pragma unroll
-        for (int i = 0; i < N; ++i) ss += s[k][i] * s[k][i];
-      ss = row_reduce<THR>(ss, red, Add());
-      inv_rms = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+          for (int i = 0; i < N; ++i) ss += s[k][i] * s[k][i];
+        const float m = uniform(row_reduce<THR>(ss, red, Add()) / (float)a.cols + eps);
+        inv_rms = 1.0f / sqrtf(m);
+        if (pass == 1 || in_range(m)) break;
+        const float f = m < 1.0f ? kUp : kDown;
+        eps = m < 1.0f ? a.eps.up : a.eps.down;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k)
+#pragma unroll
+          for (int i = 0; i < N; ++i) s[k][i] *= f;
+      }
     }
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
@@ -208,17 +235,23 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
     const E* x = (const E*)a.x + row * a.ldx;
     const E* r = a.residual != nullptr ? (const E*)a.residual + row * a.ldr : nullptr;
     auto at = [&](int64_t j) { return f32<E>(x[j]) + (r != nullptr ? f32<E>(r[j]) : 0.0f); };
-    float inv_rms = 1.0f;
+    float inv_rms = 1.0f, f = 1.0f;
     if (a.normalise) {
-      float ss = 0.0f;
-      for (int64_t j = threadIdx.x; j < a.cols; j += 1024) ss += at(j) * at(j);
-      ss = row_reduce<1024>(ss, red, Add());
-      inv_rms = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+      float eps = a.eps.plain;
+      for (int pass = 0;; ++pass) {
+        float ss = 0.0f;
+        for (int64_t j = threadIdx.x; j < a.cols; j += 1024) ss += (at(j) * f) * (at(j) * f);
+        const float m = uniform(row_reduce<1024>(ss, red, Add()) / (float)a.cols + eps);
+        inv_rms = 1.0f / sqrtf(m);
+        if (pass == 1 || in_range(m)) break;
+        f = m < 1.0f ? kUp : kDown;
+        eps = m < 1.0f ? a.eps.up : a.eps.down;
+      }
     }
     auto h = [&](int64_t j) {
       float c = W != nullptr ? f32<E>(W[j]) : 1.0f;
       if (Q8 && a.col_scale != nullptr) c *= a.col_scale[j];
-      return at(j) * inv_rms * c;
+      return at(j) * f * inv_rms * c;
     };
     float scale = 0.0f, inv = 0.0f;
     if (Q8) {
@@ -240,7 +273,9 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
 }
 
 // Gradient: as k_norm, with the columns' share of dw summed over the
-// workgroup's rows and left in part[workgroup][column].
+// workgroup's rows and left in part[workgroup][column].  Rows that need scaling
+// are left to a second turn over the workgroup's rows, taken only where there is one:
+// in one turn they cost all rows registers (1024 x 32768 bf16: 192 us, 124 so).
 template <class E, int THR, int VPT>
 __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
   constexpr int N = Vec<E>::N, RPB = block_of(THR) / THR;
@@ -257,53 +292,84 @@ __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
     for (int i = 0; i < N; ++i) dw[k][i] = 0.0f;
   }
   auto w = [&](int k, int i) { return a.weight != nullptr ? vw[k].get(i) : 1.0f; };
-  for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / THR; row < a.rows;
-       row += (int64_t)gridDim.x * RPB) {
-    Vec<E> vs[VPT], vd[VPT], vt[VPT];
+  // RARE: the rows that the other turn left; returns whether it left any (the
+  // same for every thread of a row, and of a workgroup of one row at a time)
+  auto turn = [&](auto rare) {
+    constexpr bool RARE = decltype(rare)::value;
+    bool left_over = false;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / THR; row < a.rows;
+         row += (int64_t)gridDim.x * RPB) {
+      Vec<E> vs[VPT], vd[VPT], vt[VPT];
 #pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-      const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
-      if (left > 0) {
-        vs[k] = load_row((const E*)a.s + row * a.lds + j, left);
-        vd[k] = load_row((const E*)a.dy + row * a.lddy + j, left);
-        if (a.dsum != nullptr) vt[k] = load_row((const E*)a.dsum + row * a.lddsum + j, left);
-      } else {
-        vs[k].w = vd[k].w = vt[k].w = u32x4{0, 0, 0, 0};
-      }
-    }
-    float ss = 0.0f, us = 0.0f;
-#pragma unroll
-    for (int k = 0; k < VPT; ++k)
-      if (a.cols - (int64_t)(k * THR + t) * N > 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float s = vs[k].get(i);
-          ss += s * s;
-          us += vd[k].get(i) * w(k, i) * s;
+      for (int k = 0; k < VPT; ++k) {
+        const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
+        if (left > 0) {
+          vs[k] = load_row((const E*)a.s + row * a.lds + j, left);
+          vd[k] = load_row((const E*)a.dy + row * a.lddy + j, left);
+          if (a.dsum != nullptr) vt[k] = load_row((const E*)a.dsum + row * a.lddsum + j, left);
+        } else {
+          vs[k].w = vd[k].w = vt[k].w = u32x4{0, 0, 0, 0};
         }
       }
-    ss = row_reduce<THR>(ss, red, Add());
-    us = row_reduce<THR>(us, red + 16, Add());
-    const float i1 = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
-    const float proj = us / (float)a.cols * i1 * i1;
+      float us;
+      auto sums = [&](float eps) {  // us of what vs holds; returns mean s^2 + eps
+        float ss = 0.0f;
+        us = 0.0f;
 #pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-      const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
-      if (left > 0) {
-        float g[N];
+        for (int k = 0; k < VPT; ++k)
+          if (a.cols - (int64_t)(k * THR + t) * N > 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float s = vs[k].get(i), d = vd[k].get(i);
-          dw[k][i] += d * s * i1;
-          g[i] = i1 * (d * w(k, i) - s * proj);
-          if (a.dsum != nullptr) g[i] += vt[k].get(i);
+            for (int i = 0; i < N; ++i) {
+              const float s = vs[k].get(i);
+              ss += s * s;
+              us += vd[k].get(i) * w(k, i) * s;
+            }
+          }
+        ss = row_reduce<THR>(ss, red, Add());
+        us = row_reduce<THR>(us, red + 16, Add());
+        return ss / (float)a.cols + eps;
+      };
+      float m = sums(a.eps.plain), f = 1.0f;
+      if (__builtin_expect(in_range(m) == RARE, 0)) {
+        left_over = true;
+        continue;
+      }
+      if (RARE) {
+        f = m < 1.0f ? kUp : kDown;
+        const float eps = m < 1.0f ? a.eps.up : a.eps.down;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {  // (what this takes below the type's range does not matter beside the rest)
+          float s[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) s[i] = vs[k].get(i) * f;
+          vs[k].set(s);
         }
-        Vec<E> o;
-        o.set(g);
-        store_row((E*)a.dx + row * a.lddx + j, o, left);
+        m = sums(eps);
+      }
+      const float i1 = 1.0f / sqrtf(m);
+      const float proj = us / (float)a.cols * i1 * i1;
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
+        if (left > 0) {
+          float g[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float s = vs[k].get(i), d = vd[k].get(i);
+            dw[k][i] += d * s * i1;
+            g[i] = i1 * (d * w(k, i) - s * proj);
+            if (RARE) g[i] *= f;
+            if (a.dsum != nullptr) g[i] += vt[k].get(i);
+          }
+          Vec<E> o;
+          o.set(g);
+          store_row((E*)a.dx + row * a.lddx + j, o, left);
+        }
       }
     }
-  }
+    return left_over;
+  };
+  if (__builtin_expect(turn(std::false_type()), 0)) turn(std::true_type());
   if (a.part == nullptr) return;
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
   if (RPB > 1) {
@@ -338,23 +404,31 @@ __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
     const E* s = (const E*)a.s + row * a.lds;
     const E* dy = (const E*)a.dy + row * a.lddy;
     const E* ds = a.dsum != nullptr ? (const E*)a.dsum + row * a.lddsum : nullptr;
-    float ss = 0.0f, us = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += 1024) {
-      const float v = f32<E>(s[j]);
-      ss += v * v;
-      us += f32<E>(dy[j]) * (W != nullptr ? f32<E>(W[j]) : 1.0f) * v;
-    }
-    ss = row_reduce<1024>(ss, red, Add());
-    us = row_reduce<1024>(us, red + 16, Add());
-    const float i1 = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
-    const float proj = us / (float)a.cols * i1 * i1;
-    for (int64_t j = threadIdx.x; j < a.cols; j += 1024) {
-      const float v = f32<E>(s[j]), d = f32<E>(dy[j]);
-      if (part != nullptr) part[j] += d * v * i1;
-      float g = i1 * (d * (W != nullptr ? f32<E>(W[j]) : 1.0f) - v * proj);
-      if (ds != nullptr) g += f32<E>(ds[j]);
-      ((E*)a.dx)[row * a.lddx + j] = Elem<E>::from_f32(g);
-    }
+    // the row with s scaled by f; returns mean s^2 + eps, and stores where it is in
+    // range or f is not one
+    auto turn = [&](auto f, float eps) {
+      float ss = 0.0f, us = 0.0f;
+      for (int64_t j = threadIdx.x; j < a.cols; j += 1024) {
+        const float v = f32<E>(s[j]) * f;
+        ss += v * v;
+        us += f32<E>(dy[j]) * (W != nullptr ? f32<E>(W[j]) : 1.0f) * v;
+      }
+      ss = row_reduce<1024>(ss, red, Add());
+      us = row_reduce<1024>(us, red + 16, Add());
+      const float m = uniform(ss / (float)a.cols + eps), i1 = 1.0f / sqrtf(m);
+      if (std::is_same<decltype(f), One>::value && !in_range(m)) return m;
+      const float proj = us / (float)a.cols * i1 * i1;
+      for (int64_t j = threadIdx.x; j < a.cols; j += 1024) {
+        const float v = f32<E>(s[j]) * f, d = f32<E>(dy[j]);
+        if (part != nullptr) part[j] += d * v * i1;
+        float g = i1 * (d * (W != nullptr ? f32<E>(W[j]) : 1.0f) - v * proj) * f;
+        if (ds != nullptr) g += f32<E>(ds[j]);
+        ((E*)a.dx)[row * a.lddx + j] = Elem<E>::from_f32(g);
+      }
+      return m;
+    };
+    const float m = turn(One(), a.eps.plain);
+    if (!in_range(m)) turn(m < 1.0f ? kUp : kDown, m < 1.0f ? a.eps.up : a.eps.down);
   }
 }
 
@@ -435,6 +509,12 @@ hipError_t grad_for(const NormGradArgs& a, hipStream_t s) {
 // compute unit; few rows take one, their partial sums weigh as much as they do
 // (2048 x 16384 bf16: 82 us with 512, 67 us with 256; 8191 x 4096: 60 and 84).
 int64_t norm_grad_parts(int64_t rows) { return std::min<int64_t>(rows, rows < 4096 ? 256 : 512); }
+
+Eps eps_of(double eps) {
+  // (positive where eps is: rows of zeros stay zeros)
+  auto at = [&](double f) { return eps > 0.0 ? std::max((float)(eps * f * f), 0x1p-149f) : 0.0f; };
+  return {at(1.0), at(kUp), at(kDown)};
+}
 
 hipError_t launch_norm(const NormArgs& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0 || a.cols <= 0) return hipErrorInvalidValue;

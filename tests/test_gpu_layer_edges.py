@@ -66,3 +66,62 @@ def test_results_outlive_their_use_on_the_callers_stream(gpu):
     assert again.data_ptr() != taken
     torch.cuda.synchronize()
     assert torch.equal(copy, again)
+
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}    # half a unit of a rounded value
+SUMS = 2.0 ** -16                                # fp32 sums, relative to the sum of magnitudes
+DT = {"bf16": BF16, "f32": torch.float32}
+
+
+def _rows(gpu, n, dtype, eps):
+    """Rows over all of the type's range that eps leaves a norm of any size to."""
+    g = torch.Generator().manual_seed(n)
+    sizes = torch.tensor([1e-36, 1e-30, 1e-24, 1e-19, 1e-12, 1.0, 1e12, 1e19, 1e24, 1e30, 1e37, 3.0], dtype=torch.float64)
+    x = torch.randn(12, n, generator=g, dtype=torch.float64) * sizes[:, None]
+    x[11, 0] = 1e30           # one large entry among others
+    return x.to(DT[dtype]).to(gpu)
+
+
+# rows of a wave, of a workgroup of every kind, too long for registers
+@pytest.mark.parametrize("n", [5, 700, 1500, 3000, 8192, 9000, 16000, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("eps", [0.0, 1e-70, 1e-6, 1e50])
+def test_norms_of_rows_of_any_size(gpu, n, dtype, eps):
+    x = _rows(gpu, n, dtype, eps)
+    g = torch.Generator().manual_seed(n + 1)
+    dy = torch.randn(12, n, generator=g).to(DT[dtype]).to(gpu)
+    w = (torch.rand(n, generator=g) + 0.5).to(DT[dtype]).to(gpu)
+    x64, w64, u = x.double(), w.double(), dy.double() * w.double()
+    i = 1 / torch.sqrt(x64.square().mean(-1, keepdim=True) + eps)
+    tiny = 1e-37              # what lies below the normal numbers of both types
+    want = x64 * i * w64
+    y, _ = ffe.rms_norm(x, w, eps=eps)
+    assert bool(((y.double() - want).abs() <= (HALF[dtype] + SUMS) * want.abs() + tiny).all())
+    q, scale, _ = ffe.rms_norm_q8(x, w, eps=eps)
+    top = want.abs().amax(-1)
+    some = top > 1e-35        # (a scale below the normal numbers counts as zeros)
+    assert bool((scale.double() - top / 127)[some].abs().le(SUMS * top[some] / 127).all())
+    assert bool((q.double() * scale.double()[:, None] - want)[some].abs().le(0.51 * top[some][:, None] / 127).all())
+    ds, dw = ffe.rms_norm_backward(dy, x, w, eps=eps)
+    mean = (u * x64).mean(-1, keepdim=True)
+    want = i * (u - x64 * i * i * mean)
+    mag = i * (u.abs() + x64.abs() * i * i * (u * x64).abs().mean(-1, keepdim=True))
+    fits = mag.amax(-1) < 1e38
+    off = (ds.double() - want).abs() <= HALF[dtype] * want.abs() + SUMS * mag + tiny
+    assert bool(off[fits].all())
+    share = dy.double() * x64 * i
+    assert bool(((dw.double() - share.sum(0)).abs() <= HALF[dtype] * share.sum(0).abs() + SUMS * share.abs().sum(0) + tiny).all())
+
+
+@pytest.mark.parametrize("n", [64, 700, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("eps", [1e-300, 1e-50, 1e-30, 1e300])
+def test_zero_rows_with_any_eps(gpu, n, dtype, eps):
+    """An eps that fp32 does not hold still keeps rows of zeros zeros."""
+    x = torch.zeros(7, n, dtype=DT[dtype], device=gpu)
+    w = torch.ones(n, dtype=DT[dtype], device=gpu)
+    assert not bool(ffe.rms_norm(x, w, eps=eps)[0].any())
+    q, scale, _ = ffe.rms_norm_q8(x, w, eps=eps)
+    assert not bool(q.any()) and not bool(scale.any())
+    ds, dw = ffe.rms_norm_backward(x, x, w, eps=eps)
+    assert not bool(ds.any()) and not bool(dw.any())
