@@ -535,7 +535,7 @@ typedef struct {
   int steps;                /* 1 .. 64 */
   double a, b, c;
   double eps;               /* >= 0 */
-  double scale;             /* finite */
+  double scale;             /* in fp32's range */
   void* workspace;
   size_t workspace_bytes;
   void* stream;

@@ -476,6 +476,7 @@ ff_status ff_orthogonalize(const ff_ortho_args* a) {
   for (double v : {a->a, a->b, a->c, a->eps, a->scale})
     if (!std::isfinite(v)) return bad("a, b, c, eps and scale must be finite");
   if (a->eps < 0.0) return bad("eps must be >= 0");
+  if (!std::isfinite((float)a->scale)) return bad("scale must be in fp32's range");
   if (!ortho_bounded(a->steps, a->a, a->b, a->c))
     return bad("the coefficients take singular values in [0, 1] to 16 or more");
   if (a->batch == 0) return FF_OK;
@@ -504,7 +505,7 @@ ff_status ff_orthogonalize(const ff_ortho_args* a) {
   k.a = (float)a->a;
   k.b = (float)a->b;
   k.c = (float)a->c;
-  k.eps = (float)a->eps;
+  k.eps = a->eps;
   k.scale = (float)a->scale;
   k.bf16 = a->dtype == FF_BF16;
   return hip(launch_ortho(k, a->workspace, (hipStream_t)a->stream), "orthogonalisation");

@@ -133,7 +133,8 @@ struct OrthoArgs {
   void* out;
   int64_t ldo, so;
   int steps;
-  float a, b, c, eps, scale;
+  float a, b, c, scale;
+  double eps;
   bool bf16;
 };
 // Whether the coefficients keep every singular value that starts in [0, 1]

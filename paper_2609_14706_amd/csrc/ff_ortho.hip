@@ -914,7 +914,7 @@ hipError_t run_small(const OrthoArgs& a, float sx, float sa, float sb, hipStream
   q.sx = sx;
   q.sa = sa;
   q.sb = sb;
-  q.eps = (double)a.eps;
+  q.eps = a.eps;
   hipLaunchKernelGGL((k_small<E, PARTS>), dim3((uint32_t)a.batch), dim3(kSmallThreads),
                      (uint32_t)small_layout(q.r, q.c, PARTS).bytes, s, q);
   return hipGetLastError();
@@ -944,7 +944,7 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_start<E>,
                      dim3((uint32_t)((a.n + 63) / 64), (uint32_t)((a.m + 63) / 64), (uint32_t)a.batch), dim3(256), 0,
-                     s, (const E*)a.g, a.ldg, a.sg, a.m, a.n, w.part, parts, (double)a.eps, sx,
+                     s, (const E*)a.g, a.ldg, a.sg, a.m, a.n, w.part, parts, a.eps, sx,
                      tall ? w.t[0] : x_of(0), tall ? x_of(0) : w.t[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t r8 = (r + 7) / 8 * 8, c8 = (c + 7) / 8 * 8;

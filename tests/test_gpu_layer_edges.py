@@ -125,3 +125,17 @@ def test_zero_rows_with_any_eps(gpu, n, dtype, eps):
     assert not bool(q.any()) and not bool(scale.any())
     ds, dw = ffe.rms_norm_backward(x, x, w, eps=eps)
     assert not bool(ds.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n", [(40, 50), (128, 128), (300, 200)])
+def test_updates_with_any_eps(gpu, m, n, dtype):
+    """An eps that fp32 does not hold: zeros stay zeros, tiny updates keep their size beside it."""
+    for eps in (1e-300, 1e-50, 1e300):
+        assert not bool(ffe.orthogonalize(torch.zeros(m, n, dtype=DT[dtype], device=gpu), eps=eps).any())
+    g = torch.Generator().manual_seed(m)
+    G = (1e-30 * torch.randn(m, n, generator=g)).to(DT[dtype]).to(gpu)
+    assert torch.equal(ffe.orthogonalize(G, eps=1e-60), ffe.orthogonalize(G, eps=0.0))
+    assert not bool(ffe.orthogonalize(G, eps=1e300).any())
+    with pytest.raises(ffe.FlipFlopError):
+        ffe.orthogonalize(G, scale=1e39)
