@@ -223,9 +223,9 @@ def _norm(x, weight, residual, eps, col_scale, q8, normalise):
     pr = ldr = ps = 0
     s = scale = None
     if residual is not None:
+        pr, ldr, _, _ = _rows(residual, "residual", dtype, dev, c)
         if residual.shape != x.shape:
             raise ValueError(f"residual must have x's shape {tuple(x.shape)}")
-        pr, ldr, _, _ = _rows(residual, "residual", dtype, dev, c)
         if normalise:
             s = _like(x, dtype)
             ps = s.data_ptr()
@@ -282,11 +282,11 @@ def rms_norm_backward(dy, s, weight=None, *, eps: float = 1e-6, dsum=None, works
     dt = _elem(s, "s")
     ps, lds, r, c = _rows(s, "s", s.dtype, dev)
     a = ff_norm_grad_args(r, c, dt, ps, lds)
-    if dy.shape != s.shape or (dsum is not None and dsum.shape != s.shape):
-        raise ValueError(f"dy and dsum must have the shape of s, {tuple(s.shape)}")
     a.dy, a.lddy, _, _ = _rows(dy, "dy", s.dtype, dev, c)
     if dsum is not None:
         a.dsum, a.lddsum, _, _ = _rows(dsum, "dsum", s.dtype, dev, c)
+    if dy.shape != s.shape or (dsum is not None and dsum.shape != s.shape):
+        raise ValueError(f"dy and dsum must have the shape of s, {tuple(s.shape)}")
     a.weight = _vector(weight, "weight", s.dtype, dev, c)
     a.eps = eps
     ds = _like(s, s.dtype)
@@ -307,9 +307,9 @@ def _linear(name, x, weight, dtype, x_scale, row_scale, bias, residual, activati
         _library()
     dev = _first(x, "x")
     px, ldx, T, n = _rows(x, "x", dtype, dev)
-    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
-        raise ValueError("weight must be a 2-D tensor (m, n)")
     pw, ldw, m, _ = _rows(weight, "weight", dtype, dev, n)
+    if weight.dim() != 2:
+        raise ValueError("weight must be a 2-D tensor (m, n)")
     bf16 = torch.bfloat16
     q8 = x_scale is not None
     ps = pb = pr = pm = pz = None
@@ -321,9 +321,9 @@ def _linear(name, x, weight, dtype, x_scale, row_scale, bias, residual, activati
         pb = _vector(bias, "bias", bf16, dev, m)
     shape = (T, m) if x.dim() == 2 else x.shape[:-1] + (m,)
     if residual is not None:
+        pr, ldr, _, _ = _rows(residual, "residual", bf16, dev, m)
         if residual.shape != shape:
             raise ValueError(f"residual must have the output's shape {tuple(shape)}")
-        pr, ldr, _, _ = _rows(residual, "residual", bf16, dev, m)
     y = torch.empty(shape, dtype=bf16, device=dev)
     z = None
     if keep_preact:
@@ -379,20 +379,22 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     dev = _first(x, "x")
     bf16 = torch.bfloat16
     px, ldx, T, n = _rows(x, "x", bf16, dev)
-    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
-        raise ValueError("weight must be a 2-D tensor (m, n)")
     pw, ldw, m, _ = _rows(weight, "weight", bf16, dev, n)
+    if weight.dim() != 2:
+        raise ValueError("weight must be a 2-D tensor (m, n)")
     shape = (T, m) if x.dim() == 2 else x.shape[:-1] + (m,)
+    pdy, lddy, _, _ = _rows(dy, "dy", bf16, dev, m)
     if dy.shape != shape:
         raise ValueError(f"dy must have the output's shape {tuple(shape)}")
-    pdy, lddy, _, _ = _rows(dy, "dy", bf16, dev, m)
     a = ff_linear_grad_args(T, n, m, pdy, lddy, px, ldx, pw, ldw)
     a.activation = _act(activation)
     g = dy
     if a.activation:
-        if preact is None or preact.shape != shape:
+        if preact is None:
             raise ValueError(f"preact of shape {tuple(shape)} is needed with an activation")
         a.preact, a.ldz, _, _ = _rows(preact, "preact", bf16, dev, m)
+        if preact.shape != shape:
+            raise ValueError(f"preact must have the output's shape {tuple(shape)}")
         g = _like(dy, bf16)
         a.g, a.ldg = g.data_ptr(), m
     dx = dw = db = None

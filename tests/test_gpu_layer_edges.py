@@ -139,3 +139,15 @@ def test_updates_with_any_eps(gpu, m, n, dtype):
     assert not bool(ffe.orthogonalize(G, eps=1e300).any())
     with pytest.raises(ffe.FlipFlopError):
         ffe.orthogonalize(G, scale=1e39)
+
+
+def test_what_is_no_tensor(gpu):
+    x, W, dy = (torch.ones(*s, dtype=BF16, device=gpu) for s in ((4, 64), (48, 64), (4, 48)))
+    for bad in (7, [1.0], "x", dy.cpu()):
+        for call in (lambda: ffe.rms_norm(x, residual=bad), lambda: ffe.rms_norm(x, bad),
+                     lambda: ffe.rms_norm_backward(bad, x), lambda: ffe.rms_norm_backward(x, x, dsum=bad),
+                     lambda: ffe.linear(x, bad), lambda: ffe.linear(x, W, residual=bad), lambda: ffe.linear(x, W, bias=bad),
+                     lambda: ffe.linear_backward(bad, x, W), lambda: ffe.linear_backward(dy, x, bad),
+                     lambda: ffe.linear_backward(dy, x, W, preact=bad, activation="silu"), lambda: ffe.orthogonalize(bad)):
+            with pytest.raises(TypeError, match="CUDA tensor"):
+                call()
