@@ -88,6 +88,11 @@ struct LinearPlan {
   int splits;
 };
 LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes);
+// The few-token kernel's 16-token and 16-output tiles and waves of a workgroup.
+struct SkinnyPlan {
+  int nt, rw, waves;
+};
+SkinnyPlan skinny_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes);
 // Bytes of the partial sums of a plan (0 with one split).
 size_t linear_partial_bytes(const LinearPlan& p, int64_t tokens, int64_t m);
 // Whether the tiles take rows from p on, ld elements apart, of n elements:
@@ -140,6 +145,14 @@ struct OrthoArgs {
 // Whether the coefficients keep every singular value that starts in [0, 1]
 // below 16 through the steps.
 bool ortho_bounded(int steps, double a, double b, double c);
+// How updates are run: `small` parts in one workgroup each, or (0) step by step,
+// the three products of a step by their forms (ff_ortho.hip), A = X X^T with k in
+// `gram_splits` parts.
+struct OrthoPlan {
+  int small;
+  int gram, gram_splits, square, apply;
+};
+OrthoPlan ortho_plan(int64_t batch, int64_t m, int64_t n, bool bf16);
 size_t ortho_workspace(int64_t batch, int64_t m, int64_t n, bool bf16);
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t s);
 

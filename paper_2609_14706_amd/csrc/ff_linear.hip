@@ -67,7 +67,7 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   return 1.0f;
 }
 
-// W consecutive outputs of row t from column i on (W = 1, 2, 4 or 8), `count` of
+// W consecutive outputs of row t from column i on (W = 1 or 4), `count` of
 // them inside the matrix.
 template <int W>
 __device__ __forceinline__ void finish(const LinearArgs& a, int64_t t, int64_t i, const float* acc, int count) {
@@ -582,31 +582,38 @@ hipError_t tiles(const LinearArgs& a, const LinearPlan& p, void* partial, hipStr
   return hipGetLastError();
 }
 
+// Waves that a form of the few-token kernel is ever given: two output tiles are for
+// 256 workgroups and more, with which eight waves do, and for more than 32 tokens
+// only a short k is taken there at all.
+constexpr int most_waves(int nt, int rw) { return rw == 1 ? 16 : nt == 2 ? 8 : 4; }
+
 template <class T, int NT, int RW>
-hipError_t skinny_waves(const LinearArgs& a, hipStream_t s) {
-  const int64_t groups = (a.m + 16 * RW - 1) / (16 * RW);
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  const int64_t steps = (a.n * T::kBytes + 127) / 128;
-  // enough waves to keep memory busy (8 a compute unit), each with four steps
-  // or more
-  int waves = 4;
-  while (waves < 16 && groups * waves < 2048 && steps >= 8 * waves) waves *= 2;
-  const dim3 grid((uint32_t)groups);
-  if (waves == 4)
+hipError_t skinny_waves(const LinearArgs& a, int waves, hipStream_t s) {
+  const dim3 grid((uint32_t)((a.m + 16 * RW - 1) / (16 * RW)));
+  if (waves == 4) {
     hipLaunchKernelGGL((k_skinny<T, NT, RW, 4>), grid, dim3(256), 0, s, a);
-  else if (waves == 8)
-    hipLaunchKernelGGL((k_skinny<T, NT, RW, 8>), grid, dim3(512), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_skinny<T, NT, RW, 16>), grid, dim3(1024), 0, s, a);
-  return hipGetLastError();
+    return hipGetLastError();
+  }
+  if constexpr (most_waves(NT, RW) >= 8)
+    if (waves == 8) {
+      hipLaunchKernelGGL((k_skinny<T, NT, RW, 8>), grid, dim3(512), 0, s, a);
+      return hipGetLastError();
+    }
+  if constexpr (most_waves(NT, RW) >= 16)
+    if (waves == 16) {
+      hipLaunchKernelGGL((k_skinny<T, NT, RW, 16>), grid, dim3(1024), 0, s, a);
+      return hipGetLastError();
+    }
+  return hipErrorInvalidValue;
 }
 
 template <class T>
 hipError_t linear_for(const LinearArgs& a, const LinearPlan& p, void* partial, hipStream_t s) {
   if (p.skinny) {
-    if (a.tokens <= 16) return skinny_waves<T, 1, 1>(a, s);
-    if (a.tokens <= 32) return a.m >= 8192 ? skinny_waves<T, 2, 2>(a, s) : skinny_waves<T, 2, 1>(a, s);
-    return a.m >= 8192 ? skinny_waves<T, 4, 2>(a, s) : skinny_waves<T, 4, 1>(a, s);
+    const SkinnyPlan k = skinny_plan(a.tokens, a.n, a.m, T::kBytes);
+    if (k.nt == 1) return skinny_waves<T, 1, 1>(a, k.waves, s);
+    if (k.nt == 2) return k.rw == 2 ? skinny_waves<T, 2, 2>(a, k.waves, s) : skinny_waves<T, 2, 1>(a, k.waves, s);
+    return k.rw == 2 ? skinny_waves<T, 4, 2>(a, k.waves, s) : skinny_waves<T, 4, 1>(a, k.waves, s);
   }
 #define FF_TILE(I, J, S) \
   if (p.ti == I && p.tj == J && p.slots == S) return tiles<T, I, J, S>(a, p, partial, s);
@@ -657,6 +664,16 @@ LinearPlan linear_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
     if (2.0 + (double)m * (double)n * elem_bytes / rate < least) return {true, 0, 0, 0, 1};
   }
   return best;
+}
+
+SkinnyPlan skinny_plan(int64_t tokens, int64_t n, int64_t m, int elem_bytes) {
+  const int nt = tokens <= 16 ? 1 : tokens <= 32 ? 2 : 4, rw = nt > 1 && m >= 8192 ? 2 : 1;
+  const int64_t groups = (m + 16 * rw - 1) / (16 * rw), steps = (n * elem_bytes + 127) / 128;
+  // enough waves to keep memory busy (8 a compute unit), each with four steps
+  // or more
+  int waves = 4;
+  while (waves < most_waves(nt, rw) && groups * waves < 2048 && steps >= 8 * waves) waves *= 2;
+  return {nt, rw, waves};
 }
 
 size_t linear_partial_bytes(const LinearPlan& p, int64_t tokens, int64_t m) {

@@ -509,10 +509,10 @@ hipError_t step_tiles(StepArgs a, int64_t batch, hipStream_t s) {
 }
 
 template <int PARTS>
-hipError_t sym_step(StepArgs a, const StepPlan& p, float* sums, int64_t batch, hipStream_t s) {
-  a.splits = p.splits;
-  a.sums = p.splits > 1 ? sums : nullptr;
-  switch (p.form) {
+hipError_t sym_step(StepArgs a, int form, int splits, float* sums, int64_t batch, hipStream_t s) {
+  a.splits = splits;
+  a.sums = splits > 1 ? sums : nullptr;
+  switch (form) {
     case 0: return step_tiles<PARTS, 8, 8, 2, true>(a, batch, s);
     case 1: return step_tiles<PARTS, 6, 6, 2, true>(a, batch, s);
     case 2: return step_tiles<PARTS, 4, 4, 2, true>(a, batch, s);
@@ -521,9 +521,9 @@ hipError_t sym_step(StepArgs a, const StepPlan& p, float* sums, int64_t batch, h
   }
 }
 template <int PARTS>
-hipError_t any_step(StepArgs a, const StepPlan& p, int64_t batch, hipStream_t s) {
+hipError_t any_step(StepArgs a, int form, int64_t batch, hipStream_t s) {
   a.splits = 1;
-  switch (p.form) {
+  switch (form) {
     case 0: return step_tiles<PARTS, 8, 8, 2, false>(a, batch, s);
     case 1: return step_tiles<PARTS, 6, 8, 2, false>(a, batch, s);
     case 2: return step_tiles<PARTS, 4, 8, 3, false>(a, batch, s);
@@ -609,7 +609,7 @@ Buffers layout(int64_t batch, int64_t m, int64_t n, int parts, char* base) {
     b.x[k] = operand(r, ldc, 2);
     b.t[k] = operand(c, ldr, parts);
   }
-  const int splits = step_plan(true, true, r, r, (c + 7) / 8 * 8, batch, parts).splits;
+  const int splits = ortho_plan(batch, m, n, parts == 1).gram_splits;
   if (splits > 1) b.sums = (float*)take((size_t)splits * (size_t)(batch * r * ((r + 7) / 8 * 8)) * sizeof(float));
   b.gram = operand(r, ldr, parts);
   b.poly = operand(r, ldr, parts);
@@ -924,10 +924,10 @@ template <int PARTS, class E>
 hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
   const double most = iterates_bound(a.steps, a.a, a.b, a.c);
   const float sx = scale_for(most), sa = scale_for(most * most), sb = scale_for(quad_bound(a.b, a.c, most * most));
-  const int small = small_parts(a.m, a.n, a.bf16);
-  if (small == 2) return run_small<2, E>(a, sx, sa, sb, s);
+  const OrthoPlan plan = ortho_plan(a.batch, a.m, a.n, PARTS == 1);
+  if (plan.small == 2) return run_small<2, E>(a, sx, sa, sb, s);
   if constexpr (PARTS == 1)
-    if (small == 1) return run_small<1, E>(a, sx, sa, sb, s);
+    if (plan.small == 1) return run_small<1, E>(a, sx, sa, sb, s);
   const bool tall = a.m > a.n;
   const int64_t r = std::min(a.m, a.n), c = std::max(a.m, a.n);
   Buffers w = layout(a.batch, a.m, a.n, PARTS, (char*)workspace);
@@ -948,9 +948,6 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
                      tall ? w.t[0] : x_of(0), tall ? x_of(0) : w.t[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t r8 = (r + 7) / 8 * 8, c8 = (c + 7) / 8 * 8;
-  const StepPlan gram = step_plan(true, true, r, r, c8, a.batch, PARTS);
-  const StepPlan square = step_plan(true, false, r, r, r8, a.batch, PARTS);
-  const StepPlan apply = step_plan(false, false, r, c, r8, a.batch, PARTS);
   for (int k = 0; k < a.steps; ++k) {
     const int cur = k & 1, nxt = cur ^ 1;
     StepArgs q{};
@@ -959,13 +956,13 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
     q.L = q.R = w.x[cur];
     q.o = w.gram;
     q.alpha = sa / (sx * sx);
-    if ((e = sym_step<PARTS>(q, gram, w.sums, a.batch, s)) != hipSuccess) return e;
+    if ((e = sym_step<PARTS>(q, plan.gram, plan.gram_splits, w.sums, a.batch, s)) != hipSuccess) return e;
     q.k = r8;
     q.L = q.R = q.D = w.gram;
     q.o = w.poly;
     q.alpha = a.c * sb / (sa * sa);
     q.beta = a.b * sb / sa;
-    if ((e = sym_step<PARTS>(q, square, nullptr, a.batch, s)) != hipSuccess) return e;
+    if ((e = sym_step<PARTS>(q, plan.square, 1, nullptr, a.batch, s)) != hipSuccess) return e;
     q.cols = c;
     q.L = w.poly;
     q.R = w.t[cur];
@@ -983,7 +980,7 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
       q.su = a.so;
       q.bf16 = a.bf16;
     }
-    if ((e = any_step<PARTS>(q, apply, a.batch, s)) != hipSuccess) return e;
+    if ((e = any_step<PARTS>(q, plan.apply, a.batch, s)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -992,15 +989,24 @@ hipError_t run(const OrthoArgs& a, void* workspace, hipStream_t s) {
 
 bool ortho_bounded(int steps, double a, double b, double c) { return iterates_bound(steps, a, b, c) < 16.0; }
 
+OrthoPlan ortho_plan(int64_t batch, int64_t m, int64_t n, bool bf16) {
+  const int small = small_parts(m, n, bf16), parts = bf16 ? 1 : 2;
+  if (small != 0) return {small, 0, 1, 0, 0};
+  const int64_t r = std::min(m, n), c = std::max(m, n), r8 = (r + 7) / 8 * 8, c8 = (c + 7) / 8 * 8;
+  const StepPlan gram = step_plan(true, true, r, r, c8, batch, parts);
+  return {0, gram.form, gram.splits, step_plan(true, false, r, r, r8, batch, parts).form,
+          step_plan(false, false, r, c, r8, batch, parts).form};
+}
+
 size_t ortho_workspace(int64_t batch, int64_t m, int64_t n, bool bf16) {
-  if (small_parts(m, n, bf16) != 0) return 0;
+  if (ortho_plan(batch, m, n, bf16).small != 0) return 0;
   return layout(batch, m, n, bf16 ? 1 : 2, nullptr).bytes;
 }
 
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t s) {
   // 2^20: the operands' rows stay within nt::kMaxRowBytes, the grid within its limits
   if (a.batch <= 0 || a.batch > 65535 || a.m <= 0 || a.n <= 0 || std::max(a.m, a.n) > (1 << 20) || a.steps <= 0 ||
-      (workspace == nullptr && small_parts(a.m, a.n, a.bf16) == 0) || (uintptr_t)workspace % 256 != 0 || !ortho_bounded(a.steps, a.a, a.b, a.c))
+      (workspace == nullptr && ortho_plan(a.batch, a.m, a.n, a.bf16).small == 0) || (uintptr_t)workspace % 256 != 0 || !ortho_bounded(a.steps, a.a, a.b, a.c))
     return hipErrorInvalidValue;
   return a.bf16 ? run<1, bf16_t>(a, workspace, s) : run<2, float>(a, workspace, s);
 }
