@@ -274,102 +274,141 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
 
 // Gradient: as k_norm, with the columns' share of dw summed over the
 // workgroup's rows and left in part[workgroup][column].  Rows that need scaling
-// are left to a second turn over the workgroup's rows, taken only where there is one:
-// in one turn they cost all rows registers (1024 x 32768 bf16: 192 us, 124 so).
+// are left until after up to 63 others: taken at once they cost all rows registers
+// (1024 x 32768 bf16: 188 us, 101 so).
 template <class E, int THR, int VPT>
 __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
   constexpr int N = Vec<E>::N, RPB = block_of(THR) / THR;
   __shared__ float red[32];
   __shared__ float share[RPB > 1 ? RPB * 64 * VPT * N : 1];
-  const int t = threadIdx.x % THR;
+  const int t = threadIdx.x % THR, cols = (int)a.cols;
   float dw[VPT][N];
   Vec<E> vw[VPT];
 #pragma unroll
   for (int k = 0; k < VPT; ++k) {
-    const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
+    const int j = (k * THR + t) * N, left = cols - j;
     if (a.weight != nullptr && left > 0) vw[k] = load_row((const E*)a.weight + j, left);
 #pragma unroll
     for (int i = 0; i < N; ++i) dw[k][i] = 0.0f;
   }
   auto w = [&](int k, int i) { return a.weight != nullptr ? vw[k].get(i) : 1.0f; };
-  // RARE: the rows that the other turn left; returns whether it left any (the
-  // same for every thread of a row, and of a workgroup of one row at a time)
-  auto turn = [&](auto rare) {
-    constexpr bool RARE = decltype(rare)::value;
-    bool left_over = false;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / THR; row < a.rows;
-         row += (int64_t)gridDim.x * RPB) {
-      Vec<E> vs[VPT], vd[VPT], vt[VPT];
+  // One row; false, and nothing done, where it has to be scaled (the same for every
+  // thread of a row)
+  auto plain_row = [&](int64_t row) {
+    Vec<E> vs[VPT], vd[VPT], vt[VPT];
 #pragma unroll
-      for (int k = 0; k < VPT; ++k) {
-        const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
-        if (left > 0) {
-          vs[k] = load_row((const E*)a.s + row * a.lds + j, left);
-          vd[k] = load_row((const E*)a.dy + row * a.lddy + j, left);
-          if (a.dsum != nullptr) vt[k] = load_row((const E*)a.dsum + row * a.lddsum + j, left);
-        } else {
-          vs[k].w = vd[k].w = vt[k].w = u32x4{0, 0, 0, 0};
-        }
-      }
-      float us;
-      auto sums = [&](float eps) {  // us of what vs holds; returns mean s^2 + eps
-        float ss = 0.0f;
-        us = 0.0f;
-#pragma unroll
-        for (int k = 0; k < VPT; ++k)
-          if (a.cols - (int64_t)(k * THR + t) * N > 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              const float s = vs[k].get(i);
-              ss += s * s;
-              us += vd[k].get(i) * w(k, i) * s;
-            }
-          }
-        ss = row_reduce<THR>(ss, red, Add());
-        us = row_reduce<THR>(us, red + 16, Add());
-        return ss / (float)a.cols + eps;
-      };
-      float m = sums(a.eps.plain), f = 1.0f;
-      if (__builtin_expect(in_range(m) == RARE, 0)) {
-        left_over = true;
-        continue;
-      }
-      if (RARE) {
-        f = m < 1.0f ? kUp : kDown;
-        const float eps = m < 1.0f ? a.eps.up : a.eps.down;
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {  // (what this takes below the type's range does not matter beside the rest)
-          float s[N];
-#pragma unroll
-          for (int i = 0; i < N; ++i) s[i] = vs[k].get(i) * f;
-          vs[k].set(s);
-        }
-        m = sums(eps);
-      }
-      const float i1 = 1.0f / sqrtf(m);
-      const float proj = us / (float)a.cols * i1 * i1;
-#pragma unroll
-      for (int k = 0; k < VPT; ++k) {
-        const int64_t j = (int64_t)(k * THR + t) * N, left = a.cols - j;
-        if (left > 0) {
-          float g[N];
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float s = vs[k].get(i), d = vd[k].get(i);
-            dw[k][i] += d * s * i1;
-            g[i] = i1 * (d * w(k, i) - s * proj);
-            if (RARE) g[i] *= f;
-            if (a.dsum != nullptr) g[i] += vt[k].get(i);
-          }
-          Vec<E> o;
-          o.set(g);
-          store_row((E*)a.dx + row * a.lddx + j, o, left);
-        }
+    for (int k = 0; k < VPT; ++k) {
+      const int j = (k * THR + t) * N, left = cols - j;
+      if (left > 0) {
+        vs[k] = load_row((const E*)a.s + row * a.lds + (uint32_t)j, left);
+        vd[k] = load_row((const E*)a.dy + row * a.lddy + (uint32_t)j, left);
+        if (a.dsum != nullptr) vt[k] = load_row((const E*)a.dsum + row * a.lddsum + (uint32_t)j, left);
+      } else {
+        vs[k].w = vd[k].w = vt[k].w = u32x4{0, 0, 0, 0};
       }
     }
-    return left_over;
+    float ss = 0.0f, us = 0.0f;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+      if (cols - (k * THR + t) * N > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = vs[k].get(i);
+          ss += s * s;
+          us += vd[k].get(i) * w(k, i) * s;
+        }
+      }
+    ss = row_reduce<THR>(ss, red, Add());
+    us = row_reduce<THR>(us, red + 16, Add());
+    const float m = ss / (float)a.cols + a.eps.plain;
+    if (__builtin_expect(!in_range(m), 0)) return false;
+    const float i1 = 1.0f / sqrtf(m);
+    const float proj = us / (float)a.cols * i1 * i1;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int j = (k * THR + t) * N, left = cols - j;
+      if (left > 0) {
+        float g[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = vs[k].get(i), d = vd[k].get(i);
+          dw[k][i] += d * s * i1;
+          g[i] = i1 * (d * w(k, i) - s * proj);
+          if (a.dsum != nullptr) g[i] += vt[k].get(i);
+        }
+        Vec<E> o;
+        o.set(g);
+        store_row((E*)a.dx + row * a.lddx + (uint32_t)j, o, left);
+      }
+    }
+    return true;
   };
-  if (__builtin_expect(turn(std::false_type()), 0)) turn(std::true_type());
+  // One that has to be scaled: read again for each pass, a vector at a time
+  auto scaled_row = [&](int64_t row) {
+    const E* const s_row = (const E*)a.s + row * a.lds;
+    const E* const d_row = (const E*)a.dy + row * a.lddy;
+    float f = 1.0f, us = 0.0f, m = 0.0f;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+      float ss = 0.0f;
+      us = 0.0f;
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int j = (k * THR + t) * N, left = cols - j;
+        if (left > 0) {
+          const Vec<E> vs = load_row(s_row + (uint32_t)j, left), vd = load_row(d_row + (uint32_t)j, left);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float s = vs.get(i) * f;
+            ss += s * s;
+            us += vd.get(i) * w(k, i) * s;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (the next vector's loads stay behind)
+      }
+      ss = row_reduce<THR>(ss, red, Add());
+      us = row_reduce<THR>(us, red + 16, Add());
+      m = ss / (float)a.cols + (f == 1.0f ? a.eps.plain : f == kUp ? a.eps.up : a.eps.down);
+      if (pass == 0) f = m < 1.0f ? kUp : kDown;
+    }
+    const float i1 = 1.0f / sqrtf(m);
+    const float proj = us / (float)a.cols * i1 * i1;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int j = (k * THR + t) * N, left = cols - j;
+      if (left > 0) {
+        const Vec<E> vs = load_row(s_row + (uint32_t)j, left), vd = load_row(d_row + (uint32_t)j, left);
+        float g[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = vs.get(i) * f, d = vd.get(i);
+          dw[k][i] += d * s * i1;
+          g[i] = i1 * (d * w(k, i) - s * proj) * f;
+        }
+        if (a.dsum != nullptr) {
+          const Vec<E> vt = load_row((const E*)a.dsum + row * a.lddsum + (uint32_t)j, left);
+#pragma unroll
+          for (int i = 0; i < N; ++i) g[i] += vt.get(i);
+        }
+        Vec<E> o;
+        o.set(g);
+        store_row((E*)a.dx + row * a.lddx + (uint32_t)j, o, left);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  const int wave = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;  // whose row it is
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB + wave; row0 < a.rows; row0 += 64 * step) {
+    uint64_t later = 0;  // (dx may be s itself: a row that is done is not looked at again)
+    int64_t row = row0;
+    for (int i = 0; i < 64 && row < a.rows; ++i, row += step)
+      if (!plain_row(row)) later |= uint64_t(1) << i;
+    while (__builtin_expect(later != 0, 0)) {
+      scaled_row(row0 + __builtin_ctzll(later) * step);
+      later &= later - 1;
+    }
+  }
   if (a.part == nullptr) return;
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
   if (RPB > 1) {

@@ -1,4 +1,5 @@
 """The layer operators at the ends of what they take."""
+import ctypes
 import types
 
 import pytest
@@ -151,3 +152,26 @@ def test_what_is_no_tensor(gpu):
                      lambda: ffe.linear_backward(dy, x, W, preact=bad, activation="silu"), lambda: ffe.orthogonalize(bad)):
             with pytest.raises(TypeError, match="CUDA tensor"):
                 call()
+
+
+@pytest.mark.parametrize("into", ["s", "dy", "dsum"])
+@pytest.mark.parametrize("rows,n", [(1100, 40), (1100, 700), (5000, 1500), (600, 3000), (600, 40000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradient_in_place(gpu, rows, n, dtype, into):
+    """ds in the place of an input, rows that have to be scaled among rows whose
+    gradients are as small or as large as those."""
+    g = torch.Generator(gpu).manual_seed(n)
+    sizes = torch.tensor([1.0, 1e25, 1e-25, 0.0], device=gpu)[torch.randint(0, 4, (rows, 1), device=gpu, generator=g)]
+    x = (torch.randn(rows, n, device=gpu, generator=g) * sizes).to(DT[dtype])
+    small = torch.tensor([1e-24, 1.0], device=gpu)[torch.randint(0, 2, (rows, 1), device=gpu, generator=g)]
+    dy, dsum = ((torch.randn(rows, n, device=gpu, generator=g) * small).to(DT[dtype]) for _ in range(2))
+    w = torch.ones(n, dtype=DT[dtype], device=gpu)
+    want, want_dw = ffe.rms_norm_backward(dy, x, w, eps=1e-60, dsum=dsum)
+    t = {"s": x.clone(), "dy": dy.clone(), "dsum": dsum.clone()}
+    dw = torch.empty_like(w)
+    ws = torch.empty(512 * n, dtype=torch.float32, device=gpu)
+    a = ffe.ff_norm_grad_args(rows, n, int(dtype == "bf16"), t["s"].data_ptr(), n, t["dy"].data_ptr(), n, t["dsum"].data_ptr(), n,
+                              w.data_ptr(), 1e-60, t[into].data_ptr(), n, dw.data_ptr(), ws.data_ptr(), ws.numel() * 4,
+                              torch.cuda.current_stream(gpu).cuda_stream)
+    assert ffe.load_library().ff_rms_norm_backward(ctypes.byref(a)) == ffe.FF_OK
+    assert torch.equal(t[into].nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(dw.nan_to_num(7.0), want_dw.nan_to_num(7.0))
