@@ -177,7 +177,7 @@ struct Piece {
 // the fewest operand bytes per product (1.36 us a pair, 2.0 POP/s in 8 bits for
 // 4096 x 4096 -> 11008: 180 us, of which the last, partly filled round of 688
 // tiles on 256 units costs a tenth); smaller ones fill the units where those
-// are few (1021 x 1000 -> 777 bf16: 12 to 13.5 us, 9 of it a kernel's start and end).
+// are few (1021 x 1000 -> 777 bf16: 12.7 to 13.5 us, about 4 of them in the loop).
 template <class T, int TI, int TJ, int SLOTS>
 __global__ __launch_bounds__(nt::kThreads, ((TI + TJ) * SLOTS <= 20 ? 2 : 1)) void k_tile(
     LinearArgs a, uint32_t mt, uint32_t ntl, uint32_t splits, typename Scalar<T>::type* P) {
@@ -394,7 +394,7 @@ __device__ __forceinline__ u32x4 row_bytes(const char* row, int k, int bytes) {
 // matter as long as both operands agree.  Accumulator element r of lane l:
 // output row 4 (l / 16) + r, token l % 16.  Bound by reading w and, as a call is
 // short, by the latency of its first bytes: one token, 4096 -> 11008 in 8 bits,
-// 45 MB, in 10.6 to 13.7 us (3.3 to 4.3 TB/s).
+// 45 MB, in 12.8 to 14.3 us (3.2 to 3.5 TB/s).
 template <class T, int NT, int RW, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_skinny(LinearArgs a) {
   typedef typename Scalar<T>::type S;

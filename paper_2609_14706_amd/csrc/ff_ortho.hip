@@ -451,7 +451,8 @@ __global__ __launch_bounds__(256) void k_step_join(StepArgs a, int edge) {
 
 // The fastest form of a product by a model of the forms' times (us), as for the
 // linear layers: per pair of k `pair` with a compute unit to itself, `loaded`
-// with all of them busy, `ends` for a tile's start and epilogue.
+// with all of them busy, `ends` for a tile's start and epilogue.  (Predicts too little
+// where tiles store both ways: symmetric 4096 with k = 11008 154 us for 192 measured.)
 struct StepForm {
   int ti, tj, slots, wgs;
   double pair, loaded, ends;

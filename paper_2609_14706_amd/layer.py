@@ -370,8 +370,9 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
                     need_weight: bool = True, need_bias: bool = True, workspace=None, stream=None):
     """(dx, dw, g, db) of y = act(z) + residual for the gradient dy of y (which
     is the residual's own): g = dy act'(z) (dy itself without an activation),
-    dx = g weight, dw = g^T x, db = sum of g; None for what is not needed.  The
-    rows of x and of g are the tokens of FlipFlop(tokens=(x, g))."""
+    dx = g weight, dw = g^T x, db = sum of g, all of g rounded as it is returned;
+    None for what is not needed.  The rows of x and of g are the tokens of
+    FlipFlop(tokens=(x, g))."""
     if stream is not None:
         return _on_stream(stream, linear_backward, dy, x, weight, preact=preact, activation=activation,
                           need_input=need_input, need_weight=need_weight, need_bias=need_bias, workspace=workspace)
