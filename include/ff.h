@@ -417,6 +417,7 @@ ff_status ff_rms_norm(const ff_norm_args* args);
  *     ds = d(loss)/ds through y, plus dsum (the gradient that reaches s by other ways);
  *          it is the gradient of x and of the residual alike
  *     dweight_j = sum over the rows of dy_j s_j / sqrt(mean s^2 + eps).
+ * (Rows and eps as above; the sums of dy_j weight_j s_j have to fit fp32.)
  * ds may be dy, s or dsum themselves (the same rows and ld). */
 typedef struct {
   int64_t rows, cols;       /* cols <= 2^24 */

@@ -12,7 +12,7 @@
 // long for registers (above 32768 bf16, 16384 fp32) are read again for each
 // pass (k_norm_long, k_norm_grad_long).  8192 x 8192 bf16 with residual to 8
 // bits: 99 us, 4.7 TB/s where a large copy reaches 5.1; gradient of 8191 x 4096:
-// 55 us (4.9 TB/s) and 5 us for the sums of dw.
+// 53 us (5.1 TB/s) and 5 us for the sums of dw.
 // All sums are fp32, in an order fixed by the sizes.  A row whose squares leave
 // fp32's range (mean s^2 + eps not in 2^-100 .. 2^128) is summed again with s and
 // eps scaled by a power of two.
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
 // Gradient: as k_norm, with the columns' share of dw summed over the
 // workgroup's rows and left in part[workgroup][column].  Rows that need scaling
 // are left until after up to 63 others: taken at once they cost all rows registers
-// (1024 x 32768 bf16: 188 us, 101 so).
+// (1024 x 32768 bf16: 188 us, 100 so).
 template <class E, int THR, int VPT>
 __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
   constexpr int N = Vec<E>::N, RPB = block_of(THR) / THR;
@@ -303,8 +303,6 @@ __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
         vs[k] = load_row((const E*)a.s + row * a.lds + (uint32_t)j, left);
         vd[k] = load_row((const E*)a.dy + row * a.lddy + (uint32_t)j, left);
         if (a.dsum != nullptr) vt[k] = load_row((const E*)a.dsum + row * a.lddsum + (uint32_t)j, left);
-      } else {
-        vs[k].w = vd[k].w = vt[k].w = u32x4{0, 0, 0, 0};
       }
     }
     float ss = 0.0f, us = 0.0f;
@@ -320,6 +318,9 @@ __global__ __launch_bounds__(block_of(THR)) void k_norm_grad(NormGradArgs a) {
       }
     ss = row_reduce<THR>(ss, red, Add());
     us = row_reduce<THR>(us, red + 16, Add());
+    // (dsum's loads have landed by now; said here, or the compiler waits at the next row's
+    // start for whatever is on its way, this one's stores too: 4096 x 8192 53 us, 49 so)
+    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0)
     const float m = ss / (float)a.cols + a.eps.plain;
     if (__builtin_expect(!in_range(m), 0)) return false;
     const float i1 = 1.0f / sqrtf(m);

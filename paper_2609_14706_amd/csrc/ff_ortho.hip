@@ -139,7 +139,8 @@ __global__ __launch_bounds__(256) void k_start(const E* g, int64_t ldg, int64_t 
 // `splits` parts, as partial sums (sums: splits x batch x rows x c8 fp32).
 // Large ones are bound by the matrix cores (the product with X of a 4096 x 11008
 // bf16 update: 317 us for the last step, 1.16 PFLOP/s, 688 tiles of 256 x 256 making
-// 2.7 rounds; 371 to 394 for the others, X's second part read and written), small ones by a kernel's start, first reads and stores (5 to 7 us).
+// 2.7 rounds; 371 to 394 for the others, X's second part read and written), small
+// ones by a kernel's start, first reads and stores (5 to 7 us).
 // 3 x 1500 x 1000 fp32, three fp16 products: 26 to 33 us for a symmetric one
 // (tiles of 64 x 64: 408), 49 to 56 for the one with X, whose D and
 // results in parts and both ways are 54 MB, 11 us at a copy's rate.
