@@ -516,6 +516,41 @@ ff_status ff_linear_backward_workspace_size(const ff_linear_grad_args* args, siz
  * and db are set to zeros. */
 ff_status ff_linear_backward(const ff_linear_grad_args* args);
 
+/* 8-bit checkpoints of activations: rows x cols in groups of columns with a scale each,
+ *     scale = max |x| / 127 over the group,  q = rint(127 x / max |x|),  back: x' = q scale
+ * (x' is off by at most half a scale).  A group that is not finite gets a NaN scale and
+ * zero codes, one whose largest magnitude is below 2^-118 a zero scale and zero codes.
+ * A group is 16, 32, 64, 128, 256 or 512 columns; a row's last one may be shorter. */
+typedef struct {
+  int8_t* q;                /* rows x cols */
+  int64_t ldq;
+  float* scale;             /* rows x ceil(cols / group) */
+  int64_t ld_scale;
+  int64_t group;
+} ff_q8_rows;
+typedef struct {
+  int64_t rows, cols;       /* rows <= 2^32, cols <= 2^24 */
+  ff_dtype dtype;           /* x */
+  void* x;                  /* ff_checkpoint reads it, ff_checkpoint_restore writes x' */
+  int64_t ldx;
+  ff_q8_rows kept;          /* written by ff_checkpoint, read by ff_checkpoint_restore */
+  void* stream;
+} ff_checkpoint_args;
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_HIP. */
+ff_status ff_checkpoint(const ff_checkpoint_args* args);
+ff_status ff_checkpoint_restore(const ff_checkpoint_args* args);
+
+/* ff_linear_backward from checkpoints: x_q8 (q not NULL) stands for x, whose values are
+ * rounded to bf16 for the product, preact_q8 for preact (not rounded); the other one may
+ * be bf16 as before.  The workspace is ff_linear_backward_workspace_size(&args->grad).
+ * Errors: as ff_linear_backward. */
+typedef struct {
+  ff_linear_grad_args grad; /* x, preact: NULL where a checkpoint is given */
+  ff_q8_rows x_q8;          /* tokens x n */
+  ff_q8_rows preact_q8;     /* tokens x m */
+} ff_linear_grad_q8_args;
+ff_status ff_linear_backward_q8(const ff_linear_grad_q8_args* args);
+
 /* Orthogonalisation of updates G (m x n) by `steps` Newton-Schulz products:
  *     X = G / (||G||_F + eps);  A = X X^T, X <- a X + (b A + c A A) X;  out = scale X
  * (the smaller of X X^T and X^T X, the same X).  Sums are fp32.  FF_F32:

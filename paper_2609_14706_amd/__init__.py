@@ -23,8 +23,9 @@ from .binding import (FF_APPLY, FF_APPLY_INV, FF_BF16, FF_ERR_HIP, FF_ERR_INVALI
 
 # The layer operators are torch functions: imported with the first use of one,
 # so that the rest of the package does not need torch to be imported.
-_LAYER = ("ACTIVATIONS", "ff_linear_args", "ff_linear_grad_args", "ff_norm_args", "ff_norm_grad_args",
-          "ff_ortho_args", "linear", "linear_backward", "linear_q8", "orthogonalize", "quantize_rows",
+_LAYER = ("ACTIVATIONS", "Checkpoint", "checkpoint_q8", "checkpoint_restore", "ff_checkpoint_args",
+          "ff_linear_args", "ff_linear_grad_args", "ff_linear_grad_q8_args", "ff_norm_args", "ff_norm_grad_args",
+          "ff_ortho_args", "ff_q8_rows", "linear", "linear_backward", "linear_q8", "orthogonalize", "quantize_rows",
           "rms_norm", "rms_norm_backward", "rms_norm_q8")
 
 

@@ -57,6 +57,29 @@ hipError_t launch_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t s);
 // out[j] (bf16 or fp32) = sum over the rows of part (rows x cols).
 hipError_t launch_col_sums(const float* part, int64_t rows, int64_t cols, void* out, bool bf16, hipStream_t s);
 
+// -------------------------------------------------- 8-bit activation checkpoints
+// Rows of codes, a scale for every 2^shift columns: value = q scale.
+constexpr int kMinGroupShift = 4, kMaxGroupShift = 9;
+struct Q8Rows {
+  const int8_t* q;  // null: none
+  int64_t ldq;
+  const float* scale;  // rows x ceil(cols / 2^shift)
+  int64_t lds;
+  int shift;
+};
+struct CheckpointArgs {
+  int64_t rows, cols;
+  void* x;  // read (launch_checkpoint) or written (launch_restore)
+  int64_t ldx;
+  int8_t* q;
+  int64_t ldq;
+  float* scale;
+  int64_t lds;
+  int shift;
+};
+hipError_t launch_checkpoint(const CheckpointArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_restore(const CheckpointArgs& a, bool bf16, hipStream_t s);
+
 // ------------------------------------------------------------------- linear
 enum Act : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 
@@ -112,12 +135,16 @@ hipError_t launch_zero(void* dst, int64_t ld, int64_t rows, int64_t cols, int el
 // ldgt, zeros beyond rows; null: not stored) and, with part, column sums of
 // every 64 rows (act_grad_parts(rows) x cols).  z null: g = dy, so that with
 // gt alone a job is a transposition.  One to three jobs in one launch.
+// Checkpoints in 8 bits stand for dy (dyq: its values rounded to bf16) or z (zq: not
+// rounded) where they are given.
 struct ActGradArgs {
   int64_t rows, cols;
   const bf16_t* dy;
   int64_t lddy;
+  Q8Rows dyq;
   const bf16_t* z;
   int64_t ldz;
+  Q8Rows zq;
   bf16_t* g;
   int64_t ldg;
   bf16_t* gt;

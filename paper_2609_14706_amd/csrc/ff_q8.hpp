@@ -1,0 +1,33 @@
+// Reading 8-bit activation checkpoints: codes with a scale for each group of
+// 16 to 512 columns.
+#pragma once
+
+#include "ff_layer_kernels.hpp"
+#include "ff_vec.hpp"
+
+namespace ff {
+
+// Eight codes from column `col` on (a multiple of eight: one group's), `count` of
+// them in the row, zeros after them.
+__device__ __forceinline__ void load_codes(const int8_t* p, int count, uint32_t (&w)[2]) {
+  if (count >= 8) {
+    __builtin_memcpy(w, p, 8);
+  } else {
+    w[0] = w[1] = 0;
+#pragma unroll
+    for (int k = 0; k < 7; ++k)
+      if (k < count) w[k / 4] |= (uint32_t)(uint8_t)p[k] << (8 * (k % 4));
+  }
+}
+// Their values, not rounded: a code is exact in fp32, its product rounded once.
+__device__ __forceinline__ void values_of(const uint32_t (&w)[2], float scale, float (&f)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4))) * scale;
+}
+__device__ __forceinline__ void load_q8(const Q8Rows& a, int64_t row, int64_t col, int count, float (&f)[8]) {
+  uint32_t w[2];
+  load_codes(a.q + row * a.ldq + col, count, w);
+  values_of(w, a.scale[row * a.lds + (col >> a.shift)], f);
+}
+
+}  // namespace ff

@@ -12,6 +12,7 @@ Workspaces are taken from torch unless `workspace` (a uint8 tensor) is given.
 from __future__ import annotations
 
 import ctypes
+from typing import NamedTuple
 
 import torch
 
@@ -153,13 +154,22 @@ def _elem(t, name):
     return _ELEM[t.dtype]
 
 
+def _flat(values):
+    """The values, with those of tuples (checkpoints, routings) in their place."""
+    for v in values:
+        if isinstance(v, tuple):
+            yield from _flat(v)
+        else:
+            yield v
+
+
 def _on_stream(stream, fn, *args, **kw):
     """fn on `stream`: its allocations and the inputs' lives are ordered there,
     the results' also on the caller's stream, which is to use them."""
     device = getattr(stream, "device", None)
     if device is None:
         raise TypeError("stream must be a torch.cuda.Stream")
-    inputs = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor) and t.is_cuda]
+    inputs = [t for t in _flat((*args, *kw.values())) if isinstance(t, torch.Tensor) and t.is_cuda]
     for t in inputs:
         if t.device != device:
             raise ValueError(f"stream is of {device}, the tensors are on {t.device}")
@@ -168,8 +178,8 @@ def _on_stream(stream, fn, *args, **kw):
     for t in inputs:
         t.record_stream(stream)
     caller = torch.cuda.current_stream(device)
-    for t in out if isinstance(out, tuple) else (out,):
-        if t is not None:
+    for t in _flat((out,)):
+        if isinstance(t, torch.Tensor):
             t.record_stream(caller)
     return out
 
@@ -191,22 +201,22 @@ def _workspace(args, nbytes, workspace, device):
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _launch(name, args, device):
+def _launch(name, args, device, functions=_FN):
     """Call the library on the device's current stream."""
     index = device.index
     args.stream = _raw_stream(index)
     if _current_device() == index:
-        code = _FN[name](args)
+        code = functions[name](args)
     else:
         with torch.cuda.device(index):
-            code = _FN[name](args)
+            code = functions[name](args)
     if code:
         _check(code)
 
 
-def _bytes(name, args, *more):
+def _bytes(name, args, *more, functions=_FN):
     out = _size(0)
-    code = _FN[name](args, *more, out)
+    code = functions[name](args, *more, out)
     if code:
         _check(code)
     return out.value
@@ -372,14 +382,22 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     is the residual's own): g = dy act'(z) (dy itself without an activation),
     dx = g weight, dw = g^T x, db = sum of g, all of g rounded as it is returned;
     None for what is not needed.  The rows of x and of g are the tokens of
-    FlipFlop(tokens=(x, g))."""
+    FlipFlop(tokens=(x, g)).  x and preact may be checkpoints in 8 bits
+    (checkpoint_q8): x's values are then rounded to bfloat16 for dw."""
     if stream is not None:
         return _on_stream(stream, linear_backward, dy, x, weight, preact=preact, activation=activation,
                           need_input=need_input, need_weight=need_weight, need_bias=need_bias, workspace=workspace)
     _library()
-    dev = _first(x, "x")
     bf16 = torch.bfloat16
-    px, ldx, T, n = _rows(x, "x", bf16, dev)
+    x8 = z8 = None
+    if isinstance(x, Checkpoint):
+        dev = _first(x.codes, "x.codes")
+        x8, x = x, x.codes   # (its shape from here on)
+        k8, T, n = _q8_rows(x8, "x", dev)
+        px, ldx = None, 0
+    else:
+        dev = _first(x, "x")
+        px, ldx, T, n = _rows(x, "x", bf16, dev)
     pw, ldw, m, _ = _rows(weight, "weight", bf16, dev, n)
     if weight.dim() != 2:
         raise ValueError("weight must be a 2-D tensor (m, n)")
@@ -393,14 +411,18 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     if a.activation:
         if preact is None:
             raise ValueError(f"preact of shape {tuple(shape)} is needed with an activation")
-        a.preact, a.ldz, _, _ = _rows(preact, "preact", bf16, dev, m)
+        if isinstance(preact, Checkpoint):
+            z8, preact = preact, preact.codes
+            kz8, _, _ = _q8_rows(z8, "preact", dev, m)
+        else:
+            a.preact, a.ldz, _, _ = _rows(preact, "preact", bf16, dev, m)
         if preact.shape != shape:
             raise ValueError(f"preact must have the output's shape {tuple(shape)}")
         g = _like(dy, bf16)
         a.g, a.ldg = g.data_ptr(), m
     dx = dw = db = None
     if need_input:
-        dx = _like(x, bf16)
+        dx = _like(x, bf16)   # (also of a checkpoint's codes)
         a.dx, a.lddx = dx.data_ptr(), n
     if need_weight:
         dw = _like(weight, bf16)
@@ -409,9 +431,113 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
         db = torch.empty(m, dtype=bf16, device=dev)
         a.db = db.data_ptr()
     keep = _workspace(a, _bytes("ff_linear_backward_workspace_size", a), workspace, dev)
-    _launch("ff_linear_backward", a, dev)
+    if x8 is None and z8 is None:
+        _launch("ff_linear_backward", a, dev)
+    else:
+        _q8_library()
+        _launch("ff_linear_backward_q8", ff_linear_grad_q8_args(a, k8 if x8 else ff_q8_rows(), kz8 if z8 else ff_q8_rows()),
+                dev, _Q8_FN)
     del keep
     return dx, dw, g, db
+
+
+# ------------------------------------------------------ checkpoints in 8 bits
+class Checkpoint(NamedTuple):
+    """Activations kept in 8 bits: codes (..., n) int8 and scale (..., ceil(n /
+    group)) float32, the value of column j codes_j scale_{j // group}."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    group: int
+
+
+class ff_q8_rows(ctypes.Structure):
+    _fields_ = [("q", _ptr), ("ldq", _i64), ("scale", _ptr), ("ld_scale", _i64), ("group", _i64)]
+
+
+class ff_checkpoint_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("dtype", _int), ("x", _ptr), ("ldx", _i64), ("kept", ff_q8_rows),
+                ("stream", _ptr)]
+
+
+class ff_linear_grad_q8_args(ctypes.Structure):
+    _fields_ = [("grad", ff_linear_grad_args), ("x_q8", ff_q8_rows), ("preact_q8", ff_q8_rows)]
+
+    @property
+    def stream(self):
+        return self.grad.stream
+
+    @stream.setter
+    def stream(self, value):
+        self.grad.stream = value
+
+
+_Q8_FN = {}
+
+
+def _q8_library():
+    if not _Q8_FN:
+        lib, found = load_library(), {}
+        for name, args in {"ff_checkpoint": ff_checkpoint_args, "ff_checkpoint_restore": ff_checkpoint_args,
+                           "ff_linear_backward_q8": ff_linear_grad_q8_args}.items():
+            f = getattr(lib, name)
+            f.restype, f.argtypes = _int, [ctypes.POINTER(args)]
+            found[name] = f
+        _Q8_FN.update(found)
+    return _Q8_FN
+
+
+def _group(group):
+    if not isinstance(group, int) or group not in (16, 32, 64, 128, 256, 512):
+        raise ValueError(f"group must be 16, 32, 64, 128, 256 or 512, not {group!r}")
+    return group
+
+
+def _q8_rows(kept, name, device, cols=None):
+    """(ff_q8_rows, rows, columns) of a checkpoint."""
+    group = _group(kept.group)
+    pq, ldq, r, c = _rows(kept.codes, f"{name}.codes", torch.int8, device, cols)
+    ps, lds, rs, _ = _rows(kept.scale, f"{name}.scale", torch.float32, device, (c + group - 1) // group)
+    if kept.scale.shape[:-1] != kept.codes.shape[:-1]:
+        raise ValueError(f"{name}.scale must have a row for each row of the codes, {r}, not {rs}")
+    return ff_q8_rows(pq, ldq, ps, lds, group), r, c
+
+
+def checkpoint_q8(x, *, group: int = 128, stream=None):
+    """Checkpoint of x (..., n), float32 or bfloat16, in 8 bits: for each `group`
+    columns scale = max |x| / 127 and codes = rint(127 x / max |x|), so that
+    codes scale is off by at most half a scale.  linear_backward and
+    expert_linear_backward take it for x or preact; checkpoint_restore gives
+    rows for anything else."""
+    if stream is not None:
+        return _on_stream(stream, checkpoint_q8, x, group=group)
+    _q8_library()
+    dev = _first(x, "x")
+    dt = _elem(x, "x")
+    px, ldx, r, c = _rows(x, "x", x.dtype, dev)
+    groups = (c + _group(group) - 1) // group
+    q = _like(x, torch.int8)
+    scale = torch.empty(x.shape[:-1] + (groups,), dtype=torch.float32, device=dev)
+    if r:
+        _launch("ff_checkpoint", ff_checkpoint_args(r, c, dt, px, ldx, ff_q8_rows(q.data_ptr(), c, scale.data_ptr(),
+                                                                                   groups, group)), dev, _Q8_FN)
+    return Checkpoint(q, scale, group)
+
+
+def checkpoint_restore(kept, *, dtype=torch.bfloat16, stream=None):
+    """The rows (..., n) that a checkpoint stands for, float32 or bfloat16."""
+    if stream is not None:
+        return _on_stream(stream, checkpoint_restore, kept, dtype=dtype)
+    _q8_library()
+    if not isinstance(kept, Checkpoint):
+        raise TypeError("kept must be a Checkpoint")
+    if dtype not in _ELEM:
+        raise TypeError(f"dtype must be float32 or bfloat16, not {dtype}")
+    dev = _first(kept.codes, "kept.codes")
+    k, r, c = _q8_rows(kept, "kept", dev)
+    x = _like(kept.codes, dtype)
+    if r:
+        _launch("ff_checkpoint_restore", ff_checkpoint_args(r, c, _ELEM[dtype], x.data_ptr(), c, k), dev, _Q8_FN)
+    return x
 
 
 # ---------------------------------------------------------- orthogonalisation

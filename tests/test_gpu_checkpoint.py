@@ -1,0 +1,225 @@
+"""checkpoint_q8, checkpoint_restore and linear_backward from checkpoints,
+against the formulas in 64 bits.
+
+Tolerances: a scale is one fp32 division (2^-24); codes hang on which side of a
+half 127 x / max lies, which the kernel settles in 64 bits: they are equal.  A
+restored value is one fp32 product (2^-24) and its rounding to the output's
+type.  In the gradient x' = codes scale is rounded to bf16 (2^-8 of each term),
+g as it is returned, and each result once more."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_14706_amd as ffe
+
+pytestmark = pytest.mark.gpu
+
+HALF = 2.0 ** -8
+BF16 = torch.bfloat16
+GROUPS = [16, 32, 64, 128, 256, 512]
+
+
+def _rows(gpu, T, n, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    loud = torch.exp(torch.randn(n, generator=g))
+    return (torch.randn((T, n), generator=g) * loud).to(dtype).to(gpu)
+
+
+def _want(x, group):
+    """codes, scales (fp64) of the definition; groups that are not finite or too small have zero codes."""
+    T, n = x.shape
+    cols = -(-n // group)
+    f = torch.nn.functional.pad(x.double(), (0, cols * group - n)).view(T, cols, group)
+    big = f.abs().amax(dim=2, keepdim=True)
+    ok = torch.isfinite(big) & (big >= 2.0 ** -118)
+    q = torch.where(ok, torch.round(127 * f / torch.where(ok, big, 1)), torch.zeros_like(f))
+    scale = torch.where(ok, big / 127, torch.where(torch.isfinite(big), 0.0, math.nan))
+    return q.view(T, -1)[:, :n].to(torch.int8), scale[:, :, 0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("T,n", [(1, 1), (1, 16), (3, 15), (2, 17), (5, 511), (7, 513), (1, 4096), (33, 1001), (300, 640),
+                                 (2000, 72), (129, 8200)])
+def test_checkpoint(gpu, T, n, dtype):
+    x = _rows(gpu, T, n, dtype, seed=T + n)
+    for group in GROUPS:
+        kept = ffe.checkpoint_q8(x, group=group)
+        q, scale = _want(x, group)
+        assert kept.group == group and torch.equal(kept.codes, q)
+        assert bool(((kept.scale.double() - scale).abs() <= 2.0 ** -24 * scale).all())
+        for out in (BF16, torch.float32):
+            back = ffe.checkpoint_restore(kept, dtype=out)
+            want = kept.codes.double() * torch.repeat_interleave(kept.scale.double(), group, dim=1)[:, :n]
+            half = HALF if out is BF16 else 2.0 ** -24
+            assert back.dtype is out and bool(((back.double() - want).abs() <= (half + 2.0 ** -23) * want.abs()).all())
+        # half a scale from x: scale's rounding 127 2^-24, the value's 2^-24 more
+        back = ffe.checkpoint_restore(kept, dtype=torch.float32)
+        s = torch.repeat_interleave(scale, group, dim=1)[:, :n]
+        assert bool(((back.double() - x.double()).abs() <= s * (0.5 + 255 * 2.0 ** -24)).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+def test_halves_and_special_groups(gpu, dtype):
+    n, group = 96, 16
+    x = _rows(gpu, 6, n, dtype, seed=3)
+    # halves of the largest are 63.5: the even code; so are odd 254ths of 254
+    x[0, 0:16] = torch.tensor([3.0, 1.5, -1.5, 0.75] * 4)
+    x[0, 16:32] = torch.tensor([254.0] + [2.0 * j + 1 for j in range(15)])
+    x[1, 3], x[1, 20], x[1, 40] = math.nan, math.inf, -math.inf
+    x[2, 0:16] = 0
+    x[3, 0:16] *= 0
+    x[3, 5] = 2.0 ** -119
+    x[4, 0:16] = 0
+    x[4, 7] = 2.0 ** -118
+    x[5] = torch.finfo(dtype).max
+    kept = ffe.checkpoint_q8(x, group=group)
+    q, scale = _want(x, group)
+    assert torch.equal(kept.codes, q)
+    nan = scale.isnan()
+    assert torch.equal(kept.scale.isnan(), nan) and int(nan.sum()) == 3
+    assert bool(((kept.scale.double() - scale).abs()[~nan] <= 2.0 ** -24 * scale[~nan]).all())
+    back = ffe.checkpoint_restore(kept, dtype=dtype)
+    assert bool(back[1, 0:48].isnan().all()) and not bool(back[1, 48:].isnan().any())
+    assert bool((back[2, 0:16] == 0).all()) and bool((back[3, 0:16] == 0).all()) and float(back[4, 7]) != 0
+
+
+def test_strides_rank_and_empty(gpu):
+    wide = _rows(gpu, 40, 333, BF16, seed=1)
+    x = wide[:, 7:257]
+    kept, plain = ffe.checkpoint_q8(x, group=32), ffe.checkpoint_q8(x.contiguous(), group=32)
+    assert torch.equal(kept.codes, plain.codes) and torch.equal(kept.scale, plain.scale)
+    three = ffe.checkpoint_q8(x.contiguous().view(2, 20, 250), group=32)
+    assert three.codes.shape == (2, 20, 250) and three.scale.shape == (2, 20, 8)
+    assert torch.equal(three.codes.view(40, 250), plain.codes)
+    one = ffe.checkpoint_q8(x[3].contiguous(), group=32)
+    assert one.codes.shape == (250,) and torch.equal(one.codes, plain.codes[3])
+    # codes and scales that lie apart
+    q = torch.zeros(40, 300, dtype=torch.int8, device=gpu)[:, 3:253]
+    s = torch.zeros(40, 11, device=gpu)[:, 1:9]
+    q.copy_(plain.codes), s.copy_(plain.scale)
+    assert torch.equal(ffe.checkpoint_restore(ffe.Checkpoint(q, s, 32)), ffe.checkpoint_restore(plain))
+    empty = ffe.checkpoint_q8(x[:0])
+    assert empty.codes.shape == (0, 250) and empty.scale.shape == (0, 2)
+    assert ffe.checkpoint_restore(empty).shape == (0, 250)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = ffe.checkpoint_q8(x, group=32, stream=side)
+    back = ffe.checkpoint_restore(other, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(other.codes, plain.codes) and torch.equal(back, ffe.checkpoint_restore(plain))
+
+
+def test_refusals(gpu):
+    x = _rows(gpu, 4, 64, BF16)
+    kept = ffe.checkpoint_q8(x)
+    for group in (0, 8, 24, 1024, 128.0, None):
+        with pytest.raises(ValueError):
+            ffe.checkpoint_q8(x, group=group)
+    with pytest.raises(TypeError):
+        ffe.checkpoint_q8(x.half())
+    with pytest.raises(TypeError):
+        ffe.checkpoint_q8(x.cpu())
+    with pytest.raises(ValueError):
+        ffe.checkpoint_q8(x.t())
+    with pytest.raises(TypeError):
+        ffe.checkpoint_restore(x)
+    with pytest.raises(TypeError):
+        ffe.checkpoint_restore(kept, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        ffe.checkpoint_restore(ffe.Checkpoint(kept.codes, kept.scale, 32))
+    with pytest.raises(ValueError):
+        ffe.checkpoint_restore(ffe.Checkpoint(kept.codes, kept.scale[:3], 128))
+    with pytest.raises(TypeError):
+        ffe.checkpoint_restore(ffe.Checkpoint(kept.codes.float(), kept.scale, 128))
+    W = _rows(gpu, 32, 64, BF16)
+    dy = _rows(gpu, 4, 32, BF16)
+    with pytest.raises(ValueError):
+        ffe.linear_backward(dy, kept, W[:, :60].contiguous())
+    with pytest.raises(ValueError):
+        ffe.linear_backward(dy, kept, W, preact=kept, activation="relu")
+
+
+def _slope(z, act):
+    if act == "relu":   # zero at zero, where codes often are
+        return (z > 0).double()
+    z = z.clone().requires_grad_()
+    y = {"none": lambda: z * 1, "silu": lambda: z * torch.sigmoid(z),
+         "gelu": lambda: 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))}[act]()
+    return torch.autograd.grad(y.sum(), z)[0]
+
+
+def _close(got, want, tol):
+    assert got.shape == want.shape
+    bad = (got.double() - want).abs() > tol
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("x8,z8", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("T,n,m", [(1, 1, 1), (1, 64, 16), (7, 1001, 250), (64, 130, 72), (200, 513, 129), (1021, 256, 333)])
+def test_linear_backward(gpu, T, n, m, x8, z8):
+    x, z, dy, W = (_rows(gpu, *s, BF16, seed=k) for k, s in enumerate([(T, n), (T, m), (T, m), (m, n)]))
+    group = GROUPS[(T + n) % 6]
+    kx, kz = ffe.checkpoint_q8(x, group=group), ffe.checkpoint_q8(z, group=group)
+
+    def value(k):
+        return k.codes.double() * torch.repeat_interleave(k.scale.double(), group, dim=1)[:, :k.codes.shape[1]]
+    xv, zv = value(kx) if x8 else x.double(), value(kz) if z8 else z.double()
+    for act in ("none", "relu", "gelu", "silu"):
+        dx, dw, g, db = ffe.linear_backward(dy, kx if x8 else x, W, preact=(kz if z8 else z) if act != "none" else None,
+                                            activation=act)
+        g64 = dy.double() * _slope(zv, act)
+        # a slope is good to 2^-18 of its terms (each below 1.2 |z| + 1.2)
+        _close(g, g64, HALF * 1.01 * g64.abs() + 2.0 ** -18 * dy.double().abs() * 1.2 * (1 + zv.abs()) + 1e-30)
+        gb, W64 = g.double(), W.double()
+        want, mag = gb @ W64, gb.abs() @ W64.abs()
+        _close(dx, want, HALF * want.abs() * 1.01 + m * 2.0 ** -24 * mag + 1e-30)
+        want, mag = gb.T @ xv, gb.abs().T @ xv.abs()
+        # every x' rounded to bf16: 2^-8 of each term at most
+        _close(dw, want, HALF * want.abs() * 1.01 + (T * 2.0 ** -24 + HALF * 1.01 * x8) * mag + 1e-30)
+        want, mag = gb.sum(0), gb.abs().sum(0)
+        _close(db, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + 1e-30)
+    # what the bf16 form gives for the values that the codes stand for
+    if x8 and z8:
+        rx, rz = ffe.checkpoint_restore(kx), ffe.checkpoint_restore(kz)
+        a, b = ffe.linear_backward(dy, kx, W), ffe.linear_backward(dy, rx, W)
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+        a = ffe.linear_backward(dy, rx, W, preact=kz, activation="relu")
+        b = ffe.linear_backward(dy, kx, W, preact=rz, activation="relu")
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_linear_backward_parts_and_none(gpu):
+    kx = ffe.checkpoint_q8(_rows(gpu, 30, 100, BF16))
+    W, dy = _rows(gpu, 50, 100, BF16, seed=1), _rows(gpu, 30, 50, BF16, seed=2)
+    full = ffe.linear_backward(dy, kx, W)
+    for which in range(3):
+        need = [k == which for k in range(3)]
+        part = ffe.linear_backward(dy, kx, W, need_input=need[0], need_weight=need[1], need_bias=need[2])
+        for got, want, k in zip((part[0], part[1], part[3]), (full[0], full[1], full[3]), need):
+            assert (got is None) != k and (got is None or torch.equal(got, want))
+    empty = ffe.linear_backward(dy[:0], ffe.Checkpoint(kx.codes[:0], kx.scale[:0], 128), W)
+    assert empty[0].shape == (0, 100) and not bool(empty[1].any()) and not bool(empty[3].any())
+
+
+def test_captured(gpu):
+    """Kept and used in one graph, replayed with the program's own work between."""
+    x, z, dy, W = (_rows(gpu, *s, BF16, seed=k) for k, s in enumerate([(70, 200), (70, 130), (70, 130), (130, 200)]))
+
+    def step():
+        kx, kz = ffe.checkpoint_q8(x, group=64), ffe.checkpoint_q8(z, group=32)
+        return ffe.linear_backward(dy, kx, W, preact=kz, activation="silu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        x.copy_(_rows(gpu, 70, 200, BF16, seed=10 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
