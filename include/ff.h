@@ -551,6 +551,183 @@ typedef struct {
 } ff_linear_grad_q8_args;
 ff_status ff_linear_backward_q8(const ff_linear_grad_q8_args* args);
 
+/* ---- Layers of experts ----
+ * Each of `tokens` tokens takes `top` of `experts` experts: slot s = t top + j is token t's
+ * j-th choice.  The products work on rows, one for each slot, sorted by expert and by
+ * slot within one.  top <= 64, experts <= 1024, tokens top <= 2^24.  What the arrays of a
+ * routing hold is not trusted: entries out of range are left out (no token's row, no
+ * slot's row). */
+typedef struct {
+  int64_t tokens, experts, top;
+  const float* weights;     /* tokens x top; where it is read, see below */
+  const int32_t* order;     /* tokens x top: the slot in each row, -1 after the last */
+  const int32_t* offsets;   /* experts + 1: expert e has rows offsets[e] .. offsets[e + 1] - 1 */
+  const int32_t* place;     /* tokens x top: each slot's row, or -1 */
+} ff_routing;
+
+typedef enum { FF_SCORE_SOFTMAX = 0, FF_SCORE_SIGMOID = 1 } ff_score;
+
+/* Routing.  s_e = softmax over the experts of l_e, or sigmoid(l_e);  c_e = s_e + bias_e.
+ * With groups (experts / groups neighbours each) only the top_groups groups are kept whose two
+ * largest c sum to most (the one, in groups of one).  Chosen are the `top` largest c in their
+ * order, the lowest index among equals (of groups too); weights are scale s, or with renormalise scale s over
+ * the sum of the chosen s (0 where that is 0).  Scores and sums are held in 64 bits.
+ * A NaN c or group counts as the lowest value.  Under softmax a row of -inf alone has scores 0,
+ * one with a NaN or +inf NaN scores.  Tokens whose mask is 0 take no expert: chosen -1, weights 0.
+ * order, offsets and place receive the slots' order (all or none of them); ff_expert_order
+ * makes them from `chosen` alone (any number outside 0 .. experts - 1: not routed). */
+typedef struct {
+  int64_t tokens, experts, top;
+  ff_dtype dtype;           /* logits */
+  const void* logits;       /* tokens x experts */
+  int64_t ldl;
+  const float* bias;        /* experts; or NULL */
+  const uint8_t* mask;      /* tokens; or NULL */
+  ff_score score;
+  int64_t groups;           /* 0 or 1: none; <= 64, divides experts */
+  int64_t top_groups;       /* read with groups > 1 */
+  int renormalise;          /* 0 or 1 */
+  double scale;
+  float* weights;           /* tokens x top */
+  int32_t* chosen;          /* tokens x top (ff_expert_order reads it) */
+  int32_t* order;           /* tokens x top; or NULL */
+  int32_t* offsets;         /* experts + 1; or NULL */
+  int32_t* place;           /* tokens x top; or NULL */
+  void* workspace;          /* with order; may be NULL where its size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} ff_route_args;
+/* Reads tokens, experts and top.  Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_route_workspace_size(const ff_route_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP.  With no tokens offsets is set to
+ * zeros. */
+ff_status ff_route(const ff_route_args* args);
+ff_status ff_expert_order(const ff_route_args* args);
+
+/* Gradient of the weights of ff_route with respect to the logits (bias and choice count as
+ * constants), in 64 bits.  Choices outside 0 .. experts - 1 have none.  dlogits may be the
+ * logits themselves (the same rows and ld). */
+typedef struct {
+  int64_t tokens, experts, top;
+  ff_dtype dtype;           /* logits and dlogits */
+  const void* logits;
+  int64_t ldl;
+  const float* dweights;    /* tokens x top */
+  const int32_t* chosen;    /* tokens x top */
+  ff_score score;
+  int renormalise;
+  double scale;
+  void* dlogits;            /* tokens x experts */
+  int64_t ldd;
+  void* stream;
+} ff_route_grad_args;
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_HIP. */
+ff_status ff_route_backward(const ff_route_grad_args* args);
+
+/* The experts' linear layers W_e (m x n) on the rows of a routed batch:
+ *     z = x W_e^T + bias_e,  y = act(z)
+ * All bf16.  x: the tokens' rows, or with by_slot a row for each slot (an output of this
+ * function).  Rows in no expert are zeros in y and preact.  Reads order and offsets. */
+typedef struct {
+  ff_routing routing;
+  int64_t n, m;             /* <= 2^20 */
+  const void* x;            /* tokens x n, or by_slot tokens top x n */
+  int64_t ldx;
+  int by_slot;              /* 0 or 1 */
+  const void* w;            /* experts x m rows of n */
+  int64_t ldw;
+  const void* bias;         /* experts x m; or NULL */
+  ff_activation activation;
+  void* y;                  /* tokens top x m */
+  int64_t ldy;
+  void* preact;             /* receives z; or NULL */
+  int64_t ldz;
+  void* workspace;          /* may be NULL where its size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} ff_expert_linear_args;
+/* Reads the sizes, ldx, ldw, by_slot and the alignment of x and w.  Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_expert_linear_workspace_size(const ff_expert_linear_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP. */
+ff_status ff_expert_linear(const ff_expert_linear_args* args);
+
+/* A token's rows weighted and summed, in the order of its choices:
+ *     out_t = residual_t + sum_j weights_tj y[place_tj]
+ * All bf16 but the weights (NULL: ones).  out may be the residual itself (the same rows and ld).
+ * Reads offsets, place and weights. */
+typedef struct {
+  ff_routing routing;
+  int64_t cols;             /* <= 2^20 */
+  const void* y;            /* tokens top x cols */
+  int64_t ldy;
+  const void* residual;     /* tokens x cols; or NULL */
+  int64_t ldr;
+  void* out;                /* tokens x cols */
+  int64_t ldo;
+  void* stream;
+} ff_expert_combine_args;
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_HIP. */
+ff_status ff_expert_combine(const ff_expert_combine_args* args);
+
+/* Its gradient (the residual's is dout itself): dy of a row is its weight times dout of its token
+ * (fp32: it is rounded once, as part of g; zeros for rows in no expert), dweights_tj =
+ * <dout_t, y[place_tj]> (0 where there is no row).  Reads all of the routing. */
+typedef struct {
+  ff_routing routing;
+  int64_t cols;             /* <= 2^20 */
+  const void* dout;         /* tokens x cols, bf16 */
+  int64_t ldd;
+  const void* y;            /* tokens top x cols, bf16; needed for dweights */
+  int64_t ldy;
+  float* dy;                /* tokens top x cols; or NULL */
+  int64_t lddy;
+  float* dweights;          /* tokens x top; or NULL */
+  void* stream;
+} ff_expert_combine_grad_args;
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_HIP. */
+ff_status ff_expert_combine_backward(const ff_expert_combine_grad_args* args);
+
+/* Gradient of ff_expert_linear:
+ *     g = dy act'(preact) by rows (zeros for rows in no expert)
+ *     dx = g W_e by rows, or without by_slot summed over each token's rows (in fp32)
+ *     dw_e = sum over the expert's rows of g^T x,  db_e = sum of g  (zeros for an expert without rows)
+ * bf16, but dy in either type.  g is rounded before it is used (an expert's rows of x and g
+ * are the tokens that ff_config takes).  x_q8 and preact_q8 (q not NULL) are checkpoints that stand
+ * for x and preact; for dw of a checkpoint g and x are rounded to 11 bits (fp16, scaled by powers
+ * of two) instead, each value to at least 2^-40 of the largest.  Reads order, offsets and (without by_slot) place. */
+typedef struct {
+  ff_routing routing;
+  int64_t n, m;             /* <= 2^20 */
+  ff_dtype dy_dtype;
+  const void* dy;           /* tokens top x m */
+  int64_t lddy;
+  const void* x;            /* tokens x n, or by_slot tokens top x n; needed for dw (or x_q8) */
+  int64_t ldx;
+  ff_q8_rows x_q8;
+  int by_slot;
+  const void* w;            /* experts x m rows of n; needed for dx */
+  int64_t ldw;
+  const void* preact;       /* tokens top x m; needed with an activation (or preact_q8) */
+  int64_t ldz;
+  ff_q8_rows preact_q8;
+  ff_activation activation;
+  void* g;                  /* tokens top x m; or NULL */
+  int64_t ldg;
+  void* dx;                 /* as x, bf16; or NULL */
+  int64_t lddx;
+  void* dw;                 /* experts x m rows of n; or NULL */
+  int64_t lddw;
+  void* db;                 /* experts x m; or NULL */
+  void* workspace;          /* may be NULL where its size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} ff_expert_grad_args;
+/* Reads everything but the arrays' contents.  Errors: FF_ERR_INVALID_ARG. */
+ff_status ff_expert_linear_backward_workspace_size(const ff_expert_grad_args* args, size_t* bytes);
+/* Errors: FF_ERR_INVALID_ARG, FF_ERR_WORKSPACE, FF_ERR_HIP.  With no tokens dw and db are set to
+ * zeros. */
+ff_status ff_expert_linear_backward(const ff_expert_grad_args* args);
+
 /* Orthogonalisation of updates G (m x n) by `steps` Newton-Schulz products:
  *     X = G / (||G||_F + eps);  A = X X^T, X <- a X + (b A + c A A) X;  out = scale X
  * (the smaller of X X^T and X^T X, the same X).  Sums are fp32.  FF_F32:

@@ -6,7 +6,8 @@ Hessian, Section 5), and quantises its weights with WaterKron (two-sided
 GPTQ with waterfilling scales, Section 3), entirely in the HIP library
 ``libff.so`` whose C ABI is ``include/ff.h``.  Around the layer are its
 operators (layer.py): the norm, the layer in bf16 or from the quantiser's codes, their
-gradients, the orthogonalisation of an update.  This package is the thin
+gradients, activations kept in 8 bits, the orthogonalisation of an update; and those
+of a layer of experts (experts.py): routing, the experts' products, their gradients.  This package is the thin
 binding (ctypes + torch memory).
 """
 from .binding import (FF_APPLY, FF_APPLY_INV, FF_BF16, FF_ERR_HIP, FF_ERR_INVALID_ARG,
@@ -28,13 +29,23 @@ _LAYER = ("ACTIVATIONS", "Checkpoint", "checkpoint_q8", "checkpoint_restore", "f
           "ff_ortho_args", "ff_q8_rows", "linear", "linear_backward", "linear_q8", "orthogonalize", "quantize_rows",
           "rms_norm", "rms_norm_backward", "rms_norm_q8")
 
+_EXPERTS = ("Routing", "SCORES", "expert_combine", "expert_combine_backward", "expert_linear",
+            "expert_linear_backward", "expert_order", "ff_expert_combine_args", "ff_expert_combine_grad_args",
+            "ff_expert_grad_args", "ff_expert_linear_args", "ff_route_args", "ff_route_grad_args", "ff_routing",
+            "route", "route_backward")
+
 
 def __getattr__(name):
-    if name not in _LAYER:
+    if name in _LAYER:
+        from . import layer as home
+        names = _LAYER
+    elif name in _EXPERTS:
+        from . import experts as home
+        names = _EXPERTS
+    else:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    from . import layer
-    globals().update({n: getattr(layer, n) for n in _LAYER})
+    globals().update({n: getattr(home, n) for n in names})
     return globals()[name]
 
 
-__all__ = [n for n in dir() if not n.startswith("_")] + list(_LAYER)
+__all__ = [n for n in dir() if not n.startswith("_")] + list(_LAYER) + list(_EXPERTS)

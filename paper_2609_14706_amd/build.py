@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libff.so")
 BENCH = os.path.join(HERE, "ffbench")
 SOURCES = ["ff_gemm_bf16.hip", "ff_gemm_f32.hip", "ff_gemm_split.hip", "ff_chol.hip", "ff_aux.hip", "ff_waterkron.hip",
-           "ff_norm.hip", "ff_linear.hip", "ff_checkpoint.hip", "ff_ortho.hip", "ff_layer.hip", "ff_engine.hip"]
+           "ff_norm.hip", "ff_linear.hip", "ff_checkpoint.hip", "ff_ortho.hip", "ff_layer.hip", "ff_route.hip", "ff_expert.hip",
+           "ff_expert_layer.hip", "ff_engine.hip"]
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,165 @@
+// Host-side launchers of the operators around a layer of experts: routing, the
+// experts' products and their gradients.  As in ff_layer_kernels.hpp.
+//
+// T tokens choose `top` of E experts each: slot s = t top + j is token t's j-th
+// choice.  Slots sorted by expert (and by slot within one) are the rows that the
+// experts' products work on: row p holds slot order[p], expert e rows offsets[e] ..
+// offsets[e + 1] - 1, and slot s lies at row place[s] (-1: not routed, in no row).
+#pragma once
+
+#include "ff_layer_kernels.hpp"
+
+namespace ff {
+
+constexpr int kMaxExperts = 1024, kMaxTop = 64, kMaxGroups = 64;
+
+struct RouteArgs {
+  int64_t tokens;
+  int experts, top;
+  const void* logits;  // tokens x experts
+  int64_t ldl;
+  bool bf16;
+  const float* bias;    // experts, or null
+  const uint8_t* mask;  // tokens: 0 not routed; or null
+  bool sigmoid;         // scores: else softmax
+  int groups, top_groups;
+  bool renormalise;
+  double scale;
+  float* weights;   // tokens x top
+  int32_t* chosen;  // tokens x top
+  int32_t* order;   // tokens x top; null: slots are not sorted
+  int32_t* offsets;
+  int32_t* place;
+};
+// Bytes of workspace of the sort (0 where one workgroup does it all).
+size_t route_workspace(int64_t tokens, int experts, int top);
+hipError_t launch_route(const RouteArgs& a, void* workspace, hipStream_t s);
+// order, offsets and place of the experts in a.chosen.
+hipError_t launch_order(const RouteArgs& a, void* workspace, hipStream_t s);
+
+struct RouteGradArgs {
+  int64_t tokens;
+  int experts, top;
+  const void* logits;
+  int64_t ldl;
+  bool bf16;
+  const float* dweights;  // tokens x top
+  const int32_t* chosen;
+  bool sigmoid, renormalise;
+  double scale;
+  void* dlogits;  // tokens x experts, as logits
+  int64_t ldd;
+};
+hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
+
+// The rows of a routed batch: `rows` = tokens top of them, those from offsets[experts] on
+// in no expert.  What the arrays hold is checked against rows before it is used.
+struct SlotRows {
+  int64_t tokens, rows;
+  int experts, top;
+  const int32_t* order;
+  const int32_t* offsets;
+  const int32_t* place;
+  const float* weights;
+};
+
+// y_p = act(x W_e^T + b_e) of the rows of each expert e; rows in no expert get zeros.
+// x: a token's row for each of its slots (gather), or a row for each slot.
+struct ExpertArgs {
+  SlotRows at;
+  LinearArgs lin;  // w: experts x m rows of n, bias: experts x m; y and preact by row
+  bool gather;
+};
+// How the products are run: `nt` 16-token tiles of the few-token form with `waves` waves a
+// workgroup (rw 16-output tiles), or (nt 0) tiles of 32 ti x 32 tj, `slots` pairs of k in LDS.
+struct ExpertPlan {
+  int nt, rw, waves;
+  int ti, tj, slots;
+};
+ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m);
+hipError_t launch_expert_linear(const ExpertArgs& a, const ExpertPlan& p, hipStream_t s);
+
+// out_t = residual_t + sum over the token's slots of weight y (rows of bf16), or the
+// plain sum of fp32 rows (weights null).
+struct CombineArgs {
+  SlotRows at;
+  int64_t cols;
+  const void* y;
+  int64_t ldy;
+  bool f32;
+  const bf16_t* residual;  // or null
+  int64_t ldr;
+  bf16_t* out;
+  int64_t ldo;
+};
+hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
+
+// dy_p = weight dout_t (fp32), dweight_s = <dout_t, y_p>; zeros where there is no slot or row.
+struct CombineGradArgs {
+  SlotRows at;
+  int64_t cols;
+  const bf16_t* dout;
+  int64_t ldd;
+  const bf16_t* y;
+  int64_t ldy;
+  float* dy;  // or null
+  int64_t lddy;
+  float* dweights;  // or null
+};
+hipError_t launch_combine_grad(const CombineGradArgs& a, hipStream_t s);
+
+// Rows for the products to read: dst_p = src of row p or (gather) of its token, times
+// act'(z_p) where z is given, zeros for rows in no expert.  Stored as `out` (bf16), `laid`
+// (bf16, rows of laid_ld(cols) elements with zeros beyond cols) and `scaled` (the same in fp16,
+// times the power of two that takes the peaks' largest to 2^14 .. 2^15).
+struct RowsArgs {
+  SlotRows at;
+  bool gather;
+  int64_t cols;
+  const void* src;  // bf16, or fp32 (src_f32), or null (then src_q8)
+  int64_t lds;
+  bool src_f32;
+  Q8Rows src_q8;
+  const bf16_t* z;  // or z_q8, or neither
+  int64_t ldz;
+  Q8Rows z_q8;
+  int act;
+  bf16_t* out;  // or null
+  int64_t ldo;
+  uint16_t* laid;         // or null
+  uint16_t* scaled;       // or null
+  const uint32_t* peaks;  // scaled: kPeaks bit patterns, of which the largest counts
+  float peak_factor;      // scaled: the largest value is at most that times the peak
+};
+constexpr int kPeaks = 256;
+inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
+hipError_t launch_rows(const RowsArgs& a, hipStream_t s);
+// peaks: kPeaks bit patterns of the largest finite magnitudes of rows x cols elements.
+hipError_t launch_peaks(const void* src, int64_t ld, int64_t rows, int64_t cols, bool f32, uint32_t* peaks, hipStream_t s);
+
+// dx_p = g_p W_e: g rows of bf16 (16-byte aligned, zeros up to a multiple of 8), W as it lies
+// (experts x m rows of n, 16-byte aligned); out bf16 or fp32, zeros for rows in no expert.
+struct ExpertGradArgs {
+  SlotRows at;
+  int64_t n, m;
+  const uint16_t* g;
+  int64_t ldg;
+  const bf16_t* w;  // launch_expert_dx
+  int64_t ldw;
+  const uint16_t* x;  // launch_expert_dw
+  int64_t ldx;
+  void* out;
+  int64_t ldo;
+  bool out_f32;
+  bool f16;  // launch_expert_dw: g and x are fp16 scaled by their peaks
+  const uint32_t* g_peaks;
+  const uint32_t* x_peaks;
+  float g_factor, x_factor;
+};
+hipError_t launch_expert_dx(const ExpertGradArgs& a, hipStream_t s);
+// dW_e = sum over the rows of expert e of g_p^T x_p (m x n; zeros for an expert without rows).
+hipError_t launch_expert_dw(const ExpertGradArgs& a, hipStream_t s);
+// db_e = sum over the rows of expert e of g_p (bf16 rows).
+hipError_t launch_expert_db(const SlotRows& at, const bf16_t* g, int64_t ldg, int64_t m, bf16_t* db, hipStream_t s);
+
+}  // namespace ff

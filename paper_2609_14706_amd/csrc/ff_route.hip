@@ -1,0 +1,539 @@
+// Routing to experts: from each token's logits to the experts that it takes, their
+// weights, and the slots (token, choice) sorted by expert; the weights' gradient.
+//
+//   s_e = softmax_e(l) or sigmoid(l_e);  c_e = s_e + bias_e
+//   groups of experts: the top_groups whose two best c sum to most are kept
+//   chosen: the `top` largest c, the lowest index among equals
+//   w_j = scale s_j, or scale s_j / sum of the chosen s
+//
+// Scores are held in 64 bits: which expert is chosen may hang on the last bit of c,
+// and 32 bits of exp would decide otherwise than the formula for about one token in
+// ten thousand.  A wave takes a token, V neighbouring experts a lane; it picks one
+// expert after the other, each the largest of the lanes' best: c as a whole number that
+// orders alike, its high words compared first across the wave (DPP), the low ones only
+// where two lanes share the high one.
+//
+// The sort is a counting sort, stable and without an atomic on memory: chunks of
+// tokens count their slots by expert (k_route), a wave for each expert sums the chunks'
+// counts (k_scan), and each chunk places its own slots (k_place): a wave takes 64 at a time,
+// a slot's rank among those of its expert by ballots over the expert's bits.  Few
+// tokens do all of it in one workgroup and one launch.
+#include <math.h>
+
+#include <algorithm>
+
+#include "ff_common.hpp"
+#include "ff_expert_kernels.hpp"
+
+namespace ff {
+namespace {
+
+typedef unsigned long long u64;
+
+// Largest 32-bit value of the wave, in every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, from_lane<0x111, 0xf>(v));  // row_shr 1, 2, 4, 8: lane 15 of a row holds its largest
+  v = max(v, from_lane<0x112, 0xf>(v));
+  v = max(v, from_lane<0x114, 0xf>(v));
+  v = max(v, from_lane<0x118, 0xf>(v));
+  v = max(v, from_lane<0x142, 0xa>(v));  // row_bcast 15, 31: lane 63 the wave's
+  v = max(v, from_lane<0x143, 0xc>(v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// A whole number that orders as c does, above 0 (which is "not to be chosen"); a
+// NaN counts as the lowest value.
+__device__ __forceinline__ u64 key_of(double c) {
+  if (c != c) c = -INFINITY;
+  const u64 b = (u64)__double_as_longlong(c);
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+
+// The lane that holds the largest of the lanes' keys, the lowest one among equals
+// (lanes hold ascending experts); largest: its key.
+__device__ __forceinline__ int best_lane(u64 mine) {
+  const uint32_t hi = (uint32_t)(mine >> 32), top = wave_max(hi);
+  u64 who = __ballot(hi == top);
+  if (who & (who - 1)) {
+    const uint32_t lo = hi == top ? (uint32_t)mine : 0u, low = wave_max(lo);
+    who = __ballot(hi == top && lo == low);
+  }
+  return __ffsll((long long)who) - 1;
+}
+
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const u64 b = (u64)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __longlong_as_double((long long)((u64)hi << 32 | lo));
+}
+
+// Scores of the V experts of a lane from their logits (those beyond the last: 0).
+template <class L, int V>
+__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, double (&s)[V]) {
+  const int e0 = (threadIdx.x & 63) * V;
+  float l[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) l[i] = e0 + i < experts ? Elem<L>::to_f32(row[e0 + i]) : -INFINITY;
+  if (sigmoid) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = e0 + i < experts ? 1.0 / (1.0 + exp(-(double)l[i])) : 0.0;
+    return;
+  }
+  float big = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    big = fmaxf(big, l[i]);
+    nan |= l[i] != l[i];
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+  if (__ballot(nan) != 0) big = __uint_as_float(0x7fc00000u);  // the row's scores are NaN then
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    // (a row of -inf alone has no scores: zeros, not 0 / 0)
+    s[i] = e0 + i < experts && big != -INFINITY ? exp((double)l[i] - (double)big) : 0.0;
+    sum += s[i];
+  }
+  sum = wave_sum(sum);
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = big == -INFINITY ? 0.0 : s[i] / sum;
+}
+
+// A token's choice, in lane j the j-th: expert and score (lanes from `top` on: -1, 0).
+// stage: room for the token's experts, with groups.
+template <class L, int V>
+__device__ __forceinline__ void choose(const RouteArgs& a, int64_t t, double* stage, int& expert, double& score) {
+  const int lane = threadIdx.x & 63, e0 = lane * V;
+  double s[V];
+  scores_of<L, V>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, s);
+  u64 key[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const bool in = e0 + i < a.experts;
+    const double c = a.bias != nullptr && in ? s[i] + (double)a.bias[e0 + i] : s[i];
+    key[i] = in ? key_of(c) : 0;
+    if (stage != nullptr && in) stage[e0 + i] = c;
+  }
+  if (stage != nullptr) {
+    // A lane takes a group; its experts are read from a place of its own on, so that the
+    // lanes' reads spread over the banks.  A NaN counts as the lowest value.
+    __builtin_amdgcn_wave_barrier();
+    const int size = a.experts / a.groups;
+    double first = -INFINITY, second = -INFINITY;
+    if (lane < a.groups) {
+      int j = lane % size;
+      for (int i = 0; i < size; ++i) {
+        const double c = stage[lane * size + j];
+        if (c > first) {
+          second = first;
+          first = c;
+        } else if (c > second) {
+          second = c;
+        }
+        j = j + 1 == size ? 0 : j + 1;
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    u64 rank = lane < a.groups ? key_of(size > 1 ? first + second : first) : 0, kept = 0;
+    for (int j = 0; j < a.top_groups; ++j) {
+      const int g = best_lane(rank);
+      kept |= u64(1) << g;
+      if (lane == g) rank = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (e0 + i < a.experts && !(kept >> ((e0 + i) / size) & 1)) key[i] = 0;
+  }
+  expert = -1;
+  score = 0.0;
+  u64 best = 0;
+  double best_score = 0.0;
+  int best_at = 0;
+  auto look = [&]() {
+    best = key[0];
+    best_score = s[0];
+    best_at = 0;
+#pragma unroll
+    for (int i = 1; i < V; ++i)
+      if (key[i] > best) {
+        best = key[i];
+        best_score = s[i];
+        best_at = i;
+      }
+  };
+  look();
+  for (int j = 0; j < a.top; ++j) {
+    const int l = best_lane(best);
+    const int e = l * V + __builtin_amdgcn_readlane(best_at, l);
+    const double v = lane_value(best_score, l);
+    if (lane == j) {
+      expert = e;
+      score = v;
+    }
+    if (lane == l) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i == best_at) key[i] = 0;
+      look();
+    }
+  }
+}
+
+// One token by one wave: its weights and experts.  Returns lane j's expert, or -1.
+template <class L, int V>
+__device__ __forceinline__ int route_token(const RouteArgs& a, int64_t t, double* stage) {
+  const int lane = threadIdx.x & 63;
+  int e = -1;
+  double s = 0.0;
+  if (a.mask == nullptr || a.mask[t] != 0) choose<L, V>(a, t, stage, e, s);
+  double w = s;
+  if (a.renormalise) {
+    const double sum = wave_sum(s);
+    w = sum == 0.0 ? 0.0 : s / sum;
+  }
+  if (lane < a.top) {
+    a.weights[t * a.top + lane] = (float)(w * a.scale);
+    a.chosen[t * a.top + lane] = e;
+  }
+  return e;
+}
+
+// ---------------------------------------------------------------- the sort
+// Whether expert e takes slots: anything else is in no row.
+__device__ __forceinline__ bool taken(int e, int experts) { return (unsigned)e < (unsigned)experts; }
+
+// Slots s0 .. s1 - 1 to their rows.  count: WAVES x experts numbers of LDS;
+// first(e): the first row of this chunk's slots of expert e.
+template <int WAVES, class First>
+__device__ __forceinline__ void place_slots(const RouteArgs& a, int64_t s0, int64_t s1, int* count, First first) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+  const int64_t per = ((s1 - s0 + WAVES - 1) / WAVES + 63) / 64 * 64;
+  const int64_t b0 = min(s1, s0 + wave * per), b1 = min(s1, b0 + per);
+  for (int i = tid; i < WAVES * a.experts; i += 64 * WAVES) count[i] = 0;
+  __syncthreads();
+  int* mine = count + wave * a.experts;
+  for (int64_t s = b0 + lane; s < b1; s += 64) {
+    const int e = a.chosen[s];
+    if (taken(e, a.experts)) atomicAdd(&mine[e], 1);  // (LDS; sums of ones in any order)
+  }
+  __syncthreads();
+  for (int e = tid; e < a.experts; e += 64 * WAVES) {
+    int row = first(e);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int c = count[w * a.experts + e];
+      count[w * a.experts + e] = row;
+      row += c;
+    }
+  }
+  __syncthreads();
+  const int bits = 32 - __clz(a.experts);  // of 0 .. experts
+  volatile int* next = mine;
+  for (int64_t s = b0; s < b1; s += 64) {
+    int e = s + lane < b1 ? a.chosen[s + lane] : -1;
+    const bool in = taken(e, a.experts);
+    e = in ? e : a.experts;
+    u64 same = ~u64(0);
+    for (int b = 0; b < bits; ++b) {
+      const u64 one = __ballot(e >> b & 1);
+      same &= e >> b & 1 ? one : ~one;
+    }
+    const u64 before = same & ((u64(1) << lane) - 1);
+    int row = -1;
+    if (in) row = next[e] + __popcll(before);
+    __builtin_amdgcn_wave_barrier();
+    if (in && before == 0) next[e] = row + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    if (s + lane < b1) {
+      a.place[s + lane] = row;
+      if (in) a.order[row] = (int32_t)(s + lane);
+    }
+  }
+}
+
+// Exclusive sums of the experts' totals by THREADS threads: start[e], start[experts] the
+// total.  Up to kMaxExperts / THREADS neighbours a thread; sums: a number a wave.
+template <int THREADS, class Total>
+__device__ __forceinline__ void starts(int experts, int* start, int* sums, Total total) {
+  constexpr int N = (kMaxExperts + THREADS - 1) / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int v[N], sum = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = tid * N + i;
+    v[i] = e < experts ? total(e) : 0;
+    sum += v[i];
+  }
+  int run = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(run, d);
+    if (lane >= d) run += up;
+  }
+  if (lane == 63) sums[wave] = run;
+  __syncthreads();
+  int at = run - sum;
+  for (int w = 0; w < wave; ++w) at += sums[w];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = tid * N + i;
+    if (e < experts) start[e] = at;
+    at += v[i];
+    if (e == experts - 1) start[experts] = at;
+  }
+  __syncthreads();
+}
+
+constexpr int kRouteWaves = 8, kPlaceWaves = 4;
+constexpr int kChunks = 512;      // most, and most numbers a wave of k_scan sums: 8 a lane
+constexpr int64_t kFewSlots = 512;  // one workgroup does all of them
+constexpr int64_t kFewTokens = 64;
+
+// Tokens of a chunk.
+__host__ __device__ inline int64_t chunk_tokens(int64_t tokens) {
+  const int64_t least = (tokens + kChunks - 1) / kChunks;
+  return least < kRouteWaves ? kRouteWaves : least;
+}
+
+// CHOOSE: route the chunk's tokens; else their experts are there.  counts: experts x
+// chunks (null: no sort).
+template <class L, int V, bool CHOOSE>
+__global__ __launch_bounds__(64 * kRouteWaves) void k_route(RouteArgs a, int64_t per, int* counts) {
+  extern __shared__ __align__(16) char lds[];
+  double* stages = (double*)lds;
+  int* count = (int*)(lds + (CHOOSE && a.groups > 1 ? (size_t)kRouteWaves * a.experts * 8 : 0));
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t t0 = blockIdx.x * per, t1 = min(a.tokens, t0 + per);
+  if (counts != nullptr) {
+    for (int i = threadIdx.x; i < a.experts; i += 64 * kRouteWaves) count[i] = 0;
+    __syncthreads();
+  }
+  if (CHOOSE) {
+    for (int64_t t = t0 + wave; t < t1; t += kRouteWaves) {
+      const int e = route_token<L, V>(a, t, a.groups > 1 ? stages + wave * a.experts : nullptr);
+      if (counts != nullptr && taken(e, a.experts)) atomicAdd(&count[e], 1);
+    }
+  } else {
+    for (int64_t s = t0 * a.top + threadIdx.x; s < t1 * a.top; s += 64 * kRouteWaves) {
+      const int e = a.chosen[s];
+      if (taken(e, a.experts)) atomicAdd(&count[e], 1);
+    }
+  }
+  (void)lane;
+  if (counts == nullptr) return;
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.experts; e += 64 * kRouteWaves)
+    counts[(int64_t)e * gridDim.x + blockIdx.x] = count[e];
+}
+
+// Each expert's counts by chunk to the sums before them, and its total.
+__global__ __launch_bounds__(256) void k_scan(int* counts, int* totals, int experts, int chunks) {
+  const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (e >= experts) return;
+  int* c = counts + (int64_t)e * chunks;
+  constexpr int N = kChunks / 64;
+  int v[N], sum = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = lane * N + i < chunks ? c[lane * N + i] : 0;
+    sum += v[i];
+  }
+  int run = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(run, d);
+    if (lane >= d) run += up;
+  }
+  int at = run - sum;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (lane * N + i < chunks) c[lane * N + i] = at;
+    at += v[i];
+  }
+  if (lane == 63) totals[e] = at;
+}
+
+__global__ __launch_bounds__(64 * kPlaceWaves) void k_place(RouteArgs a, int64_t per, const int* counts, const int* totals) {
+  extern __shared__ int count[];
+  __shared__ int start[kMaxExperts + 1], sums[kPlaceWaves];
+  starts<64 * kPlaceWaves>(a.experts, start, sums, [&](int e) { return totals[e]; });
+  const int64_t slots = a.tokens * a.top;
+  if (blockIdx.x == 0)
+    for (int e = threadIdx.x; e <= a.experts; e += 64 * kPlaceWaves) a.offsets[e] = start[e];
+  // rows that no slot takes
+  for (int64_t p = start[a.experts] + (int64_t)blockIdx.x * (64 * kPlaceWaves) + threadIdx.x; p < slots;
+       p += (int64_t)gridDim.x * (64 * kPlaceWaves))
+    a.order[p] = -1;
+  const int64_t s0 = blockIdx.x * per * a.top, s1 = min(slots, s0 + per * a.top);
+  place_slots<kPlaceWaves>(a, s0, s1, count,
+                           [&](int e) { return start[e] + counts[(int64_t)e * gridDim.x + blockIdx.x]; });
+}
+
+// Few tokens: all of it in one workgroup.
+template <class L, int V, bool CHOOSE>
+__global__ __launch_bounds__(512) void k_route_few(RouteArgs a) {
+  extern __shared__ __align__(16) char lds[];
+  double* stages = (double*)lds;
+  int* count = (int*)(lds + (CHOOSE && a.groups > 1 ? (size_t)8 * a.experts * 8 : 0));
+  __shared__ int start[kMaxExperts + 1], sums[8];
+  const int wave = threadIdx.x >> 6;
+  if (CHOOSE) {
+    for (int64_t t = wave; t < a.tokens; t += 8)
+      route_token<L, V>(a, t, a.groups > 1 ? stages + wave * a.experts : nullptr);
+    if (a.order == nullptr) return;
+    __threadfence_block();  // the experts are read by other waves from here on
+  }
+  for (int e = threadIdx.x; e < a.experts; e += 512) count[e] = 0;
+  __syncthreads();
+  const int slots = (int)(a.tokens * a.top);
+  for (int s = threadIdx.x; s < slots; s += 512) {
+    const int e = a.chosen[s];
+    if (taken(e, a.experts)) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  starts<512>(a.experts, start, sums, [&](int e) { return count[e]; });
+  for (int e = threadIdx.x; e <= a.experts; e += 512) a.offsets[e] = start[e];
+  for (int p = start[a.experts] + threadIdx.x; p < slots; p += 512) a.order[p] = -1;
+  place_slots<8>(a, 0, slots, count, [&](int e) { return start[e]; });
+}
+
+// --------------------------------------------------------------- gradient
+// A wave a token.  d = gradient of each score (zeros but for the chosen), then
+// softmax: dl = s (d - sum s d), sigmoid: dl = d s (1 - s).  In 64 bits: with
+// renormalised weights d is a difference that cancels for a single expert.
+template <class L, int V>
+__global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
+  const int lane = threadIdx.x & 63, e0 = lane * V;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += (int64_t)gridDim.x * 4) {
+    double s[V], d[V];
+    scores_of<L, V>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, s);
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = 0.0;
+    // lane j has the j-th choice
+    int e = -1;
+    double dw = 0.0;
+    if (lane < a.top) {
+      e = a.chosen[t * a.top + lane];
+      if (taken(e, a.experts)) dw = (double)a.dweights[t * a.top + lane] * a.scale;
+      else e = -1;
+    }
+    if (a.renormalise) {
+      // d_j = (dw_j - sum dw w / sum w) / sum w, w the chosen scores
+      double w = 0.0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {  // (the lane's choice lies with lane e / V)
+        const double v = __shfl(s[i], e < 0 ? 0 : e / V);
+        if (e >= 0 && e % V == i) w = v;
+      }
+      const double sum = wave_sum(w), dot = wave_sum(dw * w);
+      dw = sum == 0.0 ? 0.0 : (dw - dot / sum) / sum;
+    }
+    for (int j = 0; j < a.top; ++j) {
+      const int ej = __builtin_amdgcn_readlane(e, j);
+      const double dj = lane_value(dw, j);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (ej == e0 + i) d[i] += dj;
+    }
+    double dot = 0.0;
+    if (!a.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) dot += s[i] * d[i];
+      dot = wave_sum(dot);
+    }
+    L* out = (L*)a.dlogits + t * a.ldd;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (e0 + i < a.experts)
+        out[e0 + i] = Elem<L>::from_f32((float)(a.sigmoid ? d[i] * s[i] * (1.0 - s[i]) : s[i] * (d[i] - dot)));
+  }
+}
+
+// f(V) for the neighbours a lane holds of `experts`
+template <class F>
+hipError_t for_experts(int experts, F f) {
+  if (experts <= 64) return f(std::integral_constant<int, 1>());
+  if (experts <= 128) return f(std::integral_constant<int, 2>());
+  if (experts <= 256) return f(std::integral_constant<int, 4>());
+  if (experts <= 512) return f(std::integral_constant<int, 8>());
+  return f(std::integral_constant<int, 16>());
+}
+
+bool few(int64_t tokens, int top) { return tokens <= kFewTokens && tokens * top <= kFewSlots; }
+int chunks_of(int64_t tokens) { return (int)((tokens + chunk_tokens(tokens) - 1) / chunk_tokens(tokens)); }
+
+bool fits(const RouteArgs& a) {
+  return a.tokens > 0 && a.experts >= 1 && a.experts <= kMaxExperts && a.top >= 1 && a.top <= kMaxTop &&
+         a.tokens * a.top <= (int64_t(1) << 30);
+}
+
+template <class L, int V, bool CHOOSE>
+hipError_t route_for(const RouteArgs& a, void* workspace, hipStream_t s) {
+  const bool sort = a.order != nullptr, groups = CHOOSE && a.groups > 1;
+  if (few(a.tokens, a.top)) {
+    const size_t lds = (groups ? (size_t)8 * a.experts * 8 : 0) + (size_t)8 * a.experts * 4;
+    hipLaunchKernelGGL((k_route_few<L, V, CHOOSE>), dim3(1), dim3(512), lds, s, a);
+    return hipGetLastError();
+  }
+  const int64_t per = chunk_tokens(a.tokens);
+  const int chunks = chunks_of(a.tokens);
+  if (sort && workspace == nullptr) return hipErrorInvalidValue;
+  int *counts = sort ? (int*)workspace : nullptr, *totals = counts + (sort ? (size_t)chunks * a.experts : 0);
+  const size_t lds = (groups ? (size_t)kRouteWaves * a.experts * 8 : 0) + (size_t)a.experts * 4;
+  hipLaunchKernelGGL((k_route<L, V, CHOOSE>), dim3(chunks), dim3(64 * kRouteWaves), lds, s, a, per, counts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !sort) return e;
+  hipLaunchKernelGGL(k_scan, dim3((a.experts + 3) / 4), dim3(256), 0, s, counts, totals, a.experts, chunks);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(k_place, dim3(chunks), dim3(64 * kPlaceWaves), (size_t)kPlaceWaves * a.experts * 4, s, a, per,
+                     counts, totals);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t route_workspace(int64_t tokens, int experts, int top) {
+  return few(tokens, top) ? 0 : ((size_t)chunks_of(tokens) + 1) * (size_t)experts * 4;
+}
+
+hipError_t launch_route(const RouteArgs& a, void* workspace, hipStream_t s) {
+  if (!fits(a) || a.top > a.experts || a.groups < 1 || a.groups > kMaxGroups || a.experts % a.groups != 0 ||
+      a.top_groups < 1 || a.top_groups > a.groups || a.top > a.top_groups * (a.experts / a.groups))
+    return hipErrorInvalidValue;
+  return for_experts(a.experts, [&](auto v) {
+    constexpr int V = decltype(v)::value;
+    return a.bf16 ? route_for<bf16_t, V, true>(a, workspace, s) : route_for<float, V, true>(a, workspace, s);
+  });
+}
+
+hipError_t launch_order(const RouteArgs& a, void* workspace, hipStream_t s) {
+  if (!fits(a) || a.order == nullptr) return hipErrorInvalidValue;
+  return route_for<float, 1, false>(a, workspace, s);
+}
+
+hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s) {
+  if (a.tokens <= 0 || a.experts < 1 || a.experts > kMaxExperts || a.top < 1 || a.top > kMaxTop) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)std::min<int64_t>((a.tokens + 3) / 4, 1 << 16));
+  return for_experts(a.experts, [&](auto v) {
+    constexpr int V = decltype(v)::value;
+    if (a.bf16)
+      hipLaunchKernelGGL((k_route_grad<bf16_t, V>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_route_grad<float, V>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace ff

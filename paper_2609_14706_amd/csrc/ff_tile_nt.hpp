@@ -237,10 +237,14 @@ struct Tile {
   template <class Walk>
   static __device__ __forceinline__ void loop(Ring& sm, const Rows& A, const Rows& B, int count, Walk& walk,
                                               Acc& acc) {
+    loop(sm, lane_of(A, B, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), threadIdx.x & 63), count, walk, acc);
+  }
+  // The same for lanes whose rows the caller has placed.
+  template <class Walk>
+  static __device__ __forceinline__ void loop(Ring& sm, const Lane& L, int count, Walk& walk, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (count <= 0) return;
-    const Lane L = lane_of(A, B, wave, lane);
     const FragBase fb = frag_base(wave, lane);
     const char *pa, *pb;
     const int chunk = 16 * L.c;
