@@ -53,7 +53,8 @@ struct RouteGradArgs {
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
 
 // The rows of a routed batch: `rows` = tokens top of them, those from offsets[experts] on
-// in no expert.  What the arrays hold is checked against rows before it is used.
+// in no expert.  What the arrays hold is checked against rows before it is used.  Without
+// offsets all rows are the one expert's (experts 1, top 1): a plain layer.
 struct SlotRows {
   int64_t tokens, rows;
   int experts, top;
@@ -71,22 +72,25 @@ struct ExpertArgs {
   bool gather;
 };
 // How the products are run: `nt` 16-token tiles of the few-token form with `waves` waves a
-// workgroup (rw 16-output tiles), or (nt 0) tiles of 32 ti x 32 tj, `slots` pairs of k in LDS.
+// workgroup, or (nt 0) tiles of 32 ti x 32 tj, `slots` pairs of k in LDS, k in `splits` parts.
 struct ExpertPlan {
-  int nt, rw, waves;
-  int ti, tj, slots;
+  int nt, waves;
+  int ti, tj, slots, splits;
 };
 ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m);
 hipError_t launch_expert_linear(const ExpertArgs& a, const ExpertPlan& p, hipStream_t s);
 
 // out_t = residual_t + sum over the token's slots of weight y (rows of bf16), or the
-// plain sum of fp32 rows (weights null).
+// plain sum of fp32 rows, `parts` of them part_stride elements apart (weights null).  Without place
+// (top 1) token t's row is row t.
 struct CombineArgs {
   SlotRows at;
   int64_t cols;
   const void* y;
   int64_t ldy;
   bool f32;
+  int parts;
+  int64_t part_stride;
   const bf16_t* residual;  // or null
   int64_t ldr;
   bf16_t* out;
@@ -126,39 +130,52 @@ struct RowsArgs {
   int act;
   bf16_t* out;  // or null
   int64_t ldo;
-  uint16_t* laid;         // or null
-  uint16_t* scaled;       // or null
-  const uint32_t* peaks;  // scaled: kPeaks bit patterns, of which the largest counts
-  float peak_factor;      // scaled: the largest value is at most that times the peak
+  uint16_t* laid;    // or null
+  uint16_t* scaled;  // or null
+  const uint32_t* peaks;
+  float peak_factor;  // scaled: the largest value is at most that times the peak
 };
-constexpr int kPeaks = 256;
 inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
-hipError_t launch_rows(const RowsArgs& a, hipStream_t s);
-// peaks: kPeaks bit patterns of the largest finite magnitudes of rows x cols elements.
-hipError_t launch_peaks(const void* src, int64_t ld, int64_t rows, int64_t cols, bool f32, uint32_t* peaks, hipStream_t s);
+// One to three jobs in one launch.
+hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s);
+// peaks: kPeaks bit patterns of largest finite magnitudes among rows x cols elements,
+// zeros where there are none.  Two jobs in one launch.
+constexpr int kPeaks = 1024;
+struct PeaksArgs {
+  const void* src;  // bf16 or fp32
+  int64_t ld, rows, cols;
+  bool f32;
+  uint32_t* peaks;
+};
+hipError_t launch_peaks(const PeaksArgs (&jobs)[2], hipStream_t s);
 
-// dx_p = g_p W_e: g rows of bf16 (16-byte aligned, zeros up to a multiple of 8), W as it lies
-// (experts x m rows of n, 16-byte aligned); out bf16 or fp32, zeros for rows in no expert.
+// Gradients of the products; g rows of bf16, or (f16) of fp16 scaled by its peaks, 16-byte
+// aligned with zeros up to a multiple of 8.
 struct ExpertGradArgs {
   SlotRows at;
   int64_t n, m;
   const uint16_t* g;
   int64_t ldg;
-  const bf16_t* w;  // launch_expert_dx
+  const bf16_t* w;  // launch_expert_dx: experts x m rows of n, 16-byte aligned
   int64_t ldw;
-  const uint16_t* x;  // launch_expert_dw
+  const uint16_t* x;  // launch_expert_dw: by row, as g
   int64_t ldx;
-  void* out;
+  void* out;  // bf16, or fp32 (out_f32, and with splits: parts part_stride elements apart)
   int64_t ldo;
   bool out_f32;
-  bool f16;  // launch_expert_dw: g and x are fp16 scaled by their peaks
+  int64_t part_stride;
+  bf16_t* db;  // launch_expert_dw: column sums of g too; or null
+  bool f16;
   const uint32_t* g_peaks;
   const uint32_t* x_peaks;
   float g_factor, x_factor;
 };
-hipError_t launch_expert_dx(const ExpertGradArgs& a, hipStream_t s);
+// dx_p = g_p W_e, zeros for rows in no expert.
+ExpertPlan expert_dx_plan(int64_t rows, int experts, int64_t n, int64_t m);
+hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s);
 // dW_e = sum over the rows of expert e of g_p^T x_p (m x n; zeros for an expert without rows).
-hipError_t launch_expert_dw(const ExpertGradArgs& a, hipStream_t s);
+ExpertPlan expert_dw_plan(int64_t rows, int experts, int64_t n, int64_t m);
+hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s);
 // db_e = sum over the rows of expert e of g_p (bf16 rows).
 hipError_t launch_expert_db(const SlotRows& at, const bf16_t* g, int64_t ldg, int64_t m, bf16_t* db, hipStream_t s);
 

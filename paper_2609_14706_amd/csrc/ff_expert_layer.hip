@@ -175,37 +175,318 @@ ff_status forward_sizes(const ff_expert_linear_args* a) {
 }
 
 // ------------------------------------------------------------------ gradients
-// Workspace: g and x as the products read them, in bf16 or (x from a checkpoint) in
-// fp16 with their peaks, W packed, and the rows of dx before they are summed for each token.
-struct GradWs {
-  bool lay_g, scale, lay_x, pack_w;
-  size_t off_g, off_g16, off_x, off_peaks, off_w, off_dx, bytes;
+// The gradient of a layer of experts, or (at.offsets null) of one plain layer.
+struct Gradient {
+  SlotRows at;
+  int64_t n, m;
+  bool dy_f32;
+  const void* dy;
+  int64_t lddy;
+  bool gather;  // x and dx: the tokens' rows
+  const void* x;
+  int64_t ldx;
+  ff_q8_rows x_q8;
+  const void* w;
+  int64_t ldw;
+  int act;
+  const void* z;
+  int64_t ldz;
+  ff_q8_rows z_q8;
+  void *g, *dx, *dw, *db;
+  int64_t ldg, lddx, lddw;
 };
-bool has_act(const ff_expert_grad_args* a) { return a->activation != FF_ACT_NONE; }
 
-GradWs grad_ws(const ff_expert_grad_args* a) {
+// Workspace: g and x as the products read them, in bf16 or (x from a checkpoint) in
+// fp16 with their peaks, W with its rows laid out, and fp32 results before they are summed.
+struct GradWs {
+  ExpertPlan dx, dw;
+  bool dy_is_g, lay_g, scale, lay_x, lay_w, sum_dx;
+  size_t off_g, off_g16, off_x, off_peaks, off_w, off_sum, bytes;
+};
+
+GradWs grad_ws(const Gradient& a) {
   GradWs w{};
-  const int64_t T = a->routing.tokens, S = T * a->routing.top, E = a->routing.experts;
-  const bool dx = a->dx != nullptr, dw = a->dw != nullptr;
-  w.scale = dw && a->x_q8.q != nullptr;
-  // g in rows that the tiles take: the caller's, or a copy
-  w.lay_g = (dx || (dw && !w.scale) || a->db != nullptr) && (a->g == nullptr || !tile_rows_ok(a->g, a->ldg, a->m, 2));
-  w.lay_x = dw && !w.scale && (a->by_slot == 0 || !tile_rows_ok(a->x, a->ldx, a->n, 2));
-  w.pack_w = dx && !tile_rows_ok(a->w, a->ldw, a->n, 2);
-  size_t off = 0;
+  const int64_t S = a.at.rows, E = a.at.experts;
+  const bool dx = a.dx != nullptr, dw = a.dw != nullptr;
+  w.scale = dw && a.x_q8.q != nullptr;
+  // g in rows that the tiles take: dy itself, the caller's, or a copy
+  w.dy_is_g = a.act == FF_ACT_NONE && !a.dy_f32 && a.g == nullptr && a.at.offsets == nullptr && tile_rows_ok(a.dy, a.lddy, a.m, 2);
+  w.lay_g = (dx || (dw && !w.scale) || (a.db != nullptr && !dw)) && !w.dy_is_g &&
+            (a.g == nullptr || !tile_rows_ok(a.g, a.ldg, a.m, 2));
+  w.lay_x = dw && !w.scale && (a.gather || !tile_rows_ok(a.x, a.ldx, a.n, 2));
+  w.lay_w = dx && !tile_rows_ok(a.w, a.ldw, a.n, 2);
+  size_t off = 0, sum = 0;
   auto take = [&](bool need, size_t bytes) {
     const size_t at = off;
     if (need) off += up256(bytes);
     return at;
   };
-  w.off_g = take(w.lay_g, (size_t)S * (size_t)laid_ld(a->m) * 2);
-  w.off_g16 = take(w.scale, (size_t)S * (size_t)laid_ld(a->m) * 2);
-  w.off_x = take(w.lay_x || w.scale, (size_t)S * (size_t)laid_ld(a->n) * 2);
+  w.off_g = take(w.lay_g, (size_t)S * (size_t)laid_ld(a.m) * 2);
+  w.off_g16 = take(w.scale, (size_t)S * (size_t)laid_ld(a.m) * 2);
+  w.off_x = take(w.lay_x || w.scale, (size_t)S * (size_t)laid_ld(a.n) * 2);
   w.off_peaks = take(w.scale, 2 * kPeaks * 4);
-  w.off_w = take(w.pack_w, (size_t)E * (size_t)a->m * (size_t)packed_ld(a->n, 2) * 2);
-  w.off_dx = take(dx && a->by_slot == 0, (size_t)S * (size_t)laid_ld(a->n) * 4);
+  w.off_w = take(w.lay_w, (size_t)E * (size_t)a.m * (size_t)laid_ld(a.n) * 2);
+  if (dx) {
+    w.dx = expert_dx_plan(S, (int)E, a.n, a.m);
+    w.sum_dx = a.gather || w.dx.splits > 1;
+    if (w.sum_dx) sum = (size_t)w.dx.splits * (size_t)S * (size_t)laid_ld(a.n) * 4;
+  }
+  if (dw) {
+    w.dw = expert_dw_plan(S, (int)E, a.n, a.m);
+    if (w.dw.splits > 1) sum = std::max(sum, (size_t)w.dw.splits * (size_t)E * (size_t)a.m * (size_t)laid_ld(a.n) * 4);
+  }
+  w.off_sum = take(sum > 0, sum);
   w.bytes = off;
   return w;
+}
+
+// bf16 rows of dst from `parts` sums of fp32 rows.
+ff_status sum_parts(const float* parts, int count, int64_t rows, int64_t cols, void* dst, int64_t ld, hipStream_t s) {
+  CombineArgs c{};
+  c.at.tokens = c.at.rows = rows;
+  c.at.experts = c.at.top = 1;
+  c.cols = cols;
+  c.y = parts;
+  c.ldy = laid_ld(cols);
+  c.f32 = true;
+  c.parts = count;
+  c.part_stride = rows * c.ldy;
+  c.out = (bf16_t*)dst;
+  c.ldo = ld;
+  return hip(launch_combine(c, s), "sums of parts");
+}
+
+ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t s) {
+  ff_status rc;
+  const int64_t S = a.at.rows, E = a.at.experts, T = a.gather ? a.at.tokens : S;
+  const bool act = a.act != FF_ACT_NONE;
+  uint32_t* peaks = (uint32_t*)(ws + w.off_peaks);
+  // slopes of the activations are below 1.13; codes end at 127
+  const float g_factor = act ? 1.13f : 1.0f, x_factor = 127.0f;
+  if (w.scale) {
+    const PeaksArgs jobs[2] = {{a.dy, a.lddy, S, a.m, a.dy_f32, peaks},
+                               {a.x_q8.scale, a.x_q8.ld_scale, T, (a.n + a.x_q8.group - 1) / a.x_q8.group, true, peaks + kPeaks}};
+    if ((rc = hip(launch_peaks(jobs, s), "peaks of dy and x")) != FF_OK) return rc;
+  }
+  RowsArgs jobs[3];
+  int count = 0;
+  RowsArgs r{};
+  r.at = a.at;
+  r.cols = a.m;
+  r.src = a.dy;
+  r.lds = a.lddy;
+  r.src_f32 = a.dy_f32;
+  r.act = a.act;
+  if (act) {
+    r.z = (const bf16_t*)a.z;
+    r.ldz = a.ldz;
+    r.z_q8 = q8_of(a.z_q8);
+  }
+  r.out = (bf16_t*)a.g;
+  r.ldo = a.ldg;
+  if (w.lay_g) r.laid = (uint16_t*)(ws + w.off_g);
+  if (w.scale) {
+    r.scaled = (uint16_t*)(ws + w.off_g16);
+    r.peaks = peaks;
+    r.peak_factor = g_factor;
+  }
+  if (r.out != nullptr || r.laid != nullptr || r.scaled != nullptr) jobs[count++] = r;
+  ExpertGradArgs k{};
+  k.at = a.at;
+  k.n = a.n;
+  k.m = a.m;
+  k.g = w.lay_g ? r.laid : (const uint16_t*)(w.dy_is_g ? a.dy : a.g);
+  k.ldg = w.lay_g ? laid_ld(a.m) : w.dy_is_g ? a.lddy : a.ldg;
+  k.w = (const bf16_t*)a.w;
+  k.ldw = a.ldw;
+  k.x = (const uint16_t*)a.x;
+  k.ldx = a.ldx;
+  if (w.lay_x || w.scale) {
+    RowsArgs x{};
+    x.at = a.at;
+    x.gather = a.gather;
+    x.cols = a.n;
+    x.src = a.x;
+    x.lds = a.ldx;
+    if (w.scale) {
+      x.src_q8 = q8_of(a.x_q8);
+      x.scaled = (uint16_t*)(ws + w.off_x);
+      x.peaks = peaks + kPeaks;
+      x.peak_factor = x_factor;
+    } else {
+      x.laid = (uint16_t*)(ws + w.off_x);
+    }
+    jobs[count++] = x;
+    k.x = (const uint16_t*)(ws + w.off_x);
+    k.ldx = laid_ld(a.n);
+  }
+  if (w.lay_w) {
+    RowsArgs p{};
+    p.at.tokens = p.at.rows = E * a.m;
+    p.at.experts = p.at.top = 1;
+    p.cols = a.n;
+    p.src = a.w;
+    p.lds = a.ldw;
+    p.laid = (uint16_t*)(ws + w.off_w);
+    jobs[count++] = p;
+    k.w = (const bf16_t*)(ws + w.off_w);
+    k.ldw = laid_ld(a.n);
+  }
+  if (count > 0 && (rc = hip(launch_rows(jobs, count, s), "operands of the gradient")) != FF_OK) return rc;
+  if (a.db != nullptr && a.dw == nullptr &&
+      (rc = hip(launch_expert_db(k.at, k.g, k.ldg, a.m, (bf16_t*)a.db, s), "bias gradient")) != FF_OK)
+    return rc;
+  if (a.dx != nullptr) {
+    float* sum = (float*)(ws + w.off_sum);
+    k.out_f32 = w.sum_dx;
+    k.out = w.sum_dx ? (void*)sum : a.dx;
+    k.ldo = w.sum_dx ? laid_ld(a.n) : a.lddx;
+    k.part_stride = S * k.ldo;
+    if ((rc = hip(launch_expert_dx(k, w.dx, s), "input gradient")) != FF_OK) return rc;
+    if (a.gather) {
+      // a token's rows in fp32 until they are summed: a rounding of each would add to g's and dx's own
+      CombineArgs c{};
+      c.at = k.at;
+      c.at.weights = nullptr;
+      c.cols = a.n;
+      c.y = sum;
+      c.ldy = k.ldo;
+      c.f32 = true;
+      c.parts = w.dx.splits;
+      c.part_stride = k.part_stride;
+      c.out = (bf16_t*)a.dx;
+      c.ldo = a.lddx;
+      if ((rc = hip(launch_combine(c, s), "input gradient's sums")) != FF_OK) return rc;
+    } else if (w.sum_dx && (rc = sum_parts(sum, w.dx.splits, S, a.n, a.dx, a.lddx, s)) != FF_OK) {
+      return rc;
+    }
+  }
+  if (a.dw == nullptr) return FF_OK;
+  if (w.scale) {
+    k.f16 = true;
+    k.g = (const uint16_t*)(ws + w.off_g16);
+    k.ldg = laid_ld(a.m);
+    k.g_peaks = peaks;
+    k.g_factor = g_factor;
+    k.x_peaks = peaks + kPeaks;
+    k.x_factor = x_factor;
+  }
+  float* sum = (float*)(ws + w.off_sum);
+  k.out_f32 = w.dw.splits > 1;
+  k.out = k.out_f32 ? (void*)sum : a.dw;
+  k.ldo = k.out_f32 ? laid_ld(a.n) : a.lddw;
+  k.part_stride = E * a.m * k.ldo;
+  k.db = (bf16_t*)a.db;
+  if ((rc = hip(launch_expert_dw(k, w.dw, s), "weight gradient")) != FF_OK) return rc;
+  return k.out_f32 ? sum_parts(sum, w.dw.splits, E * a.m, a.n, a.dw, a.lddw, s) : FF_OK;
+}
+
+// What the layers' gradients check alike (rows of dy: S, of x and dx: X).
+ff_status gradient_ok(const Gradient& a, int64_t S, int64_t X, std::initializer_list<Block> more) {
+  const int64_t E = a.at.experts;
+  const bool act = a.act != FF_ACT_NONE, x8 = a.x_q8.q != nullptr, z8 = a.z_q8.q != nullptr && act;
+  if ((x8 && a.x != nullptr) || (a.z_q8.q != nullptr && a.z != nullptr))
+    return bad("give x and preact either in bf16 or as a checkpoint");
+  if ((x8 && !q8_ok(a.x_q8, a.n)) || (z8 && !q8_ok(a.z_q8, a.m))) return bad(kBadQ8);
+  const int64_t e = a.dy_f32 ? 4 : 2;
+  if (!rows_ok(a.dy, a.lddy, a.m, e) || (act && !z8 && !rows_ok(a.z, a.ldz, a.m, 2)) ||
+      (a.g != nullptr && !rows_ok(a.g, a.ldg, a.m, 2)))
+    return bad("dy, g and (with an activation) preact must be aligned device pointers to rows of m elements, ld >= m");
+  if ((a.dw != nullptr && !x8 && !rows_ok(a.x, a.ldx, a.n, 2)) || (a.dx != nullptr && !rows_ok(a.w, a.ldw, a.n, 2)) ||
+      (a.dx != nullptr && !rows_ok(a.dx, a.lddx, a.n, 2)))
+    return bad("x (for dw), w and dx must be aligned device pointers to rows of n elements, ld >= n");
+  auto scales = [&](bool there, const ff_q8_rows& c, int64_t rows, int64_t cols) {
+    return there ? Block{c.scale, rows, c.ld_scale * 4, (cols + c.group - 1) / c.group * 4} : Block{nullptr, 0, 0, 0};
+  };
+  const std::initializer_list<Block> outs = {{a.g, a.g != nullptr ? S : 0, a.ldg * 2, a.m * 2},
+                                             {a.dx, a.dx != nullptr ? X : 0, a.lddx * 2, a.n * 2},
+                                             {a.dw, a.dw != nullptr ? E * a.m : 0, a.lddw * 2, a.n * 2},
+                                             flat(a.db, E * a.m * 2)};
+  if (clash(outs, {{a.dy, S, a.lddy * e, a.m * e},
+                   {a.x, a.x != nullptr ? X : 0, a.ldx * 2, a.n * 2},
+                   {a.w, a.w != nullptr ? E * a.m : 0, a.ldw * 2, a.n * 2},
+                   {a.z, act && !z8 ? S : 0, a.ldz * 2, a.m * 2},
+                   {a.x_q8.q, x8 ? X : 0, a.x_q8.ldq, a.n},
+                   {a.z_q8.q, z8 ? S : 0, a.z_q8.ldq, a.m},
+                   scales(x8, a.x_q8, X, a.n),
+                   scales(z8, a.z_q8, S, a.m)}) ||
+      clash(outs, more))
+    return bad("gradients must not overlap the inputs or each other");
+  return FF_OK;
+}
+
+// With no tokens.
+ff_status zero_gradient(const Gradient& a, hipStream_t s) {
+  const int64_t E = a.at.experts;
+  ff_status rc = FF_OK;
+  if (a.dw != nullptr) rc = hip(launch_zero(a.dw, a.lddw, E * a.m, a.n, 2, s), "zero gradient");
+  if (rc == FF_OK && a.db != nullptr) rc = hip(launch_zero(a.db, E * a.m, 1, E * a.m, 2, s), "zero gradient");
+  return rc;
+}
+
+Gradient gradient_of(const ff_expert_grad_args* a) {
+  Gradient k{};
+  k.at = slot_rows(a->routing);
+  k.n = a->n;
+  k.m = a->m;
+  k.dy_f32 = a->dy_dtype == FF_F32;
+  k.dy = a->dy;
+  k.lddy = a->lddy;
+  k.gather = a->by_slot == 0;
+  k.x = a->x;
+  k.ldx = a->ldx;
+  k.x_q8 = a->x_q8;
+  k.w = a->w;
+  k.ldw = a->ldw;
+  k.act = a->activation;
+  k.z = a->preact;
+  k.ldz = a->ldz;
+  k.z_q8 = a->preact_q8;
+  k.g = a->g;
+  k.ldg = a->ldg;
+  k.dx = a->dx;
+  k.lddx = a->lddx;
+  k.dw = a->dw;
+  k.lddw = a->lddw;
+  k.db = a->db;
+  return k;
+}
+// A plain layer: all rows are one expert's.
+Gradient gradient_of(const ff_linear_grad_q8_args* a) {
+  const ff_linear_grad_args& b = a->grad;
+  Gradient k{};
+  k.at.tokens = k.at.rows = b.tokens;
+  k.at.experts = k.at.top = 1;
+  k.n = b.n;
+  k.m = b.m;
+  k.dy = b.dy;
+  k.lddy = b.lddy;
+  k.x = b.x;
+  k.ldx = b.ldx;
+  k.x_q8 = a->x_q8;
+  k.w = b.w;
+  k.ldw = b.ldw;
+  k.act = b.activation;
+  k.z = b.preact;
+  k.ldz = b.ldz;
+  k.z_q8 = a->preact_q8;
+  k.g = b.g;
+  k.ldg = b.ldg;
+  k.dx = b.dx;
+  k.lddx = b.lddx;
+  k.dw = b.dw;
+  k.lddw = b.lddw;
+  k.db = b.db;
+  return k;
+}
+
+ff_status plain_sizes(const ff_linear_grad_q8_args* a) {
+  if (a == nullptr) return bad("args is NULL");
+  if (a->grad.tokens < 0 || a->grad.tokens > (int64_t(1) << 21)) return bad("tokens must be 0 .. 2^21");
+  ff_status rc = sizes_ok(a->grad.n, a->grad.m);
+  if (rc != FF_OK) return rc;
+  if (a->grad.activation < FF_ACT_NONE || a->grad.activation > FF_ACT_SILU) return bad("unknown activation");
+  return FF_OK;
 }
 
 ff_status grad_sizes(const ff_expert_grad_args* a) {
@@ -323,7 +604,7 @@ ff_status ff_expert_linear(const ff_expert_linear_args* a) {
     r.src = a->x;
     r.lds = a->ldx;
     r.laid = (uint16_t*)ws;
-    if ((rc = hip(launch_rows(r, s), "rows of x")) != FF_OK) return rc;
+    if ((rc = hip(launch_rows(&r, 1, s), "rows of x")) != FF_OK) return rc;
     k.lin.x = ws;
     k.lin.ldx = laid_ld(a->n);
   }
@@ -396,7 +677,7 @@ ff_status ff_expert_linear_backward_workspace_size(const ff_expert_grad_args* a,
   if (bytes == nullptr) return bad("bytes is NULL");
   ff_status rc = grad_sizes(a);
   if (rc != FF_OK) return rc;
-  *bytes = a->routing.tokens == 0 ? 0 : grad_ws(a).bytes;
+  *bytes = a->routing.tokens == 0 ? 0 : grad_ws(gradient_of(a)).bytes;
   return FF_OK;
 }
 
@@ -404,140 +685,39 @@ ff_status ff_expert_linear_backward(const ff_expert_grad_args* a) {
   ff_status rc = grad_sizes(a);
   if (rc != FF_OK) return rc;
   const hipStream_t s = (hipStream_t)a->stream;
-  const int64_t T = a->routing.tokens, S = T * a->routing.top, E = a->routing.experts, X = a->by_slot ? S : T;
-  if ((uintptr_t)a->db % 2 != 0) return bad("db is misaligned");
-  if (a->dw != nullptr && !rows_ok(a->dw, a->lddw, a->n, 2)) return bad("dw must be an aligned device pointer to rows of n elements, ld >= n");
-  if (T == 0) {
-    if (a->dw != nullptr && (rc = hip(launch_zero(a->dw, a->lddw, E * a->m, a->n, 2, s), "zero gradient")) != FF_OK) return rc;
-    if (a->db != nullptr) return hip(launch_zero(a->db, E * a->m, 1, E * a->m, 2, s), "zero gradient");
-    return FF_OK;
-  }
-  if ((rc = routing_ok(a->routing, kOrder | kOffsets | (a->by_slot ? 0 : kPlace))) != FF_OK) return rc;
-  const bool act = has_act(a), x8 = a->x_q8.q != nullptr, z8 = a->preact_q8.q != nullptr && act, f32 = a->dy_dtype == FF_F32;
-  if ((x8 && a->x != nullptr) || (a->preact_q8.q != nullptr && a->preact != nullptr))
-    return bad("give x and preact either in bf16 or as a checkpoint");
-  if ((x8 && !q8_ok(a->x_q8, a->n)) || (z8 && !q8_ok(a->preact_q8, a->m))) return bad(kBadQ8);
-  const int64_t db = f32 ? 4 : 2;
-  if (!rows_ok(a->dy, a->lddy, a->m, db) || (act && !z8 && !rows_ok(a->preact, a->ldz, a->m, 2)) ||
-      (a->g != nullptr && !rows_ok(a->g, a->ldg, a->m, 2)))
-    return bad("dy, g and (with an activation) preact must be aligned device pointers to rows of m elements, ld >= m");
-  if ((a->dw != nullptr && !x8 && !rows_ok(a->x, a->ldx, a->n, 2)) || (a->dx != nullptr && !rows_ok(a->w, a->ldw, a->n, 2)) ||
-      (a->dx != nullptr && !rows_ok(a->dx, a->lddx, a->n, 2)))
-    return bad("x (for dw), w and dx must be aligned device pointers to rows of n elements, ld >= n");
-  auto scales = [&](bool there, const ff_q8_rows& c, int64_t rows, int64_t cols) {
-    return there ? Block{c.scale, rows, c.ld_scale * 4, (cols + c.group - 1) / c.group * 4} : Block{nullptr, 0, 0, 0};
-  };
-  if (clash({{a->g, a->g != nullptr ? S : 0, a->ldg * 2, a->m * 2}, {a->dx, a->dx != nullptr ? X : 0, a->lddx * 2, a->n * 2},
-             {a->dw, a->dw != nullptr ? E * a->m : 0, a->lddw * 2, a->n * 2}, flat(a->db, E * a->m * 2)},
-            {{a->dy, S, a->lddy * db, a->m * db},
-             {a->x, a->x != nullptr ? X : 0, a->ldx * 2, a->n * 2},
-             {a->w, a->w != nullptr ? E * a->m : 0, a->ldw * 2, a->n * 2},
-             {a->preact, act && !z8 ? S : 0, a->ldz * 2, a->m * 2},
-             {a->x_q8.q, x8 ? X : 0, a->x_q8.ldq, a->n},
-             {a->preact_q8.q, z8 ? S : 0, a->preact_q8.ldq, a->m},
-             scales(x8, a->x_q8, X, a->n), scales(z8, a->preact_q8, S, a->m),
-             block_of(a->routing, kOrder), block_of(a->routing, kOffsets), block_of(a->routing, kPlace)}))
-    return bad("gradients must not overlap the inputs or each other");
-  const GradWs w = grad_ws(a);
+  const Gradient k = gradient_of(a);
+  if ((uintptr_t)k.db % 2 != 0) return bad("db is misaligned");
+  if (k.dw != nullptr && !rows_ok(k.dw, k.lddw, k.n, 2)) return bad("dw must be an aligned device pointer to rows of n elements, ld >= n");
+  if (k.at.tokens == 0) return zero_gradient(k, s);
+  if ((rc = routing_ok(a->routing, kOrder | kOffsets | (k.gather ? kPlace : 0))) != FF_OK) return rc;
+  rc = gradient_ok(k, k.at.rows, k.gather ? k.at.tokens : k.at.rows,
+                   {block_of(a->routing, kOrder), block_of(a->routing, kOffsets), block_of(a->routing, kPlace)});
+  if (rc != FF_OK) return rc;
+  const GradWs w = grad_ws(k);
   if ((rc = workspace_ok(a->workspace, a->workspace_bytes, w.bytes)) != FF_OK) return rc;
-  char* ws = (char*)a->workspace;
-  uint32_t* peaks = (uint32_t*)(ws + w.off_peaks);
-  // slopes of the activations are below 1.13
-  const float g_factor = act ? 1.13f : 1.0f, x_factor = 127.0f;
-  if (w.scale) {
-    if ((rc = hip(launch_peaks(a->dy, a->lddy, S, a->m, f32, peaks, s), "peaks of dy")) != FF_OK) return rc;
-    const int64_t groups = (a->n + a->x_q8.group - 1) / a->x_q8.group;
-    if ((rc = hip(launch_peaks(a->x_q8.scale, a->x_q8.ld_scale, X, groups, true, peaks + kPeaks, s), "peaks of x")) != FF_OK) return rc;
-  }
-  RowsArgs r{};
-  r.at = slot_rows(a->routing);
-  r.cols = a->m;
-  r.src = a->dy;
-  r.lds = a->lddy;
-  r.src_f32 = f32;
-  r.z = act && !z8 ? (const bf16_t*)a->preact : nullptr;
-  r.ldz = a->ldz;
-  if (z8) r.z_q8 = q8_of(a->preact_q8);
-  r.act = a->activation;
-  r.out = (bf16_t*)a->g;
-  r.ldo = a->ldg;
-  if (w.lay_g) r.laid = (uint16_t*)(ws + w.off_g);
-  if (w.scale) {
-    r.scaled = (uint16_t*)(ws + w.off_g16);
-    r.peaks = peaks;
-    r.peak_factor = g_factor;
-  }
-  if (r.out != nullptr || r.laid != nullptr || r.scaled != nullptr)
-    if ((rc = hip(launch_rows(r, s), "rows of g")) != FF_OK) return rc;
-  ExpertGradArgs k{};
-  k.at = r.at;
-  k.n = a->n;
-  k.m = a->m;
-  k.g = w.lay_g ? r.laid : (const uint16_t*)a->g;
-  k.ldg = w.lay_g ? laid_ld(a->m) : a->ldg;
-  if (a->db != nullptr &&
-      (rc = hip(launch_expert_db(k.at, k.g, k.ldg, a->m, (bf16_t*)a->db, s), "bias gradient")) != FF_OK)
-    return rc;
-  if (a->dx != nullptr) {
-    k.w = (const bf16_t*)a->w;
-    k.ldw = a->ldw;
-    if (w.pack_w) {
-      if ((rc = hip(launch_pack_rows(a->w, a->ldw, E * a->m, a->n, 2, ws + w.off_w, s), "packing W")) != FF_OK) return rc;
-      k.w = (const bf16_t*)(ws + w.off_w);
-      k.ldw = packed_ld(a->n, 2);
-    }
-    k.out_f32 = a->by_slot == 0;
-    k.out = k.out_f32 ? (void*)(ws + w.off_dx) : a->dx;
-    k.ldo = k.out_f32 ? laid_ld(a->n) : a->lddx;
-    if ((rc = hip(launch_expert_dx(k, s), "input gradient")) != FF_OK) return rc;
-    if (k.out_f32) {
-      // a token's rows in fp32 until they are summed: a rounding of each would add to g's and dx's own
-      CombineArgs c{};
-      c.at = k.at;
-      c.at.weights = nullptr;
-      c.cols = a->n;
-      c.y = k.out;
-      c.ldy = k.ldo;
-      c.f32 = true;
-      c.out = (bf16_t*)a->dx;
-      c.ldo = a->lddx;
-      if ((rc = hip(launch_combine(c, s), "input gradient's sums")) != FF_OK) return rc;
-    }
-  }
-  if (a->dw == nullptr) return FF_OK;
-  k.x = (const uint16_t*)a->x;
-  k.ldx = a->ldx;
-  if (w.lay_x || w.scale) {
-    RowsArgs x{};
-    x.at = r.at;
-    x.gather = a->by_slot == 0;
-    x.cols = a->n;
-    x.src = a->x;
-    x.lds = a->ldx;
-    if (w.scale) {
-      x.src_q8 = q8_of(a->x_q8);
-      x.scaled = (uint16_t*)(ws + w.off_x);
-      x.peaks = peaks + kPeaks;
-      x.peak_factor = x_factor;
-    } else {
-      x.laid = (uint16_t*)(ws + w.off_x);
-    }
-    if ((rc = hip(launch_rows(x, s), "rows of x")) != FF_OK) return rc;
-    k.x = (const uint16_t*)(ws + w.off_x);
-    k.ldx = laid_ld(a->n);
-  }
-  if (w.scale) {
-    k.f16 = true;
-    k.g = (const uint16_t*)(ws + w.off_g16);
-    k.ldg = laid_ld(a->m);
-    k.g_peaks = peaks;
-    k.g_factor = g_factor;
-    k.x_peaks = peaks + kPeaks;
-    k.x_factor = x_factor;
-  }
-  k.out = a->dw;
-  k.ldo = a->lddw;
-  return hip(launch_expert_dw(k, s), "weight gradient");
+  return run_gradient(k, w, (char*)a->workspace, s);
+}
+
+ff_status ff_linear_backward_q8_workspace_size(const ff_linear_grad_q8_args* a, size_t* bytes) {
+  if (bytes == nullptr) return bad("bytes is NULL");
+  ff_status rc = plain_sizes(a);
+  if (rc != FF_OK) return rc;
+  *bytes = a->grad.tokens == 0 ? 0 : grad_ws(gradient_of(a)).bytes;
+  return FF_OK;
+}
+
+ff_status ff_linear_backward_q8(const ff_linear_grad_q8_args* a) {
+  ff_status rc = plain_sizes(a);
+  if (rc != FF_OK) return rc;
+  const hipStream_t s = (hipStream_t)a->grad.stream;
+  Gradient k = gradient_of(a);
+  if ((uintptr_t)k.db % 2 != 0) return bad("db is misaligned");
+  if (k.dw != nullptr && !rows_ok(k.dw, k.lddw, k.n, 2)) return bad("dw must be an aligned device pointer to rows of n elements, ld >= n");
+  if (k.at.tokens == 0) return zero_gradient(k, s);
+  if ((rc = gradient_ok(k, k.at.rows, k.at.rows, {})) != FF_OK) return rc;
+  const GradWs w = grad_ws(k);
+  if ((rc = workspace_ok(a->grad.workspace, a->grad.workspace_bytes, w.bytes)) != FF_OK) return rc;
+  return run_gradient(k, w, (char*)a->grad.workspace, s);
 }
 
 }  // extern "C"

@@ -190,132 +190,6 @@ ff_status grad_checks(const ff_linear_grad_args* a) {
   return FF_OK;
 }
 
-// xq, zq: checkpoints that stand for x and preact (q null: none).
-ff_status linear_backward_call(const ff_linear_grad_args* a, const ff_q8_rows& xq, const ff_q8_rows& zq) {
-  ff_status rc = grad_checks(a);
-  if (rc != FF_OK) return rc;
-  const hipStream_t s = (hipStream_t)a->stream;
-  if ((uintptr_t)a->db % 2 != 0) return bad("db is misaligned");
-  if (a->dw != nullptr && !rows_ok(a->dw, a->lddw, a->n, 2)) return bad("dw must be an aligned device pointer to rows of n elements, ld >= n");
-  if (a->tokens == 0) {
-    if (a->dw != nullptr && (rc = hip(launch_zero(a->dw, a->lddw, a->m, a->n, 2, s), "zero gradient")) != FF_OK) return rc;
-    if (a->db != nullptr) return hip(launch_zero(a->db, a->m, 1, a->m, 2, s), "zero gradient");
-    return FF_OK;
-  }
-  const bool x8 = xq.q != nullptr, z8 = zq.q != nullptr && has_act(a);
-  if ((x8 && !q8_ok(xq, a->n)) || (z8 && !q8_ok(zq, a->m))) return bad(kBadQ8);
-  if (!rows_ok(a->dy, a->lddy, a->m, 2) || (has_act(a) && !z8 && !rows_ok(a->preact, a->ldz, a->m, 2)) ||
-      (a->g != nullptr && !rows_ok(a->g, a->ldg, a->m, 2)))
-    return bad("dy, g and (with an activation) preact must be aligned device pointers to rows of m elements, ld >= m");
-  if ((a->dw != nullptr && !x8 && !rows_ok(a->x, a->ldx, a->n, 2)) || (a->dx != nullptr && !rows_ok(a->w, a->ldw, a->n, 2)) ||
-      (a->dx != nullptr && !rows_ok(a->dx, a->lddx, a->n, 2)))
-    return bad("x (for dw), w and dx must be aligned device pointers to rows of n elements, ld >= n");
-  const int64_t T = a->tokens, n2 = a->n * 2, m2 = a->m * 2;
-  struct Block {
-    const void* p;
-    int64_t rows, stride, len;
-  };
-  auto scales = [&](const ff_q8_rows& c, int64_t cols) {
-    return Block{c.scale, T, c.ld_scale * 4, (cols + c.group - 1) / c.group * 4};
-  };
-  const Block none{nullptr, 0, 0, 0};
-  const Block ins[8] = {{a->dy, T, a->lddy * 2, m2},
-                        x8 ? none : Block{a->x, T, a->ldx * 2, n2},
-                        {a->w, a->m, a->ldw * 2, n2},
-                        has_act(a) && !z8 ? Block{a->preact, T, a->ldz * 2, m2} : none,
-                        x8 ? Block{xq.q, T, xq.ldq, a->n} : none,
-                        z8 ? Block{zq.q, T, zq.ldq, a->m} : none,
-                        x8 ? scales(xq, a->n) : none,
-                        z8 ? scales(zq, a->m) : none};
-  const Block outs[4] = {{a->g, T, a->ldg * 2, m2}, {a->dx, T, a->lddx * 2, n2}, {a->dw, a->m, a->lddw * 2, n2},
-                         {a->db, a->db != nullptr ? 1 : 0, m2, m2}};
-  for (int i = 0; i < 4; ++i) {
-    for (const Block& in : ins)
-      if (meet(outs[i].p, outs[i].rows, outs[i].stride, outs[i].len, in.p, in.rows, in.stride, in.len))
-        return bad("gradients must not overlap the inputs");
-    for (int j = 0; j < i; ++j)
-      if (meet(outs[i].p, outs[i].rows, outs[i].stride, outs[i].len, outs[j].p, outs[j].rows, outs[j].stride, outs[j].len))
-        return bad("gradients must not overlap each other");
-  }
-  const GradWs w = grad_ws(a);
-  if ((rc = workspace_ok(a->workspace, a->workspace_bytes, w.bytes)) != FF_OK) return rc;
-  char* ws = (char*)a->workspace;
-  ActGradArgs k{};
-  k.rows = T;
-  k.cols = a->m;
-  k.dy = (const bf16_t*)a->dy;
-  k.lddy = a->lddy;
-  k.z = has_act(a) && !z8 ? (const bf16_t*)a->preact : nullptr;
-  k.ldz = a->ldz;
-  if (z8) k.zq = q8_of(zq);
-  k.act = a->activation;
-  const bf16_t* g = k.dy;  // by rows
-  int64_t ldg = a->lddy;
-  if (a->g != nullptr) {
-    k.g = (bf16_t*)a->g;
-    k.ldg = a->ldg;
-  } else if (w.own_g) {
-    k.g = (bf16_t*)(ws + w.off_g);
-    k.ldg = w.ldm;
-  }
-  if (k.g != nullptr) {
-    g = k.g;
-    ldg = k.ldg;
-  }
-  k.gt = a->dw != nullptr ? (bf16_t*)(ws + w.off_gt) : nullptr;
-  k.ldgt = w.ldt;
-  k.part = a->db != nullptr ? (float*)(ws + w.off_part) : nullptr;
-  // one launch for what the products read: g by rows and columns, W^T and x^T
-  ActGradArgs jobs[3];
-  int count = 0;
-  if (k.g != nullptr || k.gt != nullptr || k.part != nullptr) jobs[count++] = k;
-  auto turn = [&](const void* src, int64_t ld, int64_t rows, int64_t cols, size_t off, int64_t ldt) {
-    ActGradArgs j{};
-    j.rows = rows;
-    j.cols = cols;
-    j.dy = (const bf16_t*)src;
-    j.lddy = ld;
-    j.gt = (bf16_t*)(ws + off);
-    j.ldgt = ldt;
-    jobs[count++] = j;
-    return j.gt;
-  };
-  const bf16_t* wt = a->dx != nullptr ? turn(a->w, a->ldw, a->m, a->n, w.off_wt, w.ldm) : nullptr;
-  const bf16_t* xt = a->dw != nullptr ? turn(a->x, a->ldx, T, a->n, w.off_xt, w.ldt) : nullptr;
-  if (xt != nullptr && x8) jobs[count - 1].dyq = q8_of(xq);
-  if (count > 0 && (rc = hip(launch_act_grad(jobs, count, s), "operands of the gradient")) != FF_OK) return rc;
-  if (a->db != nullptr &&
-      (rc = hip(launch_col_sums(k.part, act_grad_parts(T), a->m, a->db, true, s), "bias gradient")) != FF_OK)
-    return rc;
-  if (a->dx != nullptr) {
-    LinearArgs p{};
-    p.tokens = T;
-    p.n = a->m;
-    p.m = a->n;
-    p.x = g;
-    p.ldx = ldg;
-    p.w = wt;
-    p.ldw = w.ldm;
-    p.y = (bf16_t*)a->dx;
-    p.ldy = a->lddx;
-    if ((rc = run_linear(p, 2, ws + w.off_lin, s, true)) != FF_OK) return rc;
-  }
-  if (a->dw != nullptr) {
-    LinearArgs p{};
-    p.tokens = a->m;
-    p.n = w.ldt;  // (zeros beyond the tokens)
-    p.m = a->n;
-    p.x = k.gt;
-    p.ldx = w.ldt;
-    p.w = xt;
-    p.ldw = w.ldt;
-    p.y = (bf16_t*)a->dw;
-    p.ldy = a->lddw;
-    if ((rc = run_linear(p, 2, ws + w.off_lin, s)) != FF_OK) return rc;
-  }
-  return FF_OK;
-}
-
 ff_status checkpoint_call(const ff_checkpoint_args* a, bool restore) {
   if (a == nullptr) return bad("args is NULL");
   if (a->rows < 0 || a->rows > (int64_t(1) << 32) || a->cols < 1 || a->cols > kMaxCols)
@@ -468,14 +342,114 @@ ff_status ff_linear_backward_workspace_size(const ff_linear_grad_args* a, size_t
 }
 
 ff_status ff_linear_backward(const ff_linear_grad_args* a) {
-  return linear_backward_call(a, ff_q8_rows{}, ff_q8_rows{});
-}
-
-ff_status ff_linear_backward_q8(const ff_linear_grad_q8_args* a) {
-  if (a == nullptr) return bad("args is NULL");
-  if ((a->x_q8.q != nullptr && a->grad.x != nullptr) || (a->preact_q8.q != nullptr && a->grad.preact != nullptr))
-    return bad("give x and preact either in bf16 or as a checkpoint");
-  return linear_backward_call(&a->grad, a->x_q8, a->preact_q8);
+  ff_status rc = grad_checks(a);
+  if (rc != FF_OK) return rc;
+  const hipStream_t s = (hipStream_t)a->stream;
+  if ((uintptr_t)a->db % 2 != 0) return bad("db is misaligned");
+  if (a->dw != nullptr && !rows_ok(a->dw, a->lddw, a->n, 2)) return bad("dw must be an aligned device pointer to rows of n elements, ld >= n");
+  if (a->tokens == 0) {
+    if (a->dw != nullptr && (rc = hip(launch_zero(a->dw, a->lddw, a->m, a->n, 2, s), "zero gradient")) != FF_OK) return rc;
+    if (a->db != nullptr) return hip(launch_zero(a->db, a->m, 1, a->m, 2, s), "zero gradient");
+    return FF_OK;
+  }
+  if (!rows_ok(a->dy, a->lddy, a->m, 2) || (has_act(a) && !rows_ok(a->preact, a->ldz, a->m, 2)) ||
+      (a->g != nullptr && !rows_ok(a->g, a->ldg, a->m, 2)))
+    return bad("dy, g and (with an activation) preact must be aligned device pointers to rows of m elements, ld >= m");
+  if ((a->dw != nullptr && !rows_ok(a->x, a->ldx, a->n, 2)) || (a->dx != nullptr && !rows_ok(a->w, a->ldw, a->n, 2)) ||
+      (a->dx != nullptr && !rows_ok(a->dx, a->lddx, a->n, 2)))
+    return bad("x (for dw), w and dx must be aligned device pointers to rows of n elements, ld >= n");
+  const int64_t T = a->tokens, n2 = a->n * 2, m2 = a->m * 2;
+  struct Block {
+    const void* p;
+    int64_t rows, stride, len;
+  };
+  const Block ins[4] = {{a->dy, T, a->lddy * 2, m2}, {a->x, T, a->ldx * 2, n2}, {a->w, a->m, a->ldw * 2, n2},
+                        {has_act(a) ? a->preact : nullptr, T, a->ldz * 2, m2}};
+  const Block outs[4] = {{a->g, T, a->ldg * 2, m2}, {a->dx, T, a->lddx * 2, n2}, {a->dw, a->m, a->lddw * 2, n2},
+                         {a->db, a->db != nullptr ? 1 : 0, m2, m2}};
+  for (int i = 0; i < 4; ++i) {
+    for (const Block& in : ins)
+      if (meet(outs[i].p, outs[i].rows, outs[i].stride, outs[i].len, in.p, in.rows, in.stride, in.len))
+        return bad("gradients must not overlap the inputs");
+    for (int j = 0; j < i; ++j)
+      if (meet(outs[i].p, outs[i].rows, outs[i].stride, outs[i].len, outs[j].p, outs[j].rows, outs[j].stride, outs[j].len))
+        return bad("gradients must not overlap each other");
+  }
+  const GradWs w = grad_ws(a);
+  if ((rc = workspace_ok(a->workspace, a->workspace_bytes, w.bytes)) != FF_OK) return rc;
+  char* ws = (char*)a->workspace;
+  ActGradArgs k{};
+  k.rows = T;
+  k.cols = a->m;
+  k.dy = (const bf16_t*)a->dy;
+  k.lddy = a->lddy;
+  k.z = has_act(a) ? (const bf16_t*)a->preact : nullptr;
+  k.ldz = a->ldz;
+  k.act = a->activation;
+  const bf16_t* g = k.dy;  // by rows
+  int64_t ldg = a->lddy;
+  if (a->g != nullptr) {
+    k.g = (bf16_t*)a->g;
+    k.ldg = a->ldg;
+  } else if (w.own_g) {
+    k.g = (bf16_t*)(ws + w.off_g);
+    k.ldg = w.ldm;
+  }
+  if (k.g != nullptr) {
+    g = k.g;
+    ldg = k.ldg;
+  }
+  k.gt = a->dw != nullptr ? (bf16_t*)(ws + w.off_gt) : nullptr;
+  k.ldgt = w.ldt;
+  k.part = a->db != nullptr ? (float*)(ws + w.off_part) : nullptr;
+  // one launch for what the products read: g by rows and columns, W^T and x^T
+  ActGradArgs jobs[3];
+  int count = 0;
+  if (k.g != nullptr || k.gt != nullptr || k.part != nullptr) jobs[count++] = k;
+  auto turn = [&](const void* src, int64_t ld, int64_t rows, int64_t cols, size_t off, int64_t ldt) {
+    ActGradArgs j{};
+    j.rows = rows;
+    j.cols = cols;
+    j.dy = (const bf16_t*)src;
+    j.lddy = ld;
+    j.gt = (bf16_t*)(ws + off);
+    j.ldgt = ldt;
+    jobs[count++] = j;
+    return j.gt;
+  };
+  const bf16_t* wt = a->dx != nullptr ? turn(a->w, a->ldw, a->m, a->n, w.off_wt, w.ldm) : nullptr;
+  const bf16_t* xt = a->dw != nullptr ? turn(a->x, a->ldx, T, a->n, w.off_xt, w.ldt) : nullptr;
+  if (count > 0 && (rc = hip(launch_act_grad(jobs, count, s), "operands of the gradient")) != FF_OK) return rc;
+  if (a->db != nullptr &&
+      (rc = hip(launch_col_sums(k.part, act_grad_parts(T), a->m, a->db, true, s), "bias gradient")) != FF_OK)
+    return rc;
+  if (a->dx != nullptr) {
+    LinearArgs p{};
+    p.tokens = T;
+    p.n = a->m;
+    p.m = a->n;
+    p.x = g;
+    p.ldx = ldg;
+    p.w = wt;
+    p.ldw = w.ldm;
+    p.y = (bf16_t*)a->dx;
+    p.ldy = a->lddx;
+    if ((rc = run_linear(p, 2, ws + w.off_lin, s, true)) != FF_OK) return rc;
+  }
+  if (a->dw != nullptr) {
+    LinearArgs p{};
+    p.tokens = a->m;
+    p.n = w.ldt;  // (zeros beyond the tokens)
+    p.m = a->n;
+    p.x = k.gt;
+    p.ldx = w.ldt;
+    p.w = xt;
+    p.ldw = w.ldt;
+    p.y = (bf16_t*)a->dw;
+    p.ldy = a->lddw;
+    if ((rc = run_linear(p, 2, ws + w.off_lin, s)) != FF_OK) return rc;
+  }
+  return FF_OK;
 }
 
 ff_status ff_checkpoint(const ff_checkpoint_args* a) { return checkpoint_call(a, false); }

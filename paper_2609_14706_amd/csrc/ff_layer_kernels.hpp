@@ -135,16 +135,12 @@ hipError_t launch_zero(void* dst, int64_t ld, int64_t rows, int64_t cols, int el
 // ldgt, zeros beyond rows; null: not stored) and, with part, column sums of
 // every 64 rows (act_grad_parts(rows) x cols).  z null: g = dy, so that with
 // gt alone a job is a transposition.  One to three jobs in one launch.
-// Checkpoints in 8 bits stand for dy (dyq: its values rounded to bf16) or z (zq: not
-// rounded) where they are given.
 struct ActGradArgs {
   int64_t rows, cols;
   const bf16_t* dy;
   int64_t lddy;
-  Q8Rows dyq;
   const bf16_t* z;
   int64_t ldz;
-  Q8Rows zq;
   bf16_t* g;
   int64_t ldg;
   bf16_t* gt;

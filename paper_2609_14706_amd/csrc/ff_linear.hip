@@ -18,7 +18,6 @@
 
 #include "ff_layer_kernels.hpp"
 #include "ff_linear_tile.hpp"
-#include "ff_q8.hpp"
 #include "ff_tile_nt.hpp"
 #include "ff_vec.hpp"
 
@@ -103,8 +102,6 @@ struct TurnJobs {
   uint32_t end[3], gx[3];  // first workgroup after the job, its 64-column blocks
 };
 
-// Q8: some job has codes for dy or z.  Eight columns lie within one group of them.
-template <bool Q8>
 __global__ __launch_bounds__(256) void k_turn(TurnJobs jobs) {
   __shared__ Turn sm;
   __shared__ float sums[4][64];
@@ -120,26 +117,12 @@ __global__ __launch_bounds__(256) void k_turn(TurnJobs jobs) {
     const int count = row < a.rows ? (int)min((int64_t)8, max((int64_t)0, a.cols - col)) : 0;
     Vec<bf16_t> v;
     v.w = u32x4{0, 0, 0, 0};
-    if (Q8 && a.dyq.q != nullptr) {
+    if (count > 0) v = load_row(a.dy + row * a.lddy + col, count);
+    if (a.z != nullptr && count > 0) {
+      const Vec<bf16_t> z = load_row(a.z + row * a.ldz + col, count);
       float f[8];
-      if (count > 0) {
-        load_q8(a.dyq, row, col, count, f);
-        v.set(f);
-      }
-    } else if (count > 0) {
-      v = load_row(a.dy + row * a.lddy + col, count);
-    }
-    if ((a.z != nullptr || (Q8 && a.zq.q != nullptr)) && count > 0) {
-      float f[8];
-      if (Q8 && a.zq.q != nullptr) {
-        load_q8(a.zq, row, col, count, f);
-      } else {
-        const Vec<bf16_t> z = load_row(a.z + row * a.ldz + col, count);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = z.get(k);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = v.get(k) * act_slope(f[k], a.act);
+      for (int k = 0; k < 8; ++k) f[k] = v.get(k) * act_slope(z.get(k), a.act);
       v.set(f);
     }
     if (a.g != nullptr && count > 0) store_row(a.g + row * a.ldg + col, v, count);
@@ -337,18 +320,12 @@ hipError_t launch_act_grad(const ActGradArgs* jobs, int count, hipStream_t s) {
   if (count < 1 || count > 3) return hipErrorInvalidValue;
   TurnJobs q{};
   int64_t total = 0;
-  bool q8 = false;
   for (int k = 0; k < count; ++k) {
     const ActGradArgs& a = jobs[k];
     const int64_t gx = (a.cols + 63) / 64, gy = (a.rows + 63) / 64;
     if (a.rows <= 0 || a.cols <= 0 || gx * gy > 0x7fffffff ||
         (a.gt != nullptr && (a.ldgt % 8 != 0 || a.ldgt < a.rows || a.ldgt > gy * 64 || (uintptr_t)a.gt % 16 != 0)))
       return hipErrorInvalidValue;
-    for (const Q8Rows* c : {&a.dyq, &a.zq}) {
-      if (c->q == nullptr) continue;
-      if (c->scale == nullptr || c->shift < kMinGroupShift || c->shift > kMaxGroupShift) return hipErrorInvalidValue;
-      q8 = true;
-    }
     total += gx * gy;
     if (total > 0x7fffffff) return hipErrorInvalidValue;
     q.job[k] = a;
@@ -356,10 +333,7 @@ hipError_t launch_act_grad(const ActGradArgs* jobs, int count, hipStream_t s) {
     q.end[k] = (uint32_t)total;
   }
   for (int k = count; k < 3; ++k) q.end[k] = (uint32_t)total;
-  if (q8)
-    hipLaunchKernelGGL(k_turn<true>, dim3((uint32_t)total), dim3(256), 0, s, q);
-  else
-    hipLaunchKernelGGL(k_turn<false>, dim3((uint32_t)total), dim3(256), 0, s, q);
+  hipLaunchKernelGGL(k_turn, dim3((uint32_t)total), dim3(256), 0, s, q);
   return hipGetLastError();
 }
 

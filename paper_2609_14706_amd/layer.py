@@ -383,7 +383,7 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     dx = g weight, dw = g^T x, db = sum of g, all of g rounded as it is returned;
     None for what is not needed.  The rows of x and of g are the tokens of
     FlipFlop(tokens=(x, g)).  x and preact may be checkpoints in 8 bits
-    (checkpoint_q8): x's values are then rounded to bfloat16 for dw."""
+    (checkpoint_q8); see ff_linear_backward_q8."""
     if stream is not None:
         return _on_stream(stream, linear_backward, dy, x, weight, preact=preact, activation=activation,
                           need_input=need_input, need_weight=need_weight, need_bias=need_bias, workspace=workspace)
@@ -430,13 +430,14 @@ def linear_backward(dy, x, weight, *, preact=None, activation: str = "none", nee
     if need_bias:
         db = torch.empty(m, dtype=bf16, device=dev)
         a.db = db.data_ptr()
-    keep = _workspace(a, _bytes("ff_linear_backward_workspace_size", a), workspace, dev)
     if x8 is None and z8 is None:
+        keep = _workspace(a, _bytes("ff_linear_backward_workspace_size", a), workspace, dev)
         _launch("ff_linear_backward", a, dev)
     else:
         _q8_library()
-        _launch("ff_linear_backward_q8", ff_linear_grad_q8_args(a, k8 if x8 else ff_q8_rows(), kz8 if z8 else ff_q8_rows()),
-                dev, _Q8_FN)
+        q = ff_linear_grad_q8_args(a, k8 if x8 else ff_q8_rows(), kz8 if z8 else ff_q8_rows())
+        keep = _workspace(q, _bytes("ff_linear_backward_q8_workspace_size", q, functions=_Q8_FN), workspace, dev)
+        _launch("ff_linear_backward_q8", q, dev, _Q8_FN)
     del keep
     return dx, dw, g, db
 
@@ -462,13 +463,11 @@ class ff_checkpoint_args(ctypes.Structure):
 class ff_linear_grad_q8_args(ctypes.Structure):
     _fields_ = [("grad", ff_linear_grad_args), ("x_q8", ff_q8_rows), ("preact_q8", ff_q8_rows)]
 
-    @property
-    def stream(self):
-        return self.grad.stream
-
-    @stream.setter
-    def stream(self, value):
-        self.grad.stream = value
+    def __setattr__(self, name, value):   # stream and workspace are the gradient's
+        if name in ("stream", "workspace", "workspace_bytes"):
+            setattr(self.grad, name, value)
+        else:
+            super().__setattr__(name, value)
 
 
 _Q8_FN = {}
@@ -476,11 +475,13 @@ _Q8_FN = {}
 
 def _q8_library():
     if not _Q8_FN:
-        lib, found = load_library(), {}
+        lib, found, size = load_library(), {}, ctypes.POINTER(_size)
         for name, args in {"ff_checkpoint": ff_checkpoint_args, "ff_checkpoint_restore": ff_checkpoint_args,
-                           "ff_linear_backward_q8": ff_linear_grad_q8_args}.items():
+                           "ff_linear_backward_q8": ff_linear_grad_q8_args,
+                           "ff_linear_backward_q8_workspace_size": ff_linear_grad_q8_args}.items():
             f = getattr(lib, name)
-            f.restype, f.argtypes = _int, [ctypes.POINTER(args)]
+            f.restype = _int
+            f.argtypes = [ctypes.POINTER(args)] + ([size] if name.endswith("_size") else [])
             found[name] = f
         _Q8_FN.update(found)
     return _Q8_FN

@@ -196,6 +196,11 @@ def test_linear_gradient_from_checkpoints(lib):
               args(x_q8=ff.ff_q8_rows()), args(preact_q8=ff.ff_q8_rows())):
         assert _code(lib, "ff_linear_backward_q8", a) == ff.FF_ERR_INVALID_ARG
     assert _code(lib, "ff_linear_backward_q8", args(workspace=None)) == ff.FF_ERR_WORKSPACE
+    size = ctypes.c_size_t(0)
+    assert lib.ff_linear_backward_q8_workspace_size(ctypes.byref(args()), ctypes.byref(size)) == 0 and size.value > 0
+    assert lib.ff_linear_backward_q8_workspace_size(ctypes.byref(args(tokens=0)), ctypes.byref(size)) == 0 and size.value == 0
+    assert lib.ff_linear_backward_q8_workspace_size(ctypes.byref(args(tokens=-1)), ctypes.byref(size)) == 1
+    assert lib.ff_linear_backward_q8_workspace_size(None, ctypes.byref(size)) == 1
 
 
 def test_another_thread_during_the_first_call(monkeypatch):
