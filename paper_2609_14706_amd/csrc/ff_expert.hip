@@ -52,10 +52,10 @@ struct GroupTile {
   uint32_t col;  // tile column
 };
 
-// The workgroup's tile among row tiles of bm rows and `cols` tile columns; false, with
+// The tile of workgroup w of `grid` among row tiles of bm rows and `cols` tile columns; false, with
 // `extra` its number among those, for workgroups beyond the last tile.
-__device__ __forceinline__ bool find_tile(const SlotRows& at, int bm, uint32_t cols, GroupTile& g, uint32_t& extra,
-                                          uint32_t& extras) {
+__device__ __forceinline__ bool find_tile(const SlotRows& at, int bm, uint32_t cols, uint32_t w, uint32_t grid, GroupTile& g,
+                                          uint32_t& extra, uint32_t& extras) {
   const int lane = threadIdx.x & 63, n = (at.experts + 63) / 64, e0 = lane * n;
   uint32_t sum = 0;  // (rows <= 2^24: 2^30 row tiles at most, whatever the offsets hold)
   for (int i = 0; i < n; ++i) {
@@ -69,13 +69,13 @@ __device__ __forceinline__ bool find_tile(const SlotRows& at, int bm, uint32_t c
     if (lane >= d) run += up;
   }
   const uint64_t total = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)run, 63) * cols;
-  const uint32_t used = (uint32_t)min(total, (uint64_t)gridDim.x);
-  if (blockIdx.x >= used) {
-    extra = blockIdx.x - used;
-    extras = gridDim.x - used;
+  const uint32_t used = (uint32_t)min(total, (uint64_t)grid);
+  if (w >= used) {
+    extra = w - used;
+    extras = grid - used;
     return false;
   }
-  const uint32_t t = xcd_remap(blockIdx.x, used);
+  const uint32_t t = xcd_remap(w, used);
   // the lane whose experts hold tile t, and which of them
   const bool mine = t >= (uint64_t)(run - sum) * cols && t < (uint64_t)run * cols;
   int expert = 0, rows = 0;
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(nt::kThreads, (LinearTile<nt::Bf16, TI, TJ, SLOTS>:
   __shared__ typename L::Shared all;
   GroupTile g;
   uint32_t extra, extras;
-  if (!find_tile(x.at, L::G::BM, cols, g, extra, extras)) {
+  if (!find_tile(x.at, L::G::BM, cols, blockIdx.x, gridDim.x, g, extra, extras)) {
     clear_outputs(x, extra, extras);
     return;
   }
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_expert_skinny(ExpertArgs x, uint
   __shared__ SkinnySums<nt::Bf16, NT, RW, WAVES> sh;
   GroupTile g;
   uint32_t extra, extras;
-  if (!find_tile(x.at, 16 * NT, cols, g, extra, extras)) {
+  if (!find_tile(x.at, 16 * NT, cols, blockIdx.x, gridDim.x, g, extra, extras)) {
     clear_outputs(x, extra, extras);
     return;
   }
@@ -336,106 +336,210 @@ __global__ __launch_bounds__(256) void k_peaks(PeaksJobs jobs) {
 struct RowsJobs {
   RowsArgs job[3];
   uint32_t end[3];  // first workgroup after the job
+  int part_rows;    // of job 0's parts
 };
+
+// Pieces of eight columns, `n` of them in their row (0: no such row, zeros), zeros beyond
+// them.  All of a kind's loads go out before the first is waited for.
+template <int U>
+__device__ __forceinline__ void load_pieces(const RowsArgs& a, const int64_t (&row)[U], const int64_t (&col)[U],
+                                            const int (&n)[U], float (&f)[U][8]) {
+  int64_t from[U];
+  int have[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    from[u] = row[u];
+    have[u] = n[u];
+    if (a.gather && n[u] > 0) {
+      from[u] = token_of(a.at, row[u]);
+      if (from[u] < 0) have[u] = 0;
+    }
+  }
+  auto codes = [&](const Q8Rows& q, const int64_t (&r)[U], auto use) {
+    uint32_t w[U][2];
+    float scale[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      w[u][0] = w[u][1] = 0;
+      scale[u] = 0.0f;
+      if (have[u] > 0) {
+        load_codes(q.q + r[u] * q.ldq + col[u], have[u], w[u]);
+        scale[u] = q.scale[r[u] * q.lds + (col[u] >> q.shift)];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[8];
+      values_of(w[u], scale[u], v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) use(u, i, i < have[u] ? v[i] : 0.0f);  // (a NaN scale)
+    }
+  };
+  auto values = [&](const bf16_t* p, int64_t ld, const int64_t (&r)[U], auto use) {
+    Vec<bf16_t> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      v[u].w = u32x4{0, 0, 0, 0};
+      if (have[u] > 0) v[u] = load_row(p + r[u] * ld + col[u], have[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) use(u, i, v[u].get(i));
+  };
+  auto put = [&](int u, int i, float v) { f[u][i] = v; };
+  auto slope = [&](int u, int i, float v) { f[u][i] *= act_slope(v, a.act); };
+  if (a.src_q8.q != nullptr) {
+    codes(a.src_q8, from, put);
+  } else if (a.src_f32) {
+    Vec<float> v[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v[u][h].w = u32x4{0, 0, 0, 0};
+        if (have[u] > 4 * h) v[u][h] = load_row((const float*)a.src + from[u] * a.lds + col[u] + 4 * h, have[u] - 4 * h);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[u][i] = v[u][i / 4].get(i % 4);
+  } else {
+    values((const bf16_t*)a.src, a.lds, from, put);
+  }
+  if (a.z_q8.q != nullptr)
+    codes(a.z_q8, row, slope);
+  else if (a.z != nullptr)
+    values(a.z, a.ldz, row, slope);
+}
+// Its outputs; the rounded values to `o`.
+__device__ __forceinline__ void store_piece(const RowsArgs& a, int64_t row, int64_t col, int n, const float (&f)[8], float scale,
+                                            Vec<bf16_t>& o) {
+  const int64_t ldl = (a.cols + 7) / 8 * 8;
+  o.set(f);
+  if (a.out != nullptr) store_row(a.out + row * a.ldo + col, o, n);
+  if (a.laid != nullptr) *reinterpret_cast<u32x4*>(a.laid + row * ldl + col) = o.w;
+  if (a.scaled != nullptr) {
+    u32x4 w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      w[q] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(f[2 * q] * scale)) |
+             (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(f[2 * q + 1] * scale)) << 16;
+    *reinterpret_cast<u32x4*>(a.scaled + row * ldl + col) = w;
+  }
+}
 
 __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
   __shared__ uint32_t red[4];
+  __shared__ float sums[256][9];
   const int which = (blockIdx.x >= jobs.end[0]) + (blockIdx.x >= jobs.end[1]);
   const RowsArgs& a = jobs.job[which];
-  const uint32_t first = which > 0 ? jobs.end[which - 1] : 0, blocks = jobs.end[which] - first;
+  const uint32_t first = which > 0 ? jobs.end[which - 1] : 0, blocks = jobs.end[which] - first, w = blockIdx.x - first;
   const uint32_t per_row = (uint32_t)((a.cols + 7) / 8);
-  const int64_t total = a.at.rows * per_row;
   float scale = 1.0f;
-  const int64_t ldl = (int64_t)per_row * 8;
-  if (a.scaled != nullptr) scale = ldexpf(1.0f, peak_exponent(peak_of(a.peaks, red), a.peak_factor));
-  const int64_t used = used_rows(a.at);
-  constexpr int U = 2;
-  for (int64_t b = (int64_t)(blockIdx.x - first) * (256 * U); b < total; b += (int64_t)blocks * (256 * U)) {
+  if (a.scaled != nullptr) {
+    const int e = peak_exponent(peak_of(a.peaks, red), a.peak_factor);
+    scale = ldexpf(1.0f, e);
+    if (w == 0 && threadIdx.x == 0) *a.inverse = ldexpf(1.0f, -e);
+  }
+  if (a.parts != nullptr) {
+    // Rows of one expert, part_rows at a time: 2^s threads across, their columns summed over the rows
+    const int s = per_row >= 64 ? 6 : 32 - __clz((int)per_row - 1 | 1), down = 256 >> s;
+    const int c = threadIdx.x & ((1 << s) - 1), r = threadIdx.x >> s;
+    GroupTile g;
+    uint32_t extra, extras;
+    if (!find_tile(a.at, jobs.part_rows, (per_row + (1u << s) - 1) >> s, w, blocks, g, extra, extras)) {
+      const int64_t ldl = (int64_t)per_row * 8;
+      if (a.out != nullptr) clear_rows(a.at, a.out, a.ldo, a.cols, extra, extras);
+      if (a.laid != nullptr) clear_rows(a.at, a.laid, ldl, ldl, extra, extras);
+      if (a.scaled != nullptr) clear_rows(a.at, a.scaled, ldl, ldl, extra, extras);
+      return;
+    }
+    const int64_t col = ((int64_t)(g.col << s) + c) * 8;
+    const int n = (int)min((int64_t)8, max((int64_t)0, a.cols - col)), rows = min(g.rows, jobs.part_rows);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    constexpr int U = 4;  // rows a thread has in flight
+    for (int k = r; n > 0 && k < rows; k += U * down) {
+      float f[U][8];
+      int64_t row[U], cols[U];
+      int count[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        row[u] = g.row0 + k + u * down;
+        cols[u] = col;
+        count[u] = k + u * down < rows ? n : 0;
+      }
+      load_pieces(a, row, cols, count, f);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (count[u] > 0) {
+          Vec<bf16_t> o;
+          store_piece(a, row[u], col, n, f[u], scale, o);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[i] += o.get(i);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    // (g.row0 is the expert's first row and a multiple of part_rows more)
+    if (r == 0 && n > 0) {
+      for (int k = 1; k < down; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += sums[(k << s) + c][i];
+      float* p = a.parts + (g.row0 / jobs.part_rows + g.expert) * (int64_t)per_row * 8 + col;
+      __builtin_memcpy(p, sum, 32);
+    }
+    return;
+  }
+  const int64_t total = a.at.rows * per_row, used = used_rows(a.at);
+  constexpr int U = 4;
+  for (int64_t b = (int64_t)w * (256 * U); b < total; b += (int64_t)blocks * (256 * U)) {
     const int64_t r = b / per_row;
     float f[U][8];
     int64_t row[U], col[U];
-    int count[U];
+    int count[U], have[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
       row[u] = r + c / per_row;
       col[u] = (int64_t)(c % per_row) * 8;
-      count[u] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[u][i] = 0.0f;
-      if (row[u] >= a.at.rows) continue;
-      const int n = (int)min((int64_t)8, a.cols - col[u]);
-      count[u] = n;
-      if (row[u] >= used) continue;
-      const int64_t from = a.gather ? token_of(a.at, row[u]) : row[u];
-      if (from < 0) continue;
-      if (a.src_q8.q != nullptr) {
-        load_q8(a.src_q8, from, col[u], n, f[u]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)  // (a NaN scale)
-          if (i >= n) f[u][i] = 0.0f;
-      } else if (a.src_f32) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (n > 4 * h) {
-            const Vec<float> v = load_row((const float*)a.src + from * a.lds + col[u] + 4 * h, n - 4 * h);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[u][4 * h + i] = v.get(i);
-          }
-      } else {
-        const Vec<bf16_t> v = load_row((const bf16_t*)a.src + from * a.lds + col[u], n);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[u][i] = v.get(i);
-      }
-      if (a.z_q8.q != nullptr) {
-        float z[8];
-        load_q8(a.z_q8, row[u], col[u], n, z);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) f[u][i] *= act_slope(z[i], a.act);
-      } else if (a.z != nullptr) {
-        const Vec<bf16_t> z = load_row(a.z + row[u] * a.ldz + col[u], n);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[u][i] *= act_slope(z.get(i), a.act);
-      }
+      count[u] = row[u] < a.at.rows ? (int)min((int64_t)8, a.cols - col[u]) : 0;
+      have[u] = row[u] < used ? count[u] : 0;
     }
+    load_pieces(a, row, col, have, f);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (count[u] <= 0) continue;
       Vec<bf16_t> o;
-      o.set(f[u]);
-      if (a.out != nullptr) store_row(a.out + row[u] * a.ldo + col[u], o, count[u]);
-      // (elements beyond the row are zeros here)
-      if (a.laid != nullptr) *reinterpret_cast<u32x4*>(a.laid + row[u] * ldl + col[u]) = o.w;
-      if (a.scaled != nullptr) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          o.w[q] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(f[u][2 * q] * scale)) |
-                   (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)(f[u][2 * q + 1] * scale)) << 16;
-        *reinterpret_cast<u32x4*>(a.scaled + row[u] * ldl + col[u]) = o.w;
-      }
+      if (count[u] > 0) store_piece(a, row[u], col[u], count[u], f[u], scale, o);
     }
   }
 }
 
 // ------------------------------------------------------------------ gradients
 // A tile of C to its rows: `rows` and `cols` from the tile's corner on exist, E is
-// bf16_t or float.  Each wave turns its own part over in its quarter of the ring, free by then: a
+// bf16_t or float.  Each wave turns its own part over in its quarter of LDS that is free by then: a
 // lane has four columns of a row, and writes 16 bytes beside its neighbours', whole lines of a
 // row at once (8192 tiles of 256 x 256 with 256 rows each: 796 us with the lanes' own 8 bytes).
 // 16-byte piece c of row r sits at c ^ (r & 15) of its row: 64 banks for either way.
-template <class G, class E>
-__device__ __forceinline__ void store_tile(typename G::Ring& ring, const typename G::Acc& acc, E* corner, int64_t ld,
-                                           int64_t rows, int64_t cols, float f1, float f2) {
+template <class G, class E, class Free>
+__device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& acc, E* corner, int64_t ld, int64_t rows,
+                                           int64_t cols, float f1, float f2) {
   constexpr int TI = (int)(sizeof(typename G::Acc) / sizeof(f32x4[G::BN / 32])), TJ = G::BN / 32;
   constexpr int kLine = 16 * TJ * (int)sizeof(E), kPieces = kLine / 16, kPer = 16 / (int)sizeof(E);  // of a wave's row
   constexpr int kSwz = kPieces < 16 ? kPieces - 1 : 15;
   // tile rows of 16 a phase
-  constexpr int kFit = (int)sizeof(typename G::Ring) / 4 / (16 * kLine), H = kFit >= TI ? TI : kFit >= TI / 2 ? TI / 2 : 1;
-  static_assert(kFit >= 1 && TI % H == 0 && (16 * H * kPieces) % 64 == 0, "a wave's part of a phase");
+  constexpr int kFit = (int)sizeof(Free) / 4 / (16 * kLine), H = kFit >= TI ? TI : kFit >= TI / 2 ? TI / 2 : 1;
+  constexpr int kRows = 64 / kPieces;  // the wave stores at once
+  static_assert(kFit >= 1 && TI % H == 0 && kPieces <= 64 && 16 * H % kRows == 0, "a wave's part of a phase");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  char* mine = reinterpret_cast<char*>(&ring) + wave * (sizeof(typename G::Ring) / 4);
-  const int r0 = (wave >> 1) * 16 * TI, c0 = (wave & 1) * 16 * TJ;
+  char* mine = reinterpret_cast<char*>(&free) + wave * (sizeof(Free) / 4);
+  const int piece = lane % kPieces, col = (wave & 1) * 16 * TJ + piece * kPer;
+  int row = (wave >> 1) * 16 * TI + lane / kPieces;
+  asm volatile("" : "+s"(ld));  // (in a loop over tiles 32 rows' offsets would be kept, and spilled)
+  E* to_row = corner + row * ld + col;
 #pragma unroll
   for (int h = 0; h < TI / H; ++h) {
 #pragma unroll
@@ -455,14 +559,14 @@ __device__ __forceinline__ void store_tile(typename G::Ring& ring, const typenam
         }
       }
     __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses are served in order)
-#pragma unroll 4
-    for (int q = lane; q < 16 * H * kPieces; q += 64) {
-      const int r = q / kPieces, c = q % kPieces, row = r0 + h * H * 16 + r, col = c0 + c * kPer;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * kLine + ((c ^ (r & kSwz)) << 4));
-      if (row >= rows) continue;
+#pragma unroll
+    for (int q = 0; q < 16 * H / kRows; ++q) {
+      const int r = q * kRows + lane / kPieces;
       Vec<E> o;
-      o.w = v;
-      store_row(corner + row * ld + col, o, cols - col);
+      o.w = *reinterpret_cast<const u32x4*>(mine + r * kLine + ((piece ^ (r & kSwz)) << 4));
+      if (row < rows) store_row(to_row, o, cols - col);
+      row += kRows;
+      to_row += kRows * ld;
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -476,7 +580,7 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<nt::Bf16, false, TI, TJ, SL
   __shared__ typename G::Ring ring;
   GroupTile g;
   uint32_t extra, extras;
-  if (!find_tile(a.at, G::BM, cols * splits, g, extra, extras)) {
+  if (!find_tile(a.at, G::BM, cols * splits, blockIdx.x, gridDim.x, g, extra, extras)) {
     if (a.out_f32)
       for (uint32_t z = 0; z < splits; ++z) clear_rows(a.at, (float*)a.out + z * a.part_stride, a.ldo, a.n, extra, extras);
     else
@@ -498,50 +602,25 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<nt::Bf16, false, TI, TJ, SL
     store_tile<G>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
 }
 
-// Sums of BM columns of rows of g from `p` on, `cols` of them there.
-template <int BM>
-__device__ __forceinline__ void column_sums(const ExpertGradArgs& a, const uint16_t* p, int64_t rows, int64_t cols, float factor,
-                                            float* lds, bf16_t* out) {
-  constexpr int kAcross = BM / 8, kDown = 256 / kAcross;
-  const int c = (threadIdx.x % kAcross) * 8, r0 = threadIdx.x / kAcross;
-  float s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i] = 0.0f;
-  if (c < cols) {  // (whole pieces: zeros beyond the last column)
-    auto add = [&](const u32x4& w) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint16_t b = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-        s[i] += a.f16 ? (float)__builtin_bit_cast(_Float16, b) : bf16_to_f32(b);
-      }
-    };
-    int64_t r = r0;
-    constexpr int U = 8;
-    for (; r + (U - 1) * kDown < rows; r += U * kDown) {
-      u32x4 w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = *reinterpret_cast<const u32x4*>(p + (r + u * kDown) * a.ldg + c);
-#pragma unroll
-      for (int u = 0; u < U; ++u) add(w[u]);
-    }
-    for (; r < rows; r += kDown) add(*reinterpret_cast<const u32x4*>(p + r * a.ldg + c));
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) lds[r0 * BM + c + i] = s[i];
-  __syncthreads();
-  if (threadIdx.x < BM && (int64_t)threadIdx.x < cols) {
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kDown; ++k) v += lds[k * BM + threadIdx.x];
-    out[threadIdx.x] = f32_to_bf16(v * factor);
-  }
-  __syncthreads();
+// An expert's column sums from those of its parts: the column of each thread.
+__device__ __forceinline__ void sum_column(const ExpertGradArgs& a, int64_t e, int64_t row0, int64_t rows, int64_t col) {
+  const int64_t ld = (a.m + 7) / 8 * 8, first = row0 / a.part_rows + e, count = (rows + a.part_rows - 1) / a.part_rows;
+  const float* p = a.parts + first * ld + col;
+  float v = 0.0f;
+#pragma unroll 8
+  for (int64_t k = 0; k < count; ++k) v += p[k * ld];
+  a.db[e * a.m + col] = f32_to_bf16(v);
+}
+__global__ __launch_bounds__(256) void k_expert_db(ExpertGradArgs a) {
+  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t row0;
+  const int64_t rows = expert_rows(a.at, blockIdx.y, row0);
+  if (col < a.m) sum_column(a, blockIdx.y, row0, rows, col);
 }
 
 // Every XCD takes an eighth of each expert's tiles: their work is the expert's rows,
 // and with whole experts to an XCD the fullest one's kept the others waiting (8 experts of 422 to 2247
-// rows, 4096 x 4096: 480 us, 292 so).  The tiles of the first columns sum g's
-// columns for db as well, whose rows their XCD's L2 has just read.
+// rows, 4096 x 4096: 480 us, 292 so).  The tiles of the first columns add up db as well.
 template <class T, int TI, int TJ, int SLOTS>
 __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kWaves)) void k_expert_dw(
     ExpertGradArgs a, uint32_t mt, uint32_t ntl, uint32_t splits) {
@@ -562,51 +641,19 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kW
   const kn::Side Q{(const char*)(a.x + (row0 + k0) * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
   float f1 = 1.0f, f2 = 1.0f;
   if (a.f16) {
-    uint32_t* red = reinterpret_cast<uint32_t*>(&ring);
-    f1 = ldexpf(1.0f, -peak_exponent(peak_of(a.g_peaks, red), a.g_factor));
-    f2 = ldexpf(1.0f, -peak_exponent(peak_of(a.x_peaks, red), a.x_factor));
+    f1 = a.inverse[0];
+    f2 = a.inverse[1];
   }
+  if (a.db != nullptr && tj == 0 && z == 0 && threadIdx.x < G::BM && m0 + threadIdx.x < a.m)
+    sum_column(a, e, row0, rows, m0 + threadIdx.x);
   typename G::Acc acc;
   G::zero(acc);
   if (k1 > k0) G::loop(ring, P, Q, k1 - k0, acc);
-  if (a.db != nullptr && tj == 0 && z == 0)
-    column_sums<G::BM>(a, a.g + row0 * a.ldg + m0, rows, a.m - m0, f1, reinterpret_cast<float*>(&ring), a.db + (int64_t)e * a.m + m0);
   const int64_t at = ((int64_t)e * a.m + m0) * a.ldo + n0;
   if (a.out_f32)
     store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
   else
     store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
-}
-
-// Column sums of an expert's rows: 128 columns a workgroup, 16 threads of eight columns
-// side by side, 16 rows at a time.
-__global__ __launch_bounds__(256) void k_expert_db(SlotRows at, const bf16_t* g, int64_t ldg, int64_t m, bf16_t* db) {
-  __shared__ float sums[16][128];
-  const int e = blockIdx.y, tid = threadIdx.x, c = (tid & 15) * 8, r = tid >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 128 + c;
-  int64_t row0;
-  const int64_t row1 = expert_rows(at, e, row0) + row0;
-  const int count = (int)min((int64_t)8, max((int64_t)0, m - col));
-  float s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i] = 0.0f;
-  if (count > 0) {
-#pragma unroll 4
-    for (int64_t p = row0 + r; p < row1; p += 16) {
-      const Vec<bf16_t> v = load_row(g + p * ldg + col, count);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += v.get(i);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sums[r][c + i] = s[i];
-  __syncthreads();
-  if (tid < 128 && (int64_t)blockIdx.x * 128 + tid < m) {
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) v += sums[k][tid];
-    db[(int64_t)e * m + (int64_t)blockIdx.x * 128 + tid] = f32_to_bf16(v);
-  }
 }
 
 // ---------------------------------------------------------------------- host
@@ -644,12 +691,105 @@ hipError_t expert_skinny(const ExpertArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Tiles in a stream (ff_tile_kn.hpp): with few rows an expert a tile is mostly starting,
+// waiting for its first rows and storing, which the next tile's copies run beside.  Each XCD's
+// workgroups, as many as its units hold, take the tiles of its eighth of every expert's in turn,
+// experts by falling numbers of rows, so that all of them end alike (64 experts of 256 rows in the mean, 4096 x
+// 2048: 518 us, one workgroup a tile 615; of 64 rows, 2048 x 1408 in tiles of 128: 115 and 132).
+template <class T, int TI, int TJ, int SLOTS>
+struct DwStream {
+  typedef kn::Tile<T, true, TI, TJ, SLOTS> G;
+  static constexpr int kStreamers = 256 * G::kWaves;
+  struct Shared {
+    typename G::Ring ring;
+    struct Stage {
+      char b[4 * 16 * 32 * TJ];
+    } stage;
+    uint16_t order[kMaxExperts];  // experts by falling rows
+  };
+
+  struct Tiles {
+    const ExpertGradArgs& a;
+    const Shared& sh;
+    uint32_t mt, ntl, share, at, expert;
+    int64_t m0, n0;
+
+    __device__ __forceinline__ bool next(kn::Side& P, kn::Side& Q, int64_t& k) {
+      for (;;) {
+        const uint32_t which = at / share;
+        if (which >= (uint32_t)a.at.experts) return false;
+        const uint32_t tile = (blockIdx.x & 7) * share + (at - which * share);
+        at += kStreamers / 8;
+        if (tile >= mt * ntl) continue;
+        expert = __builtin_amdgcn_readfirstlane((int)sh.order[which]);
+        uint32_t ti, tj;
+        tile_at(tile, mt, ntl, ti, tj);
+        m0 = (int64_t)ti * G::BM;
+        n0 = (int64_t)tj * G::BN;
+        int64_t row0;
+        k = expert_rows(a.at, (int)expert, row0);
+        P = {(const char*)(a.g + row0 * a.ldg + m0), a.m - m0, (uint32_t)(a.ldg * 2)};
+        Q = {(const char*)(a.x + row0 * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
+        return true;
+      }
+    }
+  };
+};
+
+template <class T, int TI, int TJ, int SLOTS>
+__global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kWaves)) void k_expert_dw_stream(
+    ExpertGradArgs a, uint32_t mt, uint32_t ntl) {
+  typedef DwStream<T, TI, TJ, SLOTS> S;
+  typedef typename S::G G;
+  __shared__ typename S::Shared sh;
+  // each expert's place among them: those with more rows, or as many and a lower number, come first
+  uint32_t* rows = reinterpret_cast<uint32_t*>(&sh.ring);
+  for (int e = threadIdx.x; e < a.at.experts; e += nt::kThreads) {
+    int64_t first;
+    rows[e] = (uint32_t)expert_rows(a.at, e, first);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.at.experts; e += nt::kThreads) {
+    const uint32_t mine = rows[e];
+    int place = 0;
+    for (int k = 0; k < a.at.experts; ++k) place += rows[k] > mine || (rows[k] == mine && k < e);
+    sh.order[place] = (uint16_t)e;
+  }
+  __syncthreads();
+  if (a.db != nullptr) {
+    const uint32_t across = (uint32_t)((a.m + 255) / 256);
+    for (uint32_t i = blockIdx.x; i < across * (uint32_t)a.at.experts; i += gridDim.x) {
+      const uint32_t e = i / across;
+      const int64_t col = (int64_t)(i - e * across) * 256 + threadIdx.x;
+      int64_t row0;
+      const int64_t count = expert_rows(a.at, (int)e, row0);
+      if (col < a.m) sum_column(a, e, row0, count, col);
+    }
+  }
+  const float f1 = a.f16 ? a.inverse[0] : 1.0f, f2 = a.f16 ? a.inverse[1] : 1.0f;
+  typename S::Tiles tiles{a, sh, mt, ntl, (mt * ntl + 7) / 8, blockIdx.x >> 3, 0, 0, 0};
+  G::stream(sh.ring, tiles, [&](const typename G::Acc& acc, const typename S::Tiles& t) {
+    store_tile<G>(sh.stage, acc, (bf16_t*)a.out + ((int64_t)t.expert * a.m + t.m0) * a.ldo + t.n0, a.ldo, a.m - t.m0,
+                  a.n - t.n0, f1, f2);
+  });
+}
+
 template <int TI, int TJ, int SLOTS>
 hipError_t dx_tiles(const ExpertGradArgs& a, int splits, hipStream_t s) {
   const int64_t cols = (a.n + 32 * TJ - 1) / (32 * TJ), grid = grid_for(a.at, 32 * TI, cols * splits);
   if (grid > kMaxGrid) return hipErrorInvalidValue;
   hipLaunchKernelGGL((k_expert_dx<TI, TJ, SLOTS>), dim3((uint32_t)grid), dim3(nt::kThreads), 0, s, a, (uint32_t)cols,
                      (uint32_t)splits);
+  return hipGetLastError();
+}
+
+template <class T, int TI, int TJ, int SLOTS>
+hipError_t dw_stream(const ExpertGradArgs& a, hipStream_t s) {
+  typedef DwStream<T, TI, TJ, SLOTS> S;
+  const int64_t mt = (a.m + 32 * TI - 1) / (32 * TI), ntl = (a.n + 32 * TJ - 1) / (32 * TJ);
+  if ((mt * ntl + 7) / 8 * a.at.experts > kMaxGrid) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_expert_dw_stream<T, TI, TJ, SLOTS>), dim3(S::kStreamers), dim3(nt::kThreads), 0, s, a, (uint32_t)mt,
+                     (uint32_t)ntl);
   return hipGetLastError();
 }
 
@@ -674,26 +814,25 @@ bool laid_ok(const void* p, int64_t ld, int64_t cols) {
 // with a compute unit to itself and with all busy, and around them), for products of
 // row_tiles(bm) x cols outputs, k of `pairs`.  How many tiles there are hangs on how the
 // rows split: unless that is sure, rounds are not counted whole, but half of one more.
-// split: k may be cut, for a launch more and the partial sums' traffic (4 bytes of `outputs` each).
+// longest: the pairs of the tile with most of them.  split: k may be cut, for a launch more and
+// the partial sums' traffic (4 bytes of `outputs` each).
 struct TileForm {
   int ti, tj, slots, wgs;
   double pair, loaded, ends;
 };
-constexpr TileForm kForms[] = {{8, 8, 2, 1, 1.36, 1.36, 13.0}, {6, 8, 2, 1, 1.09, 1.09, 10.0}, {4, 8, 3, 1, 0.79, 0.79, 8.0},
-                               {4, 4, 2, 2, 0.53, 0.85, 6.0},  {2, 4, 3, 2, 0.27, 0.53, 3.5}};
 template <class RowTiles>
-ExpertPlan best_tiles(std::initializer_list<int> forms, RowTiles row_tiles, int64_t cols, int64_t pairs, bool sure, bool split,
-                      double outputs) {
+ExpertPlan best_tiles(std::initializer_list<TileForm> forms, RowTiles row_tiles, int64_t cols, int64_t pairs, int64_t longest,
+                      bool sure, bool split, double outputs) {
   ExpertPlan best{0, 0, 4, 4, 2, 1};
   double least = 1e300;
-  for (int k : forms) {
-    const TileForm& f = kForms[k];
+  for (const TileForm& f : forms) {
     const double tiles = row_tiles(32 * f.ti) * (double)((cols + 32 * f.tj - 1) / (32 * f.tj));
     for (int s : {1, 2, 4, 8, 16}) {
       if (s > 1 && (!split || s * 4 > pairs || tiles * s > 768)) break;
       const double wgs = tiles * s, full = 256.0 * f.wgs;
       const double rounds = sure ? ceil(wgs / full) : std::max(1.0, wgs / full + 0.5);
       double us = rounds * (f.ends + (double)((pairs + s - 1) / s) * (wgs > 256 ? f.loaded : f.pair));
+      us = std::max(us, f.ends + (double)((longest + s - 1) / s) * f.pair);
       if (s > 1) us += 5.0 + 8.0 * s * outputs / 4e6;
       if (us < least) {
         least = us;
@@ -708,7 +847,13 @@ ExpertPlan rows_plan(int64_t rows, int experts, int64_t k, int64_t cols, bool sp
   const double active = (double)std::min<int64_t>(experts, rows);
   // an expert's last tile is half full
   auto row_tiles = [&](int bm) { return experts == 1 ? (double)((rows + bm - 1) / bm) : (double)rows / bm + 0.5 * active; };
-  return best_tiles({0, 1, 2, 3, 4}, row_tiles, cols, (k + kn::kK - 1) / kn::kK, experts == 1, split, (double)rows * (double)cols);
+  const int64_t pairs = (k + kn::kK - 1) / kn::kK;
+  return best_tiles({{8, 8, 2, 1, 1.36, 1.36, 13.0},
+                     {6, 8, 2, 1, 1.09, 1.09, 10.0},
+                     {4, 8, 3, 1, 0.79, 0.79, 8.0},
+                     {4, 4, 2, 2, 0.53, 0.90, 6.0},
+                     {2, 4, 3, 2, 0.27, 0.53, 3.5}},
+                    row_tiles, cols, pairs, pairs, experts == 1, split, (double)rows * (double)cols);
 }
 
 ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m) {
@@ -731,7 +876,10 @@ ExpertPlan expert_dx_plan(int64_t rows, int experts, int64_t n, int64_t m) {
 ExpertPlan expert_dw_plan(int64_t rows, int experts, int64_t n, int64_t m) {
   const int64_t each = std::max<int64_t>(1, rows / std::min<int64_t>(experts, rows));
   auto row_tiles = [&](int bm) { return (double)experts * (double)((m + bm - 1) / bm); };
-  return best_tiles({0, 3, 4}, row_tiles, n, (each + kn::kK - 1) / kn::kK, true, true, (double)experts * (double)m * (double)n);
+  // (the fullest expert of a batch has some three times the mean)
+  const int64_t pairs = (each + kn::kK - 1) / kn::kK, longest = experts == 1 ? pairs : 3 * pairs;
+  return best_tiles({{8, 8, 2, 1, 1.36, 1.36, 10.5}, {4, 4, 2, 2, 0.53, 0.90, each <= 128 ? 4.0 : 6.0}, {2, 4, 3, 2, 0.27, 0.53, 3.5}},
+                    row_tiles, n, pairs, longest, true, true, (double)experts * (double)m * (double)n);
 }
 
 hipError_t launch_expert_linear(const ExpertArgs& a, const ExpertPlan& p, hipStream_t s) {
@@ -781,7 +929,18 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
     if (!fits(a.at) || (a.gather && a.at.order == nullptr) || a.cols <= 0 || a.cols > (int64_t(1) << 24)) return hipErrorInvalidValue;
     if ((uintptr_t)a.laid % 16 != 0 || (uintptr_t)a.scaled % 16 != 0 || (a.scaled != nullptr && a.peaks == nullptr))
       return hipErrorInvalidValue;
-    total += std::min<int64_t>((a.at.rows * ((a.cols + 7) / 8) + 511) / 512, 4096);
+    if ((a.scaled != nullptr && a.inverse == nullptr) || (a.parts != nullptr && (k != 0 || (uintptr_t)a.parts % 16 != 0)))
+      return hipErrorInvalidValue;
+    const int64_t per_row = (a.cols + 7) / 8;
+    if (a.parts != nullptr) {
+      q.part_rows = part_rows(a.at.rows, a.cols);
+      int64_t across = 64;  // as k_rows has it
+      while (across > 2 && across / 2 >= per_row) across /= 2;
+      total += grid_for(a.at, q.part_rows, (per_row + across - 1) / across);
+      if (total > kMaxGrid) return hipErrorInvalidValue;
+    } else {
+      total += std::min<int64_t>((a.at.rows * per_row + 1023) / 1024, 4096);
+    }
     q.job[k] = a;
     q.end[k] = (uint32_t)total;
   }
@@ -814,8 +973,15 @@ hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
 
 hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s) {
   if (!fits(a.at) || a.n <= 0 || a.m <= 0 || !laid_ok(a.g, a.ldg, a.m) || !laid_ok(a.x, a.ldx, a.n) || p.splits < 1 ||
-      (p.splits > 1 && !a.out_f32))
+      (p.splits > 1 && !a.out_f32) || (a.db != nullptr && a.parts == nullptr) || (a.f16 && a.inverse == nullptr))
     return hipErrorInvalidValue;
+#define FF_STREAM(I, J, S)                                                                                   \
+  if (p.ti == I && p.tj == J && p.slots == S && p.splits == 1 && !a.out_f32)                                 \
+    return a.f16 ? dw_stream<nt::F16, I, J, S>(a, s) : dw_stream<nt::Bf16, I, J, S>(a, s);
+  FF_STREAM(8, 8, 2)
+  // (beyond two pairs the two workgroups of a unit hide each other's ends as well: 620 us, 599 without a stream)
+  if (a.at.rows <= 128 * (int64_t)a.at.experts) FF_STREAM(4, 4, 2)
+#undef FF_STREAM
 #define FF_TILE(I, J, S)                       \
   if (p.ti == I && p.tj == J && p.slots == S)  \
     return a.f16 ? dw_tiles<nt::F16, I, J, S>(a, p.splits, s) : dw_tiles<nt::Bf16, I, J, S>(a, p.splits, s);
@@ -824,9 +990,9 @@ hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_expert_db(const SlotRows& at, const bf16_t* g, int64_t ldg, int64_t m, bf16_t* db, hipStream_t s) {
-  if (!fits(at) || m <= 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_expert_db, dim3((uint32_t)((m + 127) / 128), (uint32_t)at.experts), dim3(256), 0, s, at, g, ldg, m, db);
+hipError_t launch_expert_db(const ExpertGradArgs& a, hipStream_t s) {
+  if (!fits(a.at) || a.m <= 0 || a.parts == nullptr || a.db == nullptr) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_expert_db, dim3((uint32_t)((a.m + 255) / 256), (uint32_t)a.at.experts), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

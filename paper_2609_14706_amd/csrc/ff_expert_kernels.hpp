@@ -134,7 +134,14 @@ struct RowsArgs {
   uint16_t* scaled;  // or null
   const uint32_t* peaks;
   float peak_factor;  // scaled: the largest value is at most that times the peak
+  float* inverse;     // scaled: receives the power of two that takes its values back
+  float* parts;       // column sums of every part_rows(...) rows of an expert (part_count rows of
+                      // laid_ld(cols)); or null
 };
+// Rows of an expert that are summed together, and how many such sums there can be; expert e's
+// are those from offsets[e] / part_rows + e on.
+inline int part_rows(int64_t rows, int64_t cols) { return rows * cols >= (int64_t(1) << 22) ? 64 : 16; }
+inline int64_t part_count(int64_t rows, int experts, int64_t cols) { return rows / part_rows(rows, cols) + experts + 1; }
 inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 // One to three jobs in one launch.
 hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s);
@@ -164,11 +171,11 @@ struct ExpertGradArgs {
   int64_t ldo;
   bool out_f32;
   int64_t part_stride;
-  bf16_t* db;  // launch_expert_dw: column sums of g too; or null
+  const float* parts;  // column sums of g by launch_rows, of part_rows rows each; or null
+  int part_rows;
+  bf16_t* db;  // launch_expert_dw, launch_expert_db: their sums
   bool f16;
-  const uint32_t* g_peaks;
-  const uint32_t* x_peaks;
-  float g_factor, x_factor;
+  const float* inverse;  // f16: what takes g and x back
 };
 // dx_p = g_p W_e, zeros for rows in no expert.
 ExpertPlan expert_dx_plan(int64_t rows, int experts, int64_t n, int64_t m);
@@ -176,7 +183,7 @@ hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
 // dW_e = sum over the rows of expert e of g_p^T x_p (m x n; zeros for an expert without rows).
 ExpertPlan expert_dw_plan(int64_t rows, int experts, int64_t n, int64_t m);
 hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s);
-// db_e = sum over the rows of expert e of g_p (bf16 rows).
-hipError_t launch_expert_db(const SlotRows& at, const bf16_t* g, int64_t ldg, int64_t m, bf16_t* db, hipStream_t s);
+// db_e = sum over the rows of expert e of g_p, from the parts alone.
+hipError_t launch_expert_db(const ExpertGradArgs& a, hipStream_t s);
 
 }  // namespace ff

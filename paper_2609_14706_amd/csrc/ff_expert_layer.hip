@@ -201,7 +201,7 @@ struct Gradient {
 struct GradWs {
   ExpertPlan dx, dw;
   bool dy_is_g, lay_g, scale, lay_x, lay_w, sum_dx;
-  size_t off_g, off_g16, off_x, off_peaks, off_w, off_sum, bytes;
+  size_t off_g, off_g16, off_x, off_peaks, off_w, off_parts, off_sum, bytes;
 };
 
 GradWs grad_ws(const Gradient& a) {
@@ -211,8 +211,7 @@ GradWs grad_ws(const Gradient& a) {
   w.scale = dw && a.x_q8.q != nullptr;
   // g in rows that the tiles take: dy itself, the caller's, or a copy
   w.dy_is_g = a.act == FF_ACT_NONE && !a.dy_f32 && a.g == nullptr && a.at.offsets == nullptr && tile_rows_ok(a.dy, a.lddy, a.m, 2);
-  w.lay_g = (dx || (dw && !w.scale) || (a.db != nullptr && !dw)) && !w.dy_is_g &&
-            (a.g == nullptr || !tile_rows_ok(a.g, a.ldg, a.m, 2));
+  w.lay_g = (dx || (dw && !w.scale)) && !w.dy_is_g && (a.g == nullptr || !tile_rows_ok(a.g, a.ldg, a.m, 2));
   w.lay_x = dw && !w.scale && (a.gather || !tile_rows_ok(a.x, a.ldx, a.n, 2));
   w.lay_w = dx && !tile_rows_ok(a.w, a.ldw, a.n, 2);
   size_t off = 0, sum = 0;
@@ -224,7 +223,8 @@ GradWs grad_ws(const Gradient& a) {
   w.off_g = take(w.lay_g, (size_t)S * (size_t)laid_ld(a.m) * 2);
   w.off_g16 = take(w.scale, (size_t)S * (size_t)laid_ld(a.m) * 2);
   w.off_x = take(w.lay_x || w.scale, (size_t)S * (size_t)laid_ld(a.n) * 2);
-  w.off_peaks = take(w.scale, 2 * kPeaks * 4);
+  w.off_peaks = take(w.scale, 2 * kPeaks * 4 + 8);  // and what takes g and x back
+  w.off_parts = take(a.db != nullptr, (size_t)part_count(S, (int)E, a.m) * (size_t)laid_ld(a.m) * 4);
   w.off_w = take(w.lay_w, (size_t)E * (size_t)a.m * (size_t)laid_ld(a.n) * 2);
   if (dx) {
     w.dx = expert_dx_plan(S, (int)E, a.n, a.m);
@@ -261,6 +261,7 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
   const int64_t S = a.at.rows, E = a.at.experts, T = a.gather ? a.at.tokens : S;
   const bool act = a.act != FF_ACT_NONE;
   uint32_t* peaks = (uint32_t*)(ws + w.off_peaks);
+  float* inverse = (float*)(peaks + 2 * kPeaks);
   // slopes of the activations are below 1.13; codes end at 127
   const float g_factor = act ? 1.13f : 1.0f, x_factor = 127.0f;
   if (w.scale) {
@@ -289,8 +290,10 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
     r.scaled = (uint16_t*)(ws + w.off_g16);
     r.peaks = peaks;
     r.peak_factor = g_factor;
+    r.inverse = inverse;
   }
-  if (r.out != nullptr || r.laid != nullptr || r.scaled != nullptr) jobs[count++] = r;
+  if (a.db != nullptr) r.parts = (float*)(ws + w.off_parts);
+  if (r.out != nullptr || r.laid != nullptr || r.scaled != nullptr || r.parts != nullptr) jobs[count++] = r;
   ExpertGradArgs k{};
   k.at = a.at;
   k.n = a.n;
@@ -313,6 +316,7 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
       x.scaled = (uint16_t*)(ws + w.off_x);
       x.peaks = peaks + kPeaks;
       x.peak_factor = x_factor;
+      x.inverse = inverse + 1;
     } else {
       x.laid = (uint16_t*)(ws + w.off_x);
     }
@@ -333,9 +337,10 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
     k.ldw = laid_ld(a.n);
   }
   if (count > 0 && (rc = hip(launch_rows(jobs, count, s), "operands of the gradient")) != FF_OK) return rc;
-  if (a.db != nullptr && a.dw == nullptr &&
-      (rc = hip(launch_expert_db(k.at, k.g, k.ldg, a.m, (bf16_t*)a.db, s), "bias gradient")) != FF_OK)
-    return rc;
+  k.db = (bf16_t*)a.db;
+  k.parts = r.parts;
+  k.part_rows = part_rows(S, a.m);
+  if (a.db != nullptr && a.dw == nullptr && (rc = hip(launch_expert_db(k, s), "bias gradient")) != FF_OK) return rc;
   if (a.dx != nullptr) {
     float* sum = (float*)(ws + w.off_sum);
     k.out_f32 = w.sum_dx;
@@ -366,17 +371,13 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
     k.f16 = true;
     k.g = (const uint16_t*)(ws + w.off_g16);
     k.ldg = laid_ld(a.m);
-    k.g_peaks = peaks;
-    k.g_factor = g_factor;
-    k.x_peaks = peaks + kPeaks;
-    k.x_factor = x_factor;
+    k.inverse = inverse;
   }
   float* sum = (float*)(ws + w.off_sum);
   k.out_f32 = w.dw.splits > 1;
   k.out = k.out_f32 ? (void*)sum : a.dw;
   k.ldo = k.out_f32 ? laid_ld(a.n) : a.lddw;
   k.part_stride = E * a.m * k.ldo;
-  k.db = (bf16_t*)a.db;
   if ((rc = hip(launch_expert_dw(k, w.dw, s), "weight gradient")) != FF_OK) return rc;
   return k.out_f32 ? sum_parts(sum, w.dw.splits, E * a.m, a.n, a.dw, a.lddw, s) : FF_OK;
 }

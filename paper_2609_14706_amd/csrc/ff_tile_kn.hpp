@@ -245,6 +245,82 @@ struct Tile {
     __syncthreads();
   }
 
+  // Tile after tile without a pause: the copies run ahead across the ends of tiles, so that
+  // the next tile's first pairs land while this one's results are stored.  Tiles: from `work` on,
+  // next(P, Q, k) moves to the next tile (k may be 0: all zeros) or returns false.  finish(acc, work)
+  // stores a tile; it must leave the ring alone and take no barrier.
+  template <class Tiles, class Finish>
+  static __device__ __forceinline__ void stream(Ring& sm, Tiles work, Finish finish) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const FragBase fb = frag_base();
+    Tiles ahead = work;
+    Lane L;
+    const char *pp = nullptr, *pq = nullptr, *a = nullptr, *b = nullptr;
+    int64_t step_p = 0, step_q = 0, left = 0;
+    bool more = true;
+    auto advance = [&]() -> int {  // to the next pair of any tile; its k (none left: 0)
+      while (left <= 0 && more) {
+        Side P, Q;
+        more = ahead.next(P, Q, left);
+        if (!more || left <= 0) {
+          left = 0;
+          continue;
+        }
+        L = lane_of(P, Q);
+        pp = P.p;
+        pq = Q.p;
+        step_p = PK ? (int64_t)kK * P.ld : kK * 2;
+        step_q = (int64_t)kK * Q.ld;
+      }
+      a = pp;
+      b = pq;
+      pp += step_p;
+      pq += step_q;
+      const int l = (int)min(left, (int64_t)kK);
+      left -= l;
+      return l;
+    };
+#pragma unroll
+    for (int q = 0; q < TI; ++q) L.p[q] = kOutside;
+#pragma unroll
+    for (int q = 0; q < TJ; ++q) L.q[q] = kOutside;
+    L.pk = L.qk = 0;
+#pragma unroll 1
+    for (int s = 0; s < SLOTS; ++s) {
+      const int l = advance();
+#pragma unroll
+      for (int q = 0; q < NL; ++q) issue_one(sm, s, a, b, L, l, wave, q);
+    }
+    nt::wait_vmem<(SLOTS - 1) * NL>();
+    __builtin_amdgcn_s_barrier();
+    Frags F[2];
+#pragma unroll
+    for (int q = 0; q < NL; ++q) read_one(sm, 0, 0, fb, F[0], q);
+    int slot = 0;
+    Acc acc;
+    Side P, Q;
+    int64_t k;
+    while (work.next(P, Q, k)) {
+      zero(acc);
+      pin(acc);
+      const int count = (int)((k + kK - 1) / kK);
+      for (int p = 0; p < count; ++p) {
+        step<false>(sm, F[0], F[1], slot, 1, 0, nullptr, nullptr, L, 0, wave, fb, acc);
+        // (behind a tile's stores, too, which the first pair after them waits for)
+        nt::wait_vmem<(SLOTS - 2) * NL>();
+        nt::wait_lds();
+        __builtin_amdgcn_s_barrier();
+        const int l = advance();
+        const int next = slot + 1 == SLOTS ? 0 : slot + 1;
+        step<true>(sm, F[1], F[0], next, 0, slot, a, b, L, l, wave, fb, acc);
+        slot = next;
+      }
+      pin(acc);
+      finish(acc, work);
+    }
+    nt::wait_vmem<0>();
+  }
+
   static __device__ __forceinline__ void zero(Acc& acc) {
 #pragma unroll
     for (int i = 0; i < TI; ++i)

@@ -4,8 +4,8 @@ against the formulas in 64 bits.
 Tolerances: a scale is one fp32 division (2^-24); codes hang on which side of a
 half 127 x / max lies, which the kernel settles in 64 bits: they are equal.  A
 restored value is one fp32 product (2^-24) and its rounding to the output's
-type.  In the gradient each result is rounded once; dx reads g as it is returned, dw
-and db of a checkpoint of x read g (2^-8 of the returned one) and x' = codes scale in
+type.  In the gradient each result is rounded once; dx and db read g as it is returned,
+dw of a checkpoint of x reads g (2^-8 of the returned one) and x' = codes scale in
 fp16 (2^-11 of each, or 2^-40 of the largest)."""
 import math
 
@@ -179,8 +179,7 @@ def test_linear_backward(gpu, T, n, m, x8, z8):
         far = 1.2 * 2.0 ** -40 * float(dy.double().abs().max() * xv.abs().max())
         _close(dw, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + x8 * ((HALF + 2.0 ** -10) * 1.01 * mag + T * far) + 1e-30)
         want, mag = gb.sum(0), gb.abs().sum(0)
-        far = 1.2 * 2.0 ** -40 * float(dy.double().abs().max())
-        _close(db, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + x8 * ((HALF + 2.0 ** -11) * 1.01 * mag + T * far) + 1e-30)
+        _close(db, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + 1e-30)
 
 
 @pytest.mark.parametrize("T,n,m", [(3000, 256, 200), (20000, 64, 40), (700, 1000, 333)])
@@ -195,8 +194,8 @@ def test_linear_backward_costs_little(gpu, T, n, m):
         return k.codes.double() * torch.repeat_interleave(k.scale.double(), k.group, dim=1)[:, :k.codes.shape[1]]
     dx, dw, g, db = ffe.linear_backward(dy, kx, W, preact=kz, activation="silu")
     g64 = dy.double() * _slope(value(kz), "silu")
-    for got, want in ((dw, g64.T @ value(kx)), (db, g64.sum(0))):
-        assert float((got.double() - want).norm() / want.norm()) < 1.05 * HALF / math.sqrt(3)
+    want = g64.T @ value(kx)
+    assert float((dw.double() - want).norm() / want.norm()) < 1.05 * HALF / math.sqrt(3)
 
 
 @pytest.mark.parametrize("scales", [(1e-30, 1e-25), (1e30, 1e-30), (1e18, 1e17), (1.0, 0.0), (0.0, 1.0)])
