@@ -8,10 +8,11 @@
 //
 // Scores are held in 64 bits: which expert is chosen may hang on the last bit of c,
 // and 32 bits of exp would decide otherwise than the formula for about one token in
-// ten thousand.  A wave takes a token, V neighbouring experts a lane; it picks one
-// expert after the other, each the largest of the lanes' best: c as a whole number that
-// orders alike, its high words compared first across the wave (DPP), the low ones only
-// where two lanes share the high one.
+// ten thousand.  A row of 16 lanes takes a token (for many experts or choices a whole wave),
+// V neighbouring experts a lane; it picks one expert after the other, each the largest of
+// the lanes' best: c as a whole number that orders alike, its high words compared first
+// across the lanes (DPP), the low ones only where two lanes share the high one.  What
+// bounds it is instructions: 2200 a token by whole waves, of 256 experts in 8 groups, XXX by rows.
 //
 // The sort is a counting sort, stable and without an atomic on memory: chunks of
 // tokens count their slots by expert (k_route), a wave for each expert sums the chunks'
@@ -24,6 +25,7 @@
 
 #include "ff_common.hpp"
 #include "ff_expert_kernels.hpp"
+#include "ff_vec.hpp"
 
 namespace ff {
 namespace {
@@ -77,16 +79,100 @@ __device__ __forceinline__ double lane_value(double v, int lane) {
   return __longlong_as_double((long long)((u64)hi << 32 | lo));
 }
 
-// Scores of the V experts of a lane from their logits (those beyond the last: 0).
-template <class L, int V>
-__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, double (&s)[V]) {
-  const int e0 = (threadIdx.x & 63) * V;
-  float l[V];
+// What the lanes of a token do together: a row of 16 or a whole wave.
+template <int LANES> struct Lanes;
+template <> struct Lanes<64> {
+  static __device__ __forceinline__ float largest(float v) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) l[i] = e0 + i < experts ? Elem<L>::to_f32(row[e0 + i]) : -INFINITY;
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+  }
+  static __device__ __forceinline__ double sum(double v) { return wave_sum(v); }
+  static __device__ __forceinline__ bool any(bool b) { return __ballot(b) != 0; }
+  // The lane (of the token's) that holds the largest of their keys, the lowest one among
+  // equals: lanes hold ascending experts.
+  static __device__ __forceinline__ int best(u64 key) { return best_lane(key); }
+  static __device__ __forceinline__ uint32_t largest_word(uint32_t v) { return wave_max(v); }
+  // The lanes of `who` (some of the token's own at least): whether there are several of any
+  // token's, and the lowest of this one's.
+  static __device__ __forceinline__ bool several(u64 who) { return (who & (who - 1)) != 0; }
+  static __device__ __forceinline__ int lowest(u64 who) { return __ffsll((long long)who) - 1; }
+};
+template <> struct Lanes<16> {
+  // (rotations of the row: every lane ends with the whole)
+  template <int N>
+  static __device__ __forceinline__ uint32_t turn(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, true);
+  }
+  static __device__ __forceinline__ uint32_t largest_word(uint32_t v) {
+    v = max(v, turn<8>(v));
+    v = max(v, turn<4>(v));
+    v = max(v, turn<2>(v));
+    return max(v, turn<1>(v));
+  }
+  template <int N>
+  static __device__ __forceinline__ float turn(float v) {
+    return __uint_as_float(turn<N>(__float_as_uint(v)));
+  }
+  static __device__ __forceinline__ float largest(float v) {
+    v = fmaxf(v, turn<8>(v));
+    v = fmaxf(v, turn<4>(v));
+    v = fmaxf(v, turn<2>(v));
+    return fmaxf(v, turn<1>(v));
+  }
+  template <int N>
+  static __device__ __forceinline__ double turn(double v) {
+    const u64 b = (u64)__double_as_longlong(v);
+    return __longlong_as_double((long long)((u64)turn<N>((uint32_t)(b >> 32)) << 32 | turn<N>((uint32_t)b)));
+  }
+  // (the same bits in every lane: a sum of two is the same either way round)
+  static __device__ __forceinline__ double sum(double v) {
+    v += turn<8>(v);
+    v += turn<4>(v);
+    v += turn<2>(v);
+    return v + turn<1>(v);
+  }
+  static __device__ __forceinline__ uint32_t mine(u64 mask) { return (uint32_t)(mask >> (threadIdx.x & 48)) & 0xffffu; }
+  static __device__ __forceinline__ bool any(bool b) { return mine(__ballot(b)) != 0; }
+  static __device__ __forceinline__ bool several(u64 who) { return (who & (who - 0x0001000100010001ull)) != 0; }
+  static __device__ __forceinline__ int lowest(u64 who) { return __ffs((int)mine(who)) - 1; }
+  static __device__ __forceinline__ int best(u64 key) {
+    const uint32_t hi = (uint32_t)(key >> 32), top = largest_word(hi);
+    u64 who = __ballot(hi == top);
+    if (several(who)) {
+      const uint32_t lo = hi == top ? (uint32_t)key : 0u, low = largest_word(lo);
+      who = __ballot(hi == top && lo == low);
+    }
+    return lowest(who);
+  }
+};
+
+// V neighbouring elements of a row from e0 on, `other` beyond its end.
+template <class L, int V>
+__device__ __forceinline__ void load_neighbours(const L* row, int left, float other, float (&l)[V]) {
+  if constexpr (V >= Vec<L>::N) {
+    constexpr int N = Vec<L>::N;
+    Vec<L> v[V / N];
+#pragma unroll
+    for (int h = 0; h < V / N; ++h)
+      v[h] = left > h * N ? load_row(row + h * N, left - h * N) : Vec<L>{};
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = i < left ? v[i / N].get(i % N) : other;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = i < left ? Elem<L>::to_f32(row[i]) : other;
+  }
+}
+
+// Scores of the V experts from e0 on of a lane from their logits (those beyond the last: 0).
+template <class L, int V, int LANES>
+__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, int e0, double (&s)[V]) {
+  typedef Lanes<LANES> G;
+  float l[V];
+  load_neighbours<L, V>(row + e0, experts - e0, -INFINITY, l);
   if (sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = e0 + i < experts ? 1.0 / (1.0 + exp(-(double)l[i])) : 0.0;
+    for (int i = 0; i < V; ++i) s[i] = 1.0 / (1.0 + exp(-(double)l[i]));  // (beyond the last: 0)
     return;
   }
   float big = -INFINITY;
@@ -96,118 +182,211 @@ __device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoi
     big = fmaxf(big, l[i]);
     nan |= l[i] != l[i];
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
-  if (__ballot(nan) != 0) big = __uint_as_float(0x7fc00000u);  // the row's scores are NaN then
+  big = G::largest(big);
+  if (G::any(nan)) big = __uint_as_float(0x7fc00000u);  // the row's scores are NaN then
   double sum = 0.0;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     // (a row of -inf alone has no scores: zeros, not 0 / 0)
-    s[i] = e0 + i < experts && big != -INFINITY ? exp((double)l[i] - (double)big) : 0.0;
+    s[i] = big != -INFINITY ? exp((double)l[i] - (double)big) : 0.0;  // (beyond the last: 0)
     sum += s[i];
   }
-  sum = wave_sum(sum);
+  sum = G::sum(sum);
 #pragma unroll
   for (int i = 0; i < V; ++i) s[i] = big == -INFINITY ? 0.0 : s[i] / sum;
 }
 
-// A token's choice, in lane j the j-th: expert and score (lanes from `top` on: -1, 0).
-// stage: room for the token's experts, with groups.
-template <class L, int V>
-__device__ __forceinline__ void choose(const RouteArgs& a, int64_t t, double* stage, int& expert, double& score) {
-  const int lane = threadIdx.x & 63, e0 = lane * V;
-  double s[V];
-  scores_of<L, V>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, s);
-  u64 key[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const bool in = e0 + i < a.experts;
-    const double c = a.bias != nullptr && in ? s[i] + (double)a.bias[e0 + i] : s[i];
-    key[i] = in ? key_of(c) : 0;
-    if (stage != nullptr && in) stage[e0 + i] = c;
-  }
-  if (stage != nullptr) {
-    // A lane takes a group; its experts are read from a place of its own on, so that the
-    // lanes' reads spread over the banks.  A NaN counts as the lowest value.
-    __builtin_amdgcn_wave_barrier();
-    const int size = a.experts / a.groups;
-    double first = -INFINITY, second = -INFINITY;
-    if (lane < a.groups) {
-      int j = lane % size;
-      for (int i = 0; i < size; ++i) {
-        const double c = stage[lane * size + j];
-        if (c > first) {
-          second = first;
-          first = c;
-        } else if (c > second) {
-          second = c;
-        }
-        j = j + 1 == size ? 0 : j + 1;
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    u64 rank = lane < a.groups ? key_of(size > 1 ? first + second : first) : 0, kept = 0;
-    for (int j = 0; j < a.top_groups; ++j) {
-      const int g = best_lane(rank);
-      kept |= u64(1) << g;
-      if (lane == g) rank = 0;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (e0 + i < a.experts && !(kept >> ((e0 + i) / size) & 1)) key[i] = 0;
-  }
-  expert = -1;
-  score = 0.0;
-  u64 best = 0;
-  double best_score = 0.0;
-  int best_at = 0;
-  auto look = [&]() {
-    best = key[0];
-    best_score = s[0];
-    best_at = 0;
-#pragma unroll
-    for (int i = 1; i < V; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        best_score = s[i];
-        best_at = i;
-      }
-  };
-  look();
-  for (int j = 0; j < a.top; ++j) {
-    const int l = best_lane(best);
-    const int e = l * V + __builtin_amdgcn_readlane(best_at, l);
-    const double v = lane_value(best_score, l);
-    if (lane == j) {
-      expert = e;
-      score = v;
-    }
-    if (lane == l) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i == best_at) key[i] = 0;
-      look();
-    }
-  }
+// LDS of a token: its scores, in whole lanes (before them, where a group's experts are not whole
+// lanes', its c), and what it chose.
+struct Stage {
+  double* score;
+  int* expert;
+};
+
+// Groups of `size` experts that are whole lanes, a power of two of them: their bounds are lanes'.
+__device__ __forceinline__ bool whole_lanes(int size, int v) { return size % v == 0 && (size / v & (size / v - 1)) == 0; }
+
+// One more to the two largest; the two largest of two pairs.
+__device__ __forceinline__ void enter(double& first, double& second, double c) {
+  const double low = fmin(first, c);
+  first = fmax(first, c);
+  second = fmax(second, low);
+}
+__device__ __forceinline__ void merge(double& first, double& second, double a, double b) {
+  const double low = fmin(first, a);
+  first = fmax(first, a);
+  second = fmax(low, fmax(second, b));
 }
 
-// One token by one wave: its weights and experts.  Returns lane j's expert, or -1.
-template <class L, int V>
-__device__ __forceinline__ int route_token(const RouteArgs& a, int64_t t, double* stage) {
-  const int lane = threadIdx.x & 63;
+// A token's choice to its stage, experts and scores in their order.
+template <class L, int V, int LANES>
+__device__ __forceinline__ void choose(const RouteArgs& a, int64_t t, const Stage& stage) {
+  typedef Lanes<LANES> G;
+  int lane = threadIdx.x & (LANES - 1);
+  asm volatile("" : "+v"(lane));  // (what hangs on it is done where it is needed, not before the loop over tokens)
+  const int e0 = lane * V;
+  double s[V];
+  scores_of<L, V, LANES>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, e0, s);
+  uint32_t hi[V], lo[V];  // of the experts' keys; hi 0: not to be chosen
+  float bias[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) bias[i] = 0.0f;
+  if (a.bias != nullptr) load_neighbours<float, V>(a.bias + e0, a.experts - e0, 0.0f, bias);
+  const int size = a.experts / a.groups, span = size / V;  // experts and lanes of a group
+  const bool whole = whole_lanes(size, V);
+  double first = -INFINITY, second = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const bool in = i < a.experts - e0;
+    double c = a.bias != nullptr ? s[i] + (double)bias[i] : s[i];
+    if (c != c) c = -INFINITY;  // a NaN counts as the lowest value
+    const u64 key = key_of(c);
+    hi[i] = in ? (uint32_t)(key >> 32) : 0u;
+    lo[i] = (uint32_t)key;
+    if (a.groups > 1) {
+      if (whole)
+        enter(first, second, c);  // (lanes beyond the last expert are no group's)
+      else
+        stage.score[e0 + i] = c;
+    }
+  }
+  if (a.groups > 1) {
+    const u64 none = 0;
+    if (whole) {
+      for (int d = 1; d < span; d <<= 1) merge(first, second, __shfl_xor(first, d), __shfl_xor(second, d));
+      u64 rank = (lane & (span - 1)) == 0 && e0 < a.experts ? key_of(size > 1 ? first + second : first) : none;
+      bool kept = false;
+      for (int j = 0; j < a.top_groups; ++j) {
+        const int g = G::best(rank);
+        kept |= lane / span == g / span;
+        if (lane == g) rank = none;
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) hi[i] = kept ? hi[i] : 0u;
+    } else {
+      // A lane takes a group (lanes of a row: every 16th); its experts are read from a place of its
+      // own on, so that the lanes' reads spread over the banks.
+      __builtin_amdgcn_wave_barrier();
+      constexpr int N = kMaxGroups / LANES;
+      u64 rank[N], kept = 0;
+#pragma unroll
+      for (int h = 0; h < N; ++h) {
+        const int g = lane + h * LANES;
+        first = second = -INFINITY;
+        int j = lane % size;
+        for (int i = 0; i < size && g < a.groups; ++i) {
+          enter(first, second, stage.score[g * size + j]);
+          j = j + 1 == size ? 0 : j + 1;
+        }
+        rank[h] = g < a.groups ? key_of(size > 1 ? first + second : first) : none;
+      }
+      __builtin_amdgcn_wave_barrier();
+      for (int j = 0; j < a.top_groups; ++j) {
+        u64 best = rank[0];
+        int at = 0;
+#pragma unroll
+        for (int h = 1; h < N; ++h)
+          if (rank[h] > best) {
+            best = rank[h];
+            at = h;
+          }
+        // groups ascend by h first: of equal ones the lowest h counts, then the lane
+        int g = lane + at * LANES;
+        if constexpr (N > 1) {
+          const int l = G::best(best);
+          const u64 most = __shfl(best, (threadIdx.x & 63 & ~(LANES - 1)) + l);
+          int low = best == most ? g : kMaxGroups;
+#pragma unroll
+          for (int d = LANES / 2; d > 0; d >>= 1) low = min(low, __shfl_xor(low, d));
+          if (g == low && best == most) {
+#pragma unroll
+            for (int h = 0; h < N; ++h)
+              if (h == at) rank[h] = none;
+          }
+          g = low;
+        } else {
+          g = G::best(best);
+          if (lane == g) rank[0] = none;
+        }
+        kept |= u64(1) << g;
+      }
+      int g = e0 / size, in = e0 - g * size;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (!(kept >> min(g, kMaxGroups - 1) & 1)) hi[i] = 0u;
+        g += ++in == size;
+        in = in == size ? 0 : in;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) stage.score[e0 + i] = s[i];
+  auto largest = [&]() {
+    uint32_t m = hi[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) m = max(m, hi[i]);
+    return m;
+  };
+  uint32_t most = largest();
+  for (int j = 0; j < a.top; ++j) {
+    // By the high words alone, unless they leave several lanes, or several of a lane's experts
+    const uint32_t top = G::largest_word(most);
+    u64 who = __ballot(most == top);
+    int at = 0, same = 0;
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i) {
+      const bool is = hi[i] == top;
+      at = is ? i : at;
+      same += is;
+    }
+    if (G::several(who) || __ballot(same > 1) != 0) {
+      u64 best = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const u64 key = (u64)hi[i] << 32 | lo[i];
+        if (hi[i] != 0 && key > best) {
+          best = key;
+          at = i;
+        }
+      }
+      who = u64(1) << ((threadIdx.x & 63 & ~(LANES - 1)) + G::best(best));
+    }
+    if (lane == G::lowest(who)) {
+      stage.expert[j] = e0 + at;
+#pragma unroll
+      for (int i = 0; i < V; ++i) hi[i] = i == at ? 0u : hi[i];
+      most = largest();
+    }
+  }
+  __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses are served in order)
+}
+
+// Tokens t0 on, one for each LANES lanes of a wave (those from `end` on: none): weights and
+// experts; `count`: LDS numbers of the experts' slots, or null.
+template <class L, int V, int LANES>
+__device__ __forceinline__ void route_tokens(const RouteArgs& a, int64_t t0, int64_t end, const Stage& stage, int* count) {
+  typedef Lanes<LANES> G;
+  const int lane = threadIdx.x & (LANES - 1);
+  const int64_t t = t0 + (threadIdx.x & 63) / LANES;
+  const bool there = t < end, live = there && (a.mask == nullptr || a.mask[t] != 0);
+  // (a token that is not there is routed as the last one that is, to no effect)
+  choose<L, V, LANES>(a, there ? t : end - 1, stage);
   int e = -1;
   double s = 0.0;
-  if (a.mask == nullptr || a.mask[t] != 0) choose<L, V>(a, t, stage, e, s);
+  if (live && lane < a.top) {
+    e = stage.expert[lane];
+    s = stage.score[e];
+  }
   double w = s;
   if (a.renormalise) {
-    const double sum = wave_sum(s);
+    const double sum = G::sum(s);
     w = sum == 0.0 ? 0.0 : s / sum;
   }
-  if (lane < a.top) {
+  if (there && lane < a.top) {
     a.weights[t * a.top + lane] = (float)(w * a.scale);
     a.chosen[t * a.top + lane] = e;
+    if (count != nullptr && e >= 0) atomicAdd(&count[e], 1);  // (LDS; sums of ones in any order)
   }
-  return e;
 }
 
 // ---------------------------------------------------------------- the sort
@@ -307,31 +486,38 @@ __host__ __device__ inline int64_t chunk_tokens(int64_t tokens) {
   return least < kRouteWaves ? kRouteWaves : least;
 }
 
+// LDS of the choosing waves: scores, then choices.
+__host__ __device__ inline size_t stage_bytes(int waves, int lanes, int v, int top) {
+  return (size_t)waves * (64 / lanes) * ((size_t)lanes * v * 8 + (size_t)top * 4);
+}
+template <int LANES, int V>
+__device__ __forceinline__ Stage stage_of(char* lds, int waves, int top) {
+  const int tokens = waves * (64 / LANES), k = threadIdx.x / LANES;
+  return {(double*)lds + k * (LANES * V), (int*)((double*)lds + tokens * (LANES * V)) + k * top};
+}
+
 // CHOOSE: route the chunk's tokens; else their experts are there.  counts: experts x
 // chunks (null: no sort).
-template <class L, int V, bool CHOOSE>
-__global__ __launch_bounds__(64 * kRouteWaves) void k_route(RouteArgs a, int64_t per, int* counts) {
+template <class L, int V, int LANES, bool CHOOSE>
+__global__ __launch_bounds__(64 * kRouteWaves, 4) void k_route(RouteArgs a, int64_t per, int* counts) {
   extern __shared__ __align__(16) char lds[];
-  double* stages = (double*)lds;
-  int* count = (int*)(lds + (CHOOSE && a.groups > 1 ? (size_t)kRouteWaves * a.experts * 8 : 0));
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int* count = (int*)(lds + (CHOOSE ? stage_bytes(kRouteWaves, LANES, V, a.top) : 0));
   const int64_t t0 = blockIdx.x * per, t1 = min(a.tokens, t0 + per);
   if (counts != nullptr) {
     for (int i = threadIdx.x; i < a.experts; i += 64 * kRouteWaves) count[i] = 0;
     __syncthreads();
   }
   if (CHOOSE) {
-    for (int64_t t = t0 + wave; t < t1; t += kRouteWaves) {
-      const int e = route_token<L, V>(a, t, a.groups > 1 ? stages + wave * a.experts : nullptr);
-      if (counts != nullptr && taken(e, a.experts)) atomicAdd(&count[e], 1);
-    }
+    const Stage stage = stage_of<LANES, V>(lds, kRouteWaves, a.top);
+    constexpr int kEach = 64 / LANES;
+    for (int64_t t = t0 + (threadIdx.x >> 6) * kEach; t < t1; t += kRouteWaves * kEach)
+      route_tokens<L, V, LANES>(a, t, t1, stage, counts != nullptr ? count : nullptr);
   } else {
     for (int64_t s = t0 * a.top + threadIdx.x; s < t1 * a.top; s += 64 * kRouteWaves) {
       const int e = a.chosen[s];
       if (taken(e, a.experts)) atomicAdd(&count[e], 1);
     }
   }
-  (void)lane;
   if (counts == nullptr) return;
   __syncthreads();
   for (int e = threadIdx.x; e < a.experts; e += 64 * kRouteWaves)
@@ -382,16 +568,16 @@ __global__ __launch_bounds__(64 * kPlaceWaves) void k_place(RouteArgs a, int64_t
 }
 
 // Few tokens: all of it in one workgroup.
-template <class L, int V, bool CHOOSE>
+template <class L, int V, int LANES, bool CHOOSE>
 __global__ __launch_bounds__(512) void k_route_few(RouteArgs a) {
   extern __shared__ __align__(16) char lds[];
-  double* stages = (double*)lds;
-  int* count = (int*)(lds + (CHOOSE && a.groups > 1 ? (size_t)8 * a.experts * 8 : 0));
+  int* count = (int*)(lds + (CHOOSE ? stage_bytes(8, LANES, V, a.top) : 0));
   __shared__ int start[kMaxExperts + 1], sums[8];
-  const int wave = threadIdx.x >> 6;
   if (CHOOSE) {
-    for (int64_t t = wave; t < a.tokens; t += 8)
-      route_token<L, V>(a, t, a.groups > 1 ? stages + wave * a.experts : nullptr);
+    const Stage stage = stage_of<LANES, V>(lds, 8, a.top);
+    constexpr int kEach = 64 / LANES;
+    for (int64_t t = (threadIdx.x >> 6) * kEach; t < a.tokens; t += 8 * kEach)
+      route_tokens<L, V, LANES>(a, t, a.tokens, stage, nullptr);
     if (a.order == nullptr) return;
     __threadfence_block();  // the experts are read by other waves from here on
   }
@@ -418,7 +604,7 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
   const int lane = threadIdx.x & 63, e0 = lane * V;
   for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += (int64_t)gridDim.x * 4) {
     double s[V], d[V];
-    scores_of<L, V>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, s);
+    scores_of<L, V, 64>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, e0, s);
 #pragma unroll
     for (int i = 0; i < V; ++i) d[i] = 0.0;
     // lane j has the j-th choice
@@ -479,20 +665,20 @@ bool fits(const RouteArgs& a) {
          a.tokens * a.top <= (int64_t(1) << 30);
 }
 
-template <class L, int V, bool CHOOSE>
+template <class L, int V, int LANES, bool CHOOSE>
 hipError_t route_for(const RouteArgs& a, void* workspace, hipStream_t s) {
-  const bool sort = a.order != nullptr, groups = CHOOSE && a.groups > 1;
+  const bool sort = a.order != nullptr;
   if (few(a.tokens, a.top)) {
-    const size_t lds = (groups ? (size_t)8 * a.experts * 8 : 0) + (size_t)8 * a.experts * 4;
-    hipLaunchKernelGGL((k_route_few<L, V, CHOOSE>), dim3(1), dim3(512), lds, s, a);
+    const size_t lds = (CHOOSE ? stage_bytes(8, LANES, V, a.top) : 0) + (size_t)8 * a.experts * 4;
+    hipLaunchKernelGGL((k_route_few<L, V, LANES, CHOOSE>), dim3(1), dim3(512), lds, s, a);
     return hipGetLastError();
   }
   const int64_t per = chunk_tokens(a.tokens);
   const int chunks = chunks_of(a.tokens);
   if (sort && workspace == nullptr) return hipErrorInvalidValue;
   int *counts = sort ? (int*)workspace : nullptr, *totals = counts + (sort ? (size_t)chunks * a.experts : 0);
-  const size_t lds = (groups ? (size_t)kRouteWaves * a.experts * 8 : 0) + (size_t)a.experts * 4;
-  hipLaunchKernelGGL((k_route<L, V, CHOOSE>), dim3(chunks), dim3(64 * kRouteWaves), lds, s, a, per, counts);
+  const size_t lds = (CHOOSE ? stage_bytes(kRouteWaves, LANES, V, a.top) : 0) + (size_t)a.experts * 4;
+  hipLaunchKernelGGL((k_route<L, V, LANES, CHOOSE>), dim3(chunks), dim3(64 * kRouteWaves), lds, s, a, per, counts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sort) return e;
   hipLaunchKernelGGL(k_scan, dim3((a.experts + 3) / 4), dim3(256), 0, s, counts, totals, a.experts, chunks);
@@ -512,15 +698,21 @@ hipError_t launch_route(const RouteArgs& a, void* workspace, hipStream_t s) {
   if (!fits(a) || a.top > a.experts || a.groups < 1 || a.groups > kMaxGroups || a.experts % a.groups != 0 ||
       a.top_groups < 1 || a.top_groups > a.groups || a.top > a.top_groups * (a.experts / a.groups))
     return hipErrorInvalidValue;
+  // rows of 16 lanes: up to 16 experts a lane, a lane for each choice
+  if (a.experts <= 256 && a.top <= 16)
+    return for_experts(4 * a.experts, [&](auto v) {
+      constexpr int V = decltype(v)::value;
+      return a.bf16 ? route_for<bf16_t, V, 16, true>(a, workspace, s) : route_for<float, V, 16, true>(a, workspace, s);
+    });
   return for_experts(a.experts, [&](auto v) {
     constexpr int V = decltype(v)::value;
-    return a.bf16 ? route_for<bf16_t, V, true>(a, workspace, s) : route_for<float, V, true>(a, workspace, s);
+    return a.bf16 ? route_for<bf16_t, V, 64, true>(a, workspace, s) : route_for<float, V, 64, true>(a, workspace, s);
   });
 }
 
 hipError_t launch_order(const RouteArgs& a, void* workspace, hipStream_t s) {
   if (!fits(a) || a.order == nullptr) return hipErrorInvalidValue;
-  return route_for<float, 1, false>(a, workspace, s);
+  return route_for<float, 1, 64, false>(a, workspace, s);
 }
 
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s) {
