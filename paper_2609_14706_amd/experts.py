@@ -17,7 +17,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from .binding import load_library
-from .layer import (Checkpoint, _act, _bytes, _elem, _first, _i64, _int, _f64, _launch, _like, _on_stream, _ptr,
+from .layer import (Checkpoint, _act, _bytes, _elem, _first, _i64, _int, _f64, _launch, _like, _matrix_of, _on_stream, _ptr,
                     _q8_rows, _refuse, _rows, _size, _vector, _workspace, ff_q8_rows)
 
 FF_SCORE_SOFTMAX, FF_SCORE_SIGMOID = 0, 1
@@ -129,13 +129,18 @@ def _slots(t, name, dtype, device, shape):
     return p
 
 
-def _new_routing(a, tokens, experts, top, dev):
-    """order, offsets and place for args a; what has to live until its launch."""
-    i32 = torch.int32
-    order, place = torch.empty(tokens * top, dtype=i32, device=dev), torch.empty((tokens, top), dtype=i32, device=dev)
-    offsets = torch.empty(experts + 1, dtype=i32, device=dev)
-    a.order, a.offsets, a.place = order.data_ptr(), offsets.data_ptr(), place.data_ptr()
-    return order, offsets, place
+def _new_routing(a, tokens, experts, top, dev, choose):
+    """experts (with choose), place, order and offsets of one allocation, for args a."""
+    slots = tokens * top
+    sizes = [slots, slots, slots, experts + 1] if choose else [slots, slots, experts + 1]
+    all_ = torch.empty_strided((sum(sizes),), (1,), dtype=torch.int32, device=dev)
+    parts, at = all_.split_with_sizes(sizes), all_.data_ptr()
+    chosen = None
+    if choose:
+        chosen, parts, a.chosen = parts[0].view(tokens, top), parts[1:], at
+        at += 4 * slots
+    a.place, a.order, a.offsets = at, at + 4 * slots, at + 8 * slots
+    return chosen, parts[1], parts[2], parts[0].view(tokens, top)
 
 
 def route(logits, top: int, *, score: str = "softmax", bias=None, groups: int = 1, top_groups: int = 1,
@@ -155,13 +160,11 @@ def route(logits, top: int, *, score: str = "softmax", bias=None, groups: int = 
     dt = _elem(logits, "logits")
     p, ld, T, E = _matrix(logits, "logits", logits.dtype, dev)
     top = _count(top, "top")
-    weights = torch.empty((T, top), dtype=torch.float32, device=dev)
-    experts = torch.empty((T, top), dtype=torch.int32, device=dev)
+    weights = _matrix_of(T, top, torch.float32, dev)
     a = ff_route_args(T, E, top, dt, p, ld, _vector(bias, "bias", torch.float32, dev, E),
                       _vector(mask, "mask", torch.bool, dev, T), _score(score), _count(groups, "groups"),
-                      _count(top_groups, "top_groups"), 1 if renormalise else 0, scale, weights.data_ptr(),
-                      experts.data_ptr())
-    order, offsets, place = _new_routing(a, T, E, top, dev)
+                      _count(top_groups, "top_groups"), 1 if renormalise else 0, scale, weights.data_ptr())
+    experts, order, offsets, place = _new_routing(a, T, E, top, dev, True)
     keep = _workspace(a, _bytes("ff_route_workspace_size", a, functions=_FN), workspace, dev)
     _launch("ff_route", a, dev, _FN)
     del keep
@@ -184,7 +187,7 @@ def expert_order(experts, num_experts: int, *, weights=None, workspace=None, str
     T, top = experts.shape
     a = ff_route_args(T, _count(num_experts, "num_experts"), top)
     a.chosen = p
-    order, offsets, place = _new_routing(a, T, num_experts, top, dev)
+    _, order, offsets, place = _new_routing(a, T, num_experts, top, dev, False)
     keep = _workspace(a, _bytes("ff_route_workspace_size", a, functions=_FN), workspace, dev)
     _launch("ff_expert_order", a, dev, _FN)
     del keep
@@ -205,7 +208,7 @@ def route_backward(dweights, logits, experts, *, score: str = "softmax", renorma
     p, ld, T, E = _matrix(logits, "logits", logits.dtype, dev)
     if not isinstance(experts, torch.Tensor) or experts.dim() != 2 or experts.shape[0] != T:
         raise ValueError(f"experts must be a tensor of shape ({T}, top)")
-    out = _like(logits, logits.dtype)
+    out = _matrix_of(T, E, logits.dtype, dev)
     a = ff_route_grad_args(T, E, experts.shape[1], dt, p, ld,
                            _slots(dweights, "dweights", torch.float32, dev, experts.shape),
                            _slots(experts, "experts", torch.int32, dev, experts.shape), _score(score),
@@ -278,8 +281,9 @@ def expert_linear(x, weight, routing, *, bias=None, activation: str = "none", ke
     r = _routing(routing, dev)
     px, ldx, n = _slot_rows(x, "x", bf16, dev, r, by_slot)
     pw, ldw, m, _ = _weights(weight, dev, r.experts, n)
-    y = torch.empty((r.tokens * r.top, m), dtype=bf16, device=dev)
-    z = torch.empty_like(y) if keep_preact else None
+    rows = r.tokens * r.top
+    y = _matrix_of(rows, m, bf16, dev)
+    z = _matrix_of(rows, m, bf16, dev) if keep_preact else None
     a = ff_expert_linear_args(r, n, m, px, ldx, 1 if by_slot else 0, pw, ldw, _bias(bias, dev, r.experts, m),
                               _act(activation), y.data_ptr(), m, z.data_ptr() if keep_preact else None, m)
     if r.tokens:
@@ -302,7 +306,7 @@ def expert_combine(y, routing, *, residual=None, stream=None):
     pr = ldr = 0
     if residual is not None:
         pr, ldr, _ = _slot_rows(residual, "residual", torch.bfloat16, dev, r, False, m)
-    out = torch.empty((r.tokens, m), dtype=torch.bfloat16, device=dev)
+    out = _matrix_of(r.tokens, m, torch.bfloat16, dev)
     if r.tokens:
         _launch("ff_expert_combine", ff_expert_combine_args(r, m, py, ldy, pr, ldr, out.data_ptr(), m), dev, _FN)
     return out
@@ -327,10 +331,10 @@ def expert_combine_backward(dout, y, routing, *, need_rows: bool = True, need_we
     dy = dweights = None
     if need_weights:
         a.y, a.ldy, _ = _slot_rows(y, "y", torch.bfloat16, dev, r, True, m)
-        dweights = torch.empty((r.tokens, r.top), dtype=torch.float32, device=dev)
+        dweights = _matrix_of(r.tokens, r.top, torch.float32, dev)
         a.dweights = dweights.data_ptr()
     if need_rows:
-        dy = torch.empty((r.tokens * r.top, m), dtype=torch.float32, device=dev)
+        dy = _matrix_of(r.tokens * r.top, m, torch.float32, dev)
         a.dy, a.lddy = dy.data_ptr(), m
     if r.tokens:
         _launch("ff_expert_combine_backward", a, dev, _FN)
@@ -380,17 +384,17 @@ def expert_linear_backward(dy, x, weight, routing, *, preact=None, activation: s
             a.preact_q8, _ = kept(preact, "preact", r.tokens * r.top, m)
         else:
             a.preact, a.ldz, _ = _slot_rows(preact, "preact", bf16, dev, r, True, m)
-    g = torch.empty((r.tokens * r.top, m), dtype=bf16, device=dev)
+    g = _matrix_of(r.tokens * r.top, m, bf16, dev)
     a.g, a.ldg = g.data_ptr(), m
     dx = dw = db = None
     if need_input:
-        dx = torch.empty((X, n), dtype=bf16, device=dev)
+        dx = _matrix_of(X, n, bf16, dev)
         a.dx, a.lddx = dx.data_ptr(), n
     if need_weight:
         dw = torch.empty_like(weight)
         a.dw, a.lddw = dw.data_ptr(), n
     if need_bias:
-        db = torch.empty((r.experts, m), dtype=bf16, device=dev)
+        db = _matrix_of(r.experts, m, bf16, dev)
         a.db = db.data_ptr()
     keep = _workspace(a, _bytes("ff_expert_linear_backward_workspace_size", a, functions=_FN), workspace, dev)
     _launch("ff_expert_linear_backward", a, dev, _FN)
