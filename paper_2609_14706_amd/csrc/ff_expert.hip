@@ -144,11 +144,20 @@ __device__ __forceinline__ void clear_outputs(const ExpertArgs& x, uint32_t extr
   if (x.lin.preact != nullptr) clear_rows(x.at, x.lin.preact, x.lin.ldz, x.lin.m, extra, extras);
 }
 
+// An expert's last tile takes half the height where that holds its rows: of 64 experts
+// with 256 rows in the mean a quarter of the tiles' rows were none (4096 -> 2048: 384 us, 372 so).
+constexpr int half_of(int ti) { return ti >= 4 && ti % 4 == 0 ? ti / 2 : ti; }
+constexpr int half_slots(int ti, int slots) { return ti == 8 ? 3 : slots; }
+
 template <int TI, int TJ, int SLOTS, bool GATHER>
 __global__ __launch_bounds__(nt::kThreads, (LinearTile<nt::Bf16, TI, TJ, SLOTS>::kWaves)) void k_expert_tile(
     ExpertArgs x, uint32_t cols) {
   typedef LinearTile<nt::Bf16, TI, TJ, SLOTS> L;
-  __shared__ typename L::Shared all;
+  typedef LinearTile<nt::Bf16, half_of(TI), TJ, half_slots(TI, SLOTS)> H;
+  __shared__ union {
+    typename L::Shared whole;
+    typename H::Shared half;
+  } all;
   GroupTile g;
   uint32_t extra, extras;
   if (!find_tile(x.at, L::G::BM, cols, blockIdx.x, gridDim.x, g, extra, extras)) {
@@ -156,8 +165,11 @@ __global__ __launch_bounds__(nt::kThreads, (LinearTile<nt::Bf16, TI, TJ, SLOTS>:
     return;
   }
   const LinearArgs a = args_of(x, g);
-  L::template run<GATHER>(all, a, 0, (int64_t)g.col * L::G::BN, 0, 1, nullptr, x.at.order + g.row0, x.at.top,
-                          x.at.tokens);
+  const int64_t i0 = (int64_t)g.col * L::G::BN;
+  if (half_of(TI) < TI && g.rows <= H::G::BM)
+    H::template run<GATHER>(all.half, a, 0, i0, 0, 1, nullptr, x.at.order + g.row0, x.at.top, x.at.tokens);
+  else
+    L::template run<GATHER>(all.whole, a, 0, i0, 0, 1, nullptr, x.at.order + g.row0, x.at.top, x.at.tokens);
 }
 
 template <int NT, int RW, int WAVES, bool GATHER>
@@ -572,34 +584,55 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
   }
 }
 
-// k in `splits` parts: the workgroups of part z are z-th in each XCD's share of the launch.
+// A tile of dx by workgroup w of `grid`, k in `splits` parts.
 template <int TI, int TJ, int SLOTS>
-__global__ __launch_bounds__(nt::kThreads, (kn::Tile<nt::Bf16, false, TI, TJ, SLOTS>::kWaves)) void k_expert_dx(
-    ExpertGradArgs a, uint32_t cols, uint32_t splits) {
+struct DxTile {
   typedef kn::Tile<nt::Bf16, false, TI, TJ, SLOTS> G;
-  __shared__ typename G::Ring ring;
-  GroupTile g;
-  uint32_t extra, extras;
-  if (!find_tile(a.at, G::BM, cols * splits, blockIdx.x, gridDim.x, g, extra, extras)) {
-    if (a.out_f32)
-      for (uint32_t z = 0; z < splits; ++z) clear_rows(a.at, (float*)a.out + z * a.part_stride, a.ldo, a.n, extra, extras);
+  typedef kn::Tile<nt::Bf16, false, half_of(TI), TJ, half_slots(TI, SLOTS)> H;
+  union Shared {
+    typename G::Ring whole;
+    typename H::Ring half;
+  };
+  static __device__ __forceinline__ void run(Shared& rings, const ExpertGradArgs& a, uint32_t cols, uint32_t splits, uint32_t w,
+                                             uint32_t grid) {
+    GroupTile g;
+    uint32_t extra, extras;
+    if (!find_tile(a.at, G::BM, cols * splits, w, grid, g, extra, extras)) {
+      if (a.out_f32)
+        for (uint32_t z = 0; z < splits; ++z) clear_rows(a.at, (float*)a.out + z * a.part_stride, a.ldo, a.n, extra, extras);
+      else
+        clear_rows(a.at, (uint16_t*)a.out, a.ldo, a.n, extra, extras);
+      return;
+    }
+    const uint32_t z = g.col / cols;
+    const int64_t n0 = (int64_t)(g.col - z * cols) * G::BN;
+    const int64_t pairs = (a.m + kn::kK - 1) / kn::kK, k0 = pairs * z / splits * kn::kK;
+    const int64_t k1 = min(a.m, pairs * (z + 1) / splits * kn::kK);
+    const kn::Side P{(const char*)(a.g + g.row0 * a.ldg + k0), g.rows, (uint32_t)(a.ldg * 2)};
+    const kn::Side Q{(const char*)(a.w + ((int64_t)g.expert * a.m + k0) * a.ldw + n0), a.n - n0, (uint32_t)(a.ldw * 2)};
+    auto one = [&](auto& ring, auto tile) {
+      typedef decltype(tile) T;
+      typename T::Acc acc;
+      T::zero(acc);
+      T::loop(ring, P, Q, k1 - k0, acc);
+      if (a.out_f32)
+        store_tile<T>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
+      else
+        store_tile<T>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
+    };
+    if (half_of(TI) < TI && g.rows <= H::BM)
+      one(rings.half, H());
     else
-      clear_rows(a.at, (uint16_t*)a.out, a.ldo, a.n, extra, extras);
-    return;
+      one(rings.whole, G());
   }
-  const uint32_t z = g.col / cols;
-  const int64_t n0 = (int64_t)(g.col - z * cols) * G::BN;
-  const int64_t pairs = (a.m + kn::kK - 1) / kn::kK, k0 = pairs * z / splits * kn::kK;
-  const int64_t k1 = min(a.m, pairs * (z + 1) / splits * kn::kK);
-  const kn::Side P{(const char*)(a.g + g.row0 * a.ldg + k0), g.rows, (uint32_t)(a.ldg * 2)};
-  const kn::Side Q{(const char*)(a.w + ((int64_t)g.expert * a.m + k0) * a.ldw + n0), a.n - n0, (uint32_t)(a.ldw * 2)};
-  typename G::Acc acc;
-  G::zero(acc);
-  G::loop(ring, P, Q, k1 - k0, acc);
-  if (a.out_f32)
-    store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
-  else
-    store_tile<G>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
+};
+
+template <int TI, int TJ, int SLOTS>
+__global__ __launch_bounds__(nt::kThreads, (DxTile<TI, TJ, SLOTS>::G::kWaves)) void k_expert_dx(ExpertGradArgs a, uint32_t cols,
+                                                                                                uint32_t splits) {
+  typedef DxTile<TI, TJ, SLOTS> D;
+  __shared__ typename D::Shared rings;
+  D::run(rings, a, cols, splits, blockIdx.x, gridDim.x);
 }
 
 // An expert's column sums from those of its parts: the column of each thread.
@@ -618,42 +651,65 @@ __global__ __launch_bounds__(256) void k_expert_db(ExpertGradArgs a) {
   if (col < a.m) sum_column(a, blockIdx.y, row0, rows, col);
 }
 
-// Every XCD takes an eighth of each expert's tiles: their work is the expert's rows,
-// and with whole experts to an XCD the fullest one's kept the others waiting (8 experts of 422 to 2247
-// rows, 4096 x 4096: 480 us, 292 so).  The tiles of the first columns add up db as well.
+// A tile of dW by workgroup w.  Every XCD takes an eighth of each expert's tiles: their work is the
+// expert's rows, and with whole experts to an XCD the fullest one's kept the others waiting (8 experts of
+// 422 to 2247 rows, 4096 x 4096: 480 us, 292 so).  The tiles of the first columns add up db as well.
+template <class T, int TI, int TJ, int SLOTS>
+struct DwTile {
+  typedef kn::Tile<T, true, TI, TJ, SLOTS> G;
+  static __device__ __forceinline__ void run(typename G::Ring& ring, const ExpertGradArgs& a, uint32_t mt, uint32_t ntl,
+                                             uint32_t splits, uint32_t w) {
+    const uint32_t tiles = mt * ntl * splits, share = (tiles + 7) / 8, local = w >> 3, e = local / share;
+    const uint32_t tile = (w & 7) * share + (local - e * share);
+    if (tile >= tiles) return;
+    const uint32_t z = tile / (mt * ntl);
+    uint32_t ti, tj;
+    tile_at(tile - z * (mt * ntl), mt, ntl, ti, tj);
+    const int64_t m0 = (int64_t)ti * G::BM, n0 = (int64_t)tj * G::BN;
+    int64_t row0;
+    const int64_t rows = expert_rows(a.at, (int)e, row0);
+    const int64_t pairs = (rows + kn::kK - 1) / kn::kK, k0 = pairs * z / splits * kn::kK;
+    const int64_t k1 = min(rows, pairs * (z + 1) / splits * kn::kK);
+    const kn::Side P{(const char*)(a.g + (row0 + k0) * a.ldg + m0), a.m - m0, (uint32_t)(a.ldg * 2)};
+    const kn::Side Q{(const char*)(a.x + (row0 + k0) * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
+    const float f1 = a.f16 ? a.inverse[0] : 1.0f, f2 = a.f16 ? a.inverse[1] : 1.0f;
+    if (a.db != nullptr && tj == 0 && z == 0 && threadIdx.x < G::BM && m0 + threadIdx.x < a.m)
+      sum_column(a, e, row0, rows, m0 + threadIdx.x);
+    typename G::Acc acc;
+    G::zero(acc);
+    if (k1 > k0) G::loop(ring, P, Q, k1 - k0, acc);
+    const int64_t at = ((int64_t)e * a.m + m0) * a.ldo + n0;
+    if (a.out_f32)
+      store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+    else
+      store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+  }
+};
+
 template <class T, int TI, int TJ, int SLOTS>
 __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kWaves)) void k_expert_dw(
     ExpertGradArgs a, uint32_t mt, uint32_t ntl, uint32_t splits) {
-  typedef kn::Tile<T, true, TI, TJ, SLOTS> G;
-  __shared__ typename G::Ring ring;
-  const uint32_t tiles = mt * ntl * splits, share = (tiles + 7) / 8, local = blockIdx.x >> 3, e = local / share;
-  const uint32_t tile = (blockIdx.x & 7) * share + (local - e * share);
-  if (tile >= tiles) return;
-  const uint32_t z = tile / (mt * ntl);
-  uint32_t ti, tj;
-  tile_at(tile - z * (mt * ntl), mt, ntl, ti, tj);
-  const int64_t m0 = (int64_t)ti * G::BM, n0 = (int64_t)tj * G::BN;
-  int64_t row0;
-  const int64_t rows = expert_rows(a.at, (int)e, row0);
-  const int64_t pairs = (rows + kn::kK - 1) / kn::kK, k0 = pairs * z / splits * kn::kK;
-  const int64_t k1 = min(rows, pairs * (z + 1) / splits * kn::kK);
-  const kn::Side P{(const char*)(a.g + (row0 + k0) * a.ldg + m0), a.m - m0, (uint32_t)(a.ldg * 2)};
-  const kn::Side Q{(const char*)(a.x + (row0 + k0) * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
-  float f1 = 1.0f, f2 = 1.0f;
-  if (a.f16) {
-    f1 = a.inverse[0];
-    f2 = a.inverse[1];
-  }
-  if (a.db != nullptr && tj == 0 && z == 0 && threadIdx.x < G::BM && m0 + threadIdx.x < a.m)
-    sum_column(a, e, row0, rows, m0 + threadIdx.x);
-  typename G::Acc acc;
-  G::zero(acc);
-  if (k1 > k0) G::loop(ring, P, Q, k1 - k0, acc);
-  const int64_t at = ((int64_t)e * a.m + m0) * a.ldo + n0;
-  if (a.out_f32)
-    store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+  typedef DwTile<T, TI, TJ, SLOTS> D;
+  __shared__ typename D::G::Ring ring;
+  D::run(ring, a, mt, ntl, splits, blockIdx.x);
+}
+
+// Both gradients in one launch where each alone would leave units empty (the smallest tiles; 1021 tokens,
+// 1000 x 777: 9.5 and 13 us one after the other, 13.8 so).  The first `first` workgroups take dx.
+template <class T, int TI, int TJ, int SLOTS>
+__global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kWaves)) void k_expert_both(
+    ExpertGradArgs x, uint32_t cols, uint32_t x_splits, uint32_t first, ExpertGradArgs w, uint32_t mt, uint32_t ntl,
+    uint32_t w_splits) {
+  typedef DxTile<TI, TJ, SLOTS> X;
+  typedef DwTile<T, TI, TJ, SLOTS> W;
+  __shared__ union {
+    typename X::Shared x;
+    typename W::G::Ring w;
+  } sh;
+  if (blockIdx.x < first)
+    X::run(sh.x, x, cols, x_splits, blockIdx.x, first);
   else
-    store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+    W::run(sh.w, w, mt, ntl, w_splits, blockIdx.x - first);
 }
 
 // ---------------------------------------------------------------------- host
@@ -806,6 +862,15 @@ hipError_t dw_tiles(const ExpertGradArgs& a, int splits, hipStream_t s) {
 // Rows of whole 16-byte pieces (zeros, or nothing that is stored, beyond cols).
 bool laid_ok(const void* p, int64_t ld, int64_t cols) {
   return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld >= laid_ld(cols) && ld * 2 <= nt::kMaxRowBytes;
+}
+
+bool dx_ok(const ExpertGradArgs& a, const ExpertPlan& p) {
+  return fits(a.at) && a.n > 0 && a.m > 0 && laid_ok(a.g, a.ldg, a.m) && laid_ok(a.w, a.ldw, a.n) && p.splits >= 1 &&
+         (p.splits == 1 || a.out_f32);
+}
+bool dw_ok(const ExpertGradArgs& a, const ExpertPlan& p) {
+  return fits(a.at) && a.n > 0 && a.m > 0 && laid_ok(a.g, a.ldg, a.m) && laid_ok(a.x, a.ldx, a.n) && p.splits >= 1 &&
+         (p.splits == 1 || a.out_f32) && (a.db == nullptr || a.parts != nullptr) && (!a.f16 || a.inverse != nullptr);
 }
 
 }  // namespace
@@ -961,9 +1026,7 @@ hipError_t launch_peaks(const PeaksArgs (&jobs)[2], hipStream_t s) {
 }
 
 hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s) {
-  if (!fits(a.at) || a.n <= 0 || a.m <= 0 || !laid_ok(a.g, a.ldg, a.m) || !laid_ok(a.w, a.ldw, a.n) || p.splits < 1 ||
-      (p.splits > 1 && !a.out_f32))
-    return hipErrorInvalidValue;
+  if (!dx_ok(a, p)) return hipErrorInvalidValue;
 #define FF_TILE(I, J, S) \
   if (p.ti == I && p.tj == J && p.slots == S) return dx_tiles<I, J, S>(a, p.splits, s);
   FF_TILE(8, 8, 2) FF_TILE(6, 8, 2) FF_TILE(4, 8, 3) FF_TILE(4, 4, 2) FF_TILE(2, 4, 3)
@@ -972,9 +1035,7 @@ hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
 }
 
 hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s) {
-  if (!fits(a.at) || a.n <= 0 || a.m <= 0 || !laid_ok(a.g, a.ldg, a.m) || !laid_ok(a.x, a.ldx, a.n) || p.splits < 1 ||
-      (p.splits > 1 && !a.out_f32) || (a.db != nullptr && a.parts == nullptr) || (a.f16 && a.inverse == nullptr))
-    return hipErrorInvalidValue;
+  if (!dw_ok(a, p)) return hipErrorInvalidValue;
 #define FF_STREAM(I, J, S)                                                                                   \
   if (p.ti == I && p.tj == J && p.slots == S && p.splits == 1 && !a.out_f32)                                 \
     return a.f16 ? dw_stream<nt::F16, I, J, S>(a, s) : dw_stream<nt::Bf16, I, J, S>(a, s);
@@ -988,6 +1049,23 @@ hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
   FF_TILE(8, 8, 2) FF_TILE(4, 4, 2) FF_TILE(2, 4, 3)
 #undef FF_TILE
   return hipErrorInvalidValue;
+}
+
+bool expert_both(const ExpertPlan& dx, const ExpertPlan& dw) { return dx.ti == 2 && dw.ti == 2; }
+
+hipError_t launch_expert_both(const ExpertGradArgs& x, const ExpertPlan& px, const ExpertGradArgs& w, const ExpertPlan& pw,
+                              hipStream_t s) {
+  if (!dx_ok(x, px) || !dw_ok(w, pw) || !expert_both(px, pw)) return hipErrorInvalidValue;
+  const int64_t cols = (x.n + 127) / 128, first = (grid_for(x.at, 64, cols * px.splits) + 7) / 8 * 8;
+  const int64_t mt = (w.m + 63) / 64, ntl = (w.n + 127) / 128, grid = first + (mt * ntl * pw.splits + 7) / 8 * 8 * w.at.experts;
+  if (grid > kMaxGrid) return hipErrorInvalidValue;
+  if (w.f16)
+    hipLaunchKernelGGL((k_expert_both<nt::F16, 2, 4, 3>), dim3((uint32_t)grid), dim3(nt::kThreads), 0, s, x, (uint32_t)cols,
+                       (uint32_t)px.splits, (uint32_t)first, w, (uint32_t)mt, (uint32_t)ntl, (uint32_t)pw.splits);
+  else
+    hipLaunchKernelGGL((k_expert_both<nt::Bf16, 2, 4, 3>), dim3((uint32_t)grid), dim3(nt::kThreads), 0, s, x, (uint32_t)cols,
+                       (uint32_t)px.splits, (uint32_t)first, w, (uint32_t)mt, (uint32_t)ntl, (uint32_t)pw.splits);
+  return hipGetLastError();
 }
 
 hipError_t launch_expert_db(const ExpertGradArgs& a, hipStream_t s) {

@@ -183,6 +183,10 @@ hipError_t launch_expert_dx(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
 // dW_e = sum over the rows of expert e of g_p^T x_p (m x n; zeros for an expert without rows).
 ExpertPlan expert_dw_plan(int64_t rows, int experts, int64_t n, int64_t m);
 hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStream_t s);
+// Both in one launch, for plans that leave units empty.
+bool expert_both(const ExpertPlan& dx, const ExpertPlan& dw);
+hipError_t launch_expert_both(const ExpertGradArgs& x, const ExpertPlan& px, const ExpertGradArgs& w, const ExpertPlan& pw,
+                              hipStream_t s);
 // db_e = sum over the rows of expert e of g_p, from the parts alone.
 hipError_t launch_expert_db(const ExpertGradArgs& a, hipStream_t s);
 

@@ -201,7 +201,7 @@ struct Gradient {
 struct GradWs {
   ExpertPlan dx, dw;
   bool dy_is_g, lay_g, scale, lay_x, lay_w, sum_dx;
-  size_t off_g, off_g16, off_x, off_peaks, off_w, off_parts, off_sum, bytes;
+  size_t off_g, off_g16, off_x, off_peaks, off_w, off_parts, off_sum_x, off_sum_w, bytes;
 };
 
 GradWs grad_ws(const Gradient& a) {
@@ -214,7 +214,7 @@ GradWs grad_ws(const Gradient& a) {
   w.lay_g = (dx || (dw && !w.scale)) && !w.dy_is_g && (a.g == nullptr || !tile_rows_ok(a.g, a.ldg, a.m, 2));
   w.lay_x = dw && !w.scale && (a.gather || !tile_rows_ok(a.x, a.ldx, a.n, 2));
   w.lay_w = dx && !tile_rows_ok(a.w, a.ldw, a.n, 2);
-  size_t off = 0, sum = 0;
+  size_t off = 0;
   auto take = [&](bool need, size_t bytes) {
     const size_t at = off;
     if (need) off += up256(bytes);
@@ -229,13 +229,12 @@ GradWs grad_ws(const Gradient& a) {
   if (dx) {
     w.dx = expert_dx_plan(S, (int)E, a.n, a.m);
     w.sum_dx = a.gather || w.dx.splits > 1;
-    if (w.sum_dx) sum = (size_t)w.dx.splits * (size_t)S * (size_t)laid_ld(a.n) * 4;
+    w.off_sum_x = take(w.sum_dx, (size_t)w.dx.splits * (size_t)S * (size_t)laid_ld(a.n) * 4);
   }
   if (dw) {
     w.dw = expert_dw_plan(S, (int)E, a.n, a.m);
-    if (w.dw.splits > 1) sum = std::max(sum, (size_t)w.dw.splits * (size_t)E * (size_t)a.m * (size_t)laid_ld(a.n) * 4);
+    w.off_sum_w = take(w.dw.splits > 1, (size_t)w.dw.splits * (size_t)E * (size_t)a.m * (size_t)laid_ld(a.n) * 4);
   }
-  w.off_sum = take(sum > 0, sum);
   w.bytes = off;
   return w;
 }
@@ -341,45 +340,47 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
   k.parts = r.parts;
   k.part_rows = part_rows(S, a.m);
   if (a.db != nullptr && a.dw == nullptr && (rc = hip(launch_expert_db(k, s), "bias gradient")) != FF_OK) return rc;
-  if (a.dx != nullptr) {
-    float* sum = (float*)(ws + w.off_sum);
-    k.out_f32 = w.sum_dx;
-    k.out = w.sum_dx ? (void*)sum : a.dx;
-    k.ldo = w.sum_dx ? laid_ld(a.n) : a.lddx;
-    k.part_stride = S * k.ldo;
-    if ((rc = hip(launch_expert_dx(k, w.dx, s), "input gradient")) != FF_OK) return rc;
-    if (a.gather) {
-      // a token's rows in fp32 until they are summed: a rounding of each would add to g's and dx's own
-      CombineArgs c{};
-      c.at = k.at;
-      c.at.weights = nullptr;
-      c.cols = a.n;
-      c.y = sum;
-      c.ldy = k.ldo;
-      c.f32 = true;
-      c.parts = w.dx.splits;
-      c.part_stride = k.part_stride;
-      c.out = (bf16_t*)a.dx;
-      c.ldo = a.lddx;
-      if ((rc = hip(launch_combine(c, s), "input gradient's sums")) != FF_OK) return rc;
-    } else if (w.sum_dx && (rc = sum_parts(sum, w.dx.splits, S, a.n, a.dx, a.lddx, s)) != FF_OK) {
-      return rc;
-    }
-  }
-  if (a.dw == nullptr) return FF_OK;
+  ExpertGradArgs x = k;
+  float *sum_x = (float*)(ws + w.off_sum_x), *sum_w = (float*)(ws + w.off_sum_w);
+  x.out_f32 = w.sum_dx;
+  x.out = w.sum_dx ? (void*)sum_x : a.dx;
+  x.ldo = w.sum_dx ? laid_ld(a.n) : a.lddx;
+  x.part_stride = S * x.ldo;
   if (w.scale) {
     k.f16 = true;
     k.g = (const uint16_t*)(ws + w.off_g16);
     k.ldg = laid_ld(a.m);
     k.inverse = inverse;
   }
-  float* sum = (float*)(ws + w.off_sum);
   k.out_f32 = w.dw.splits > 1;
-  k.out = k.out_f32 ? (void*)sum : a.dw;
+  k.out = k.out_f32 ? (void*)sum_w : a.dw;
   k.ldo = k.out_f32 ? laid_ld(a.n) : a.lddw;
   k.part_stride = E * a.m * k.ldo;
-  if ((rc = hip(launch_expert_dw(k, w.dw, s), "weight gradient")) != FF_OK) return rc;
-  return k.out_f32 ? sum_parts(sum, w.dw.splits, E * a.m, a.n, a.dw, a.lddw, s) : FF_OK;
+  const bool both = a.dx != nullptr && a.dw != nullptr && expert_both(w.dx, w.dw);
+  if (both && (rc = hip(launch_expert_both(x, w.dx, k, w.dw, s), "gradients")) != FF_OK) return rc;
+  if (a.dx != nullptr) {
+    if (!both && (rc = hip(launch_expert_dx(x, w.dx, s), "input gradient")) != FF_OK) return rc;
+    if (a.gather) {
+      // a token's rows in fp32 until they are summed: a rounding of each would add to g's and dx's own
+      CombineArgs c{};
+      c.at = k.at;
+      c.at.weights = nullptr;
+      c.cols = a.n;
+      c.y = sum_x;
+      c.ldy = x.ldo;
+      c.f32 = true;
+      c.parts = w.dx.splits;
+      c.part_stride = x.part_stride;
+      c.out = (bf16_t*)a.dx;
+      c.ldo = a.lddx;
+      if ((rc = hip(launch_combine(c, s), "input gradient's sums")) != FF_OK) return rc;
+    } else if (w.sum_dx && (rc = sum_parts(sum_x, w.dx.splits, S, a.n, a.dx, a.lddx, s)) != FF_OK) {
+      return rc;
+    }
+  }
+  if (a.dw == nullptr) return FF_OK;
+  if (!both && (rc = hip(launch_expert_dw(k, w.dw, s), "weight gradient")) != FF_OK) return rc;
+  return k.out_f32 ? sum_parts(sum_w, w.dw.splits, E * a.m, a.n, a.dw, a.lddw, s) : FF_OK;
 }
 
 // What the layers' gradients check alike (rows of dy: S, of x and dx: X).

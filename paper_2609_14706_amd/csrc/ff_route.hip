@@ -12,7 +12,7 @@
 // V neighbouring experts a lane; it picks one expert after the other, each the largest of
 // the lanes' best: c as a whole number that orders alike, its high words compared first
 // across the lanes (DPP), the low ones only where two lanes share the high one.  What
-// bounds it is instructions: 2200 a token by whole waves, of 256 experts in 8 groups, XXX by rows.
+// bounds it is instructions: 2200 a token by whole waves, of 256 experts in 8 groups, half that by rows.
 //
 // The sort is a counting sort, stable and without an atomic on memory: chunks of
 // tokens count their slots by expert (k_route), a wave for each expert sums the chunks'
