@@ -312,16 +312,18 @@ __device__ __forceinline__ uint32_t peak_bits(const PeaksArgs& a, int64_t block,
   constexpr int N = Vec<E>::N, U = 4;
   uint32_t big = 0;
   const uint32_t per_row = (uint32_t)((a.cols + N - 1) / N);
-  const int64_t total = a.rows * per_row;
+  const int64_t rows = used_rows(a.at), total = rows * per_row;
   for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
     const int64_t r = b / per_row;
     Vec<E> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
-      const int64_t row = r + c / per_row, col = (int64_t)(c % per_row) * N;
+      const int64_t col = (int64_t)(c % per_row) * N;
+      int64_t row = r + c / per_row;
       v[u].w = u32x4{0, 0, 0, 0};
-      if (row < a.rows) v[u] = load_row((const E*)a.src + row * a.ld + col, a.cols - col);
+      if (row < rows && (!a.gather || (row = token_of(a.at, row)) >= 0))
+        v[u] = load_row((const E*)a.src + row * a.ld + col, a.cols - col);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -1017,7 +1019,7 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
 hipError_t launch_peaks(const PeaksArgs (&jobs)[2], hipStream_t s) {
   PeaksJobs q{};
   for (int k = 0; k < 2; ++k) {
-    if (jobs[k].rows <= 0 || jobs[k].cols <= 0 || jobs[k].cols > (int64_t(1) << 24) || (uintptr_t)jobs[k].peaks % 16 != 0)
+    if (!fits(jobs[k].at) || (jobs[k].gather && jobs[k].at.order == nullptr) || jobs[k].cols <= 0 || jobs[k].cols > (int64_t(1) << 24) || (uintptr_t)jobs[k].peaks % 16 != 0)
       return hipErrorInvalidValue;
     q.job[k] = jobs[k];
   }

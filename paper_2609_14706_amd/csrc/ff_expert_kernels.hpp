@@ -145,12 +145,14 @@ inline int64_t part_count(int64_t rows, int experts, int64_t cols) { return rows
 inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 // One to three jobs in one launch.
 hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s);
-// peaks: kPeaks bit patterns of largest finite magnitudes among rows x cols elements,
-// zeros where there are none.  Two jobs in one launch.
+// peaks: kPeaks bit patterns of largest finite magnitudes among the `cols` elements of the rows that
+// are in an expert (gather: of their tokens' rows), zeros where there are none.  Two jobs in one launch.
 constexpr int kPeaks = 1024;
 struct PeaksArgs {
+  SlotRows at;
+  bool gather;
   const void* src;  // bf16 or fp32
-  int64_t ld, rows, cols;
+  int64_t ld, cols;
   bool f32;
   uint32_t* peaks;
 };

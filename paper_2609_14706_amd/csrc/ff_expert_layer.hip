@@ -257,15 +257,16 @@ ff_status sum_parts(const float* parts, int count, int64_t rows, int64_t cols, v
 
 ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t s) {
   ff_status rc;
-  const int64_t S = a.at.rows, E = a.at.experts, T = a.gather ? a.at.tokens : S;
+  const int64_t S = a.at.rows, E = a.at.experts;
   const bool act = a.act != FF_ACT_NONE;
   uint32_t* peaks = (uint32_t*)(ws + w.off_peaks);
   float* inverse = (float*)(peaks + 2 * kPeaks);
   // slopes of the activations are below 1.13; codes end at 127
   const float g_factor = act ? 1.13f : 1.0f, x_factor = 127.0f;
   if (w.scale) {
-    const PeaksArgs jobs[2] = {{a.dy, a.lddy, S, a.m, a.dy_f32, peaks},
-                               {a.x_q8.scale, a.x_q8.ld_scale, T, (a.n + a.x_q8.group - 1) / a.x_q8.group, true, peaks + kPeaks}};
+    const int64_t groups = (a.n + a.x_q8.group - 1) / a.x_q8.group;
+    const PeaksArgs jobs[2] = {{a.at, false, a.dy, a.lddy, a.m, a.dy_f32, peaks},
+                               {a.at, a.gather, a.x_q8.scale, a.x_q8.ld_scale, groups, true, peaks + kPeaks}};
     if ((rc = hip(launch_peaks(jobs, s), "peaks of dy and x")) != FF_OK) return rc;
   }
   RowsArgs jobs[3];

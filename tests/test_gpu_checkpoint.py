@@ -6,7 +6,7 @@ half 127 x / max lies, which the kernel settles in 64 bits: they are equal.  A
 restored value is one fp32 product (2^-24) and its rounding to the output's
 type.  In the gradient each result is rounded once; dx and db read g as it is returned,
 dw of a checkpoint of x reads g (2^-8 of the returned one) and x' = codes scale in
-fp16 (2^-11 of each, or 2^-40 of the largest)."""
+fp16 (2^-11 of each, or 2^-38 of the largest)."""
 import math
 
 import pytest
@@ -176,7 +176,7 @@ def test_linear_backward(gpu, T, n, m, x8, z8):
         want, mag = gb @ W64, gb.abs() @ W64.abs()
         _close(dx, want, HALF * want.abs() * 1.01 + m * 2.0 ** -24 * mag + 1e-30)
         want, mag = gb.T @ xv, gb.abs().T @ xv.abs()
-        far = 1.2 * 2.0 ** -40 * float(dy.double().abs().max() * xv.abs().max())
+        far = 1.2 * 2.0 ** -38 * float(dy.double().abs().max() * xv.abs().max())
         _close(dw, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + x8 * ((HALF + 2.0 ** -10) * 1.01 * mag + T * far) + 1e-30)
         want, mag = gb.sum(0), gb.abs().sum(0)
         _close(db, want, HALF * want.abs() * 1.01 + T * 2.0 ** -24 * mag + 1e-30)
@@ -208,7 +208,7 @@ def test_linear_backward_of_any_magnitude(gpu, scales):
     _, dw, g, _ = ffe.linear_backward(dy, kx, _rows(gpu, m, n, BF16), need_input=False)
     xv = kx.codes.double() * torch.repeat_interleave(kx.scale.double(), 16, dim=1)[:, :n]
     want, mag = dy.double().T @ xv, dy.double().abs().T @ xv.abs()
-    far = 2.0 ** -40 * T * float(dy.double().abs().max() * xv.abs().max())
+    far = 2.0 ** -38 * T * float(dy.double().abs().max() * xv.abs().max())
     _close(dw, want, HALF * 1.01 * want.abs() + 2.0 ** -9 * mag + far + 2.0 ** -133)
 
 
