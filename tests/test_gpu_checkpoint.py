@@ -225,6 +225,32 @@ def test_linear_backward_parts_and_none(gpu):
     assert empty[0].shape == (0, 100) and not bool(empty[1].any()) and not bool(empty[3].any())
 
 
+def test_linear_backward_rank_and_strides(gpu):
+    x, z, dy, W = (_rows(gpu, *s, BF16, seed=k) for k, s in enumerate([(60, 100), (60, 50), (60, 50), (50, 100)]))
+    kx, kz = ffe.checkpoint_q8(x, group=32), ffe.checkpoint_q8(z, group=16)
+    want = ffe.linear_backward(dy, kx, W, preact=kz, activation="gelu")
+
+    def three(k):
+        return ffe.Checkpoint(k.codes.view(3, 20, -1), k.scale.view(3, 20, -1), k.group)
+    got = ffe.linear_backward(dy.view(3, 20, 50), three(kx), W, preact=three(kz), activation="gelu")
+    assert got[0].shape == (3, 20, 100) and got[2].shape == (3, 20, 50)
+    assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(got, want))
+
+    def apart(t, left, right):   # rows that lie apart and begin anywhere
+        wide = torch.zeros(t.shape[0], left + t.shape[1] + right, dtype=t.dtype, device=gpu)
+        view = wide[:, left:left + t.shape[1]]
+        view.copy_(t)
+        return view
+    got = ffe.linear_backward(apart(dy, 3, 5), ffe.Checkpoint(apart(kx.codes, 1, 2), apart(kx.scale, 2, 1), 32), apart(W, 5, 6),
+                              preact=ffe.Checkpoint(apart(kz.codes, 7, 0), apart(kz.scale, 1, 0), 16), activation="gelu")
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = ffe.linear_backward(dy, kx, W, preact=kz, activation="gelu", stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_captured(gpu):
     """Kept and used in one graph, replayed with the program's own work between."""
     x, z, dy, W = (_rows(gpu, *s, BF16, seed=k) for k, s in enumerate([(70, 200), (70, 130), (70, 130), (130, 200)]))

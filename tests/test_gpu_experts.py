@@ -282,6 +282,18 @@ def test_special_values(gpu):
     assert not bool(dx.isnan().any()) and not bool(dw[2].any()) and not bool(db[2].any())
 
 
+@pytest.mark.parametrize("T,E,top,n,m", [(1, 3, 2, 40, 24), (70, 4, 2, 250, 77), (400, 2, 3, 136, 72), (1500, 2, 2, 1032, 2056)])
+def test_nothing_routed(gpu, T, E, top, n, m):
+    """No token takes any expert: zeros everywhere, whatever the inputs hold."""
+    r = _routing(gpu, T, E, top, "none")
+    x, W = torch.full((T, n), math.nan, dtype=BF16, device=gpu), _rand(gpu, E, m, n)
+    dy = torch.full((T * top, m), math.inf, dtype=BF16, device=gpu)
+    y, z = ffe.expert_linear(x, W, r, activation="gelu", keep_preact=True)
+    assert not bool(y.any()) and not bool(z.any()) and not bool(ffe.expert_combine(y, r).any())
+    for kept in (x, ffe.checkpoint_q8(x)):
+        assert not any(bool(v.any()) for v in ffe.expert_linear_backward(dy, kept, W, r, preact=z, activation="gelu"))
+
+
 @pytest.mark.parametrize("by_slot", [False, True])
 def test_rows_in_no_expert_do_not_count(gpu, by_slot):
     """Tokens that are not routed and rows behind the last one may hold any numbers: they do not set
