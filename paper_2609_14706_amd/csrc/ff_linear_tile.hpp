@@ -15,7 +15,7 @@ namespace {
 // sigmoid(x) = 1 / (1 + 2^(-x log2 e)) by the exponential and reciprocal
 // instructions (one unit in the last place each; 0 below x = -87, 1 far out).  The
 // argument's roundings, up to 3 2^-24 |x|, are relative errors of the exponential:
-// 2^-19 of an activation at x = -10, 2^-16 where it ends, 1e-36; bf16's own is 2^-9.
+// 2^-19 of an activation at x = -10, 2^-16 where it ends, 1e-36; bf16's own is 2^-8.
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float sigmoid_of(float minus_x_log2e) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_x_log2e));

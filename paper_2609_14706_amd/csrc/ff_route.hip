@@ -12,7 +12,9 @@
 // V neighbouring experts a lane; it picks one expert after the other, each the largest of
 // the lanes' best: c as a whole number that orders alike, its high words compared first
 // across the lanes (DPP), the low ones only where two lanes share the high one.  What
-// bounds it is instructions: 2200 a token by whole waves, of 256 experts in 8 groups, half that by rows.
+// bounds it is instructions, 2200 a token by whole waves: 16384 tokens, 8 of 256 experts in
+// 8 groups, 36 us so and 26 by rows, the sort's two launches 5 each (their bytes: 4 us in all).
+// One token's 8 of 128: 7.4 us, the latency of the steps one after the other.
 //
 // The sort is a counting sort, stable and without an atomic on memory: chunks of
 // tokens count their slots by expert (k_route), a wave for each expert sums the chunks'
