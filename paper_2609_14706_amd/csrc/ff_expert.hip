@@ -543,6 +543,16 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
 }
 
 // ------------------------------------------------------------------ gradients
+// The lane, counted where it is asked for: addresses of a tile's results would otherwise be kept through
+// a loop over tiles, and spilled.
+__device__ __forceinline__ int lane_here() {
+  uint32_t none = 0;
+  asm volatile("" : "+v"(none));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
+
+__device__ __forceinline__ int wave_here() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // A tile of C to its rows: `rows` and `cols` from the tile's corner on exist, E is
 // bf16_t or float.  Each wave turns its own part over in its quarter of LDS that is free by then: a
 // lane has four columns of a row, and writes 16 bytes beside its neighbours', whole lines of a
@@ -550,7 +560,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
 // 16-byte piece c of row r sits at c ^ (r & 15) of its row: 64 banks for either way.
 template <class G, class E, class Free>
 __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& acc, E* corner, int64_t ld, int64_t rows,
-                                           int64_t cols, float f1, float f2) {
+                                           int64_t cols, float f1, float f2, int wave) {
   constexpr int TI = (int)(sizeof(typename G::Acc) / sizeof(f32x4[G::BN / 32])), TJ = G::BN / 32;
   constexpr int kLine = 16 * TJ * (int)sizeof(E), kPieces = kLine / 16, kPer = 16 / (int)sizeof(E);  // of a wave's row
   constexpr int kSwz = kPieces < 16 ? kPieces - 1 : 15;
@@ -558,11 +568,11 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
   constexpr int kFit = (int)sizeof(Free) / 4 / (16 * kLine), H = kFit >= TI ? TI : kFit >= TI / 2 ? TI / 2 : 1;
   constexpr int kRows = 64 / kPieces;  // the wave stores at once
   static_assert(kFit >= 1 && TI % H == 0 && kPieces <= 64 && 16 * H % kRows == 0, "a wave's part of a phase");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = lane_here();
   char* mine = reinterpret_cast<char*>(&free) + wave * (sizeof(Free) / 4);
   const int piece = lane % kPieces, col = (wave & 1) * 16 * TJ + piece * kPer;
   int row = (wave >> 1) * 16 * TI + lane / kPieces;
-  asm volatile("" : "+s"(ld));  // (in a loop over tiles 32 rows' offsets would be kept, and spilled)
+  asm volatile("" : "+s"(ld));  // (so would 32 rows' offsets)
   E* to_row = corner + row * ld + col;
 #pragma unroll
   for (int h = 0; h < TI / H; ++h) {
@@ -570,6 +580,7 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
     for (int i = 0; i < H; ++i)
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // (read here, not all of them beforehand)
         const f32x4 a = acc[h * H + i][j];
         const float f[4] = {a[0] * f1 * f2, a[1] * f1 * f2, a[2] * f1 * f2, a[3] * f1 * f2};
         const int r = i * 16 + (lane & 15), at = (16 * j + 4 * (lane >> 4)) * (int)sizeof(E);
@@ -593,6 +604,60 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
       to_row += kRows * ld;
     }
     __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The same for a whole tile of bf16 whose rows begin at 16 bytes, times 2^e: in a stream of tiles
+// nothing else runs meanwhile, and the general way has two products, a conversion and half a test for each number
+// (64 experts of 256 rows in the mean, 4096 x 2048, 256 x 256 a tile: 520 us, 484 so; 64 of 64 rows, 2048 x 1408, in
+// tiles of 128: 120 and 101 with the scalar loads of stream_rows).
+template <class G, class Free>
+__device__ __forceinline__ void store_whole(Free& free, const typename G::Acc& acc, bf16_t* corner, int64_t ld, int e,
+                                            int wave) {
+  constexpr int TI = (int)(sizeof(typename G::Acc) / sizeof(f32x4[G::BN / 32])), TJ = G::BN / 32;
+  constexpr int kLine = 32 * TJ, kPieces = kLine / 16, kSwz = kPieces - 1, kRows = 64 / kPieces;
+  static_assert(sizeof(Free) / 4 >= 16 * kLine && kPieces <= 16, "a wave's part of a phase");
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  const int lane = lane_here();
+  char* mine = reinterpret_cast<char*>(&free) + wave * (sizeof(Free) / 4);
+  const int r16 = lane & 15, piece = lane % kPieces, row = lane / kPieces, step = (int)(kRows * ld * 2);
+  const uint32_t at = (uint32_t)(row * ld * 2) + 16u * (uint32_t)piece;
+  const auto to = nt::rsrc((const char*)(corner + (int64_t)(wave >> 1) * 16 * TI * ld + (wave & 1) * 16 * TJ));
+  // (rows are stored when the next ones' are on their way through LDS: a wave's accesses are served in order)
+  constexpr int kEach = 16 / kRows;
+  u32x4 o[2][kEach];
+  int down = 0;
+#pragma unroll
+  for (int i = 0; i <= TI; ++i) {
+    if (i < TI) {
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // (the sums are read here, not all of them beforehand)
+        const f32x4 a = acc[i][j];
+        const bf16x2 lo = __builtin_convertvector((f32x2{ldexpf(a[0], e), ldexpf(a[1], e)}), bf16x2);
+        const bf16x2 hi = __builtin_convertvector((f32x2{ldexpf(a[2], e), ldexpf(a[3], e)}), bf16x2);
+        const int b = 32 * j + 8 * (lane >> 4);
+        *reinterpret_cast<u32x2*>(mine + r16 * kLine + (((b >> 4) ^ (r16 & kSwz)) << 4) + (b & 15)) =
+            u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+      }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < kEach; ++q) {
+        const int r = q * kRows + row;
+        o[i & 1][q] = *reinterpret_cast<const u32x4*>(mine + r * kLine + ((piece ^ (r & kSwz)) << 4));
+      }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (i > 0)
+#pragma unroll
+      for (int q = 0; q < kEach; ++q) {
+        __builtin_amdgcn_raw_buffer_store_b128(o[(i - 1) & 1][q], to, (int)at, down, 0);
+        down += step;
+      }
   }
 }
 
@@ -630,9 +695,9 @@ struct DxTile {
       T::zero(acc);
       T::loop(ring, P, Q, k1 - k0, acc);
       if (a.out_f32)
-        store_tile<T>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
+        store_tile<T>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f, wave_here());
       else
-        store_tile<T>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f);
+        store_tile<T>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f, wave_here());
     };
     if (half_of(TI) < TI && g.rows <= H::BM)
       one(rings.half, H());
@@ -694,9 +759,9 @@ struct DwTile {
     if (k1 > k0) G::loop(ring, P, Q, k1 - k0, acc);
     const int64_t at = ((int64_t)e * a.m + m0) * a.ldo + n0;
     if (a.out_f32)
-      store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+      store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2, wave_here());
     else
-      store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2);
+      store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2, wave_here());
   }
 };
 
@@ -765,7 +830,20 @@ hipError_t expert_skinny(const ExpertArgs& a, hipStream_t s) {
 // waiting for its first rows and storing, which the next tile's copies run beside.  Each XCD's
 // workgroups, as many as its units hold, take the tiles of its eighth of every expert's in turn,
 // experts by falling numbers of rows, so that all of them end alike (64 experts of 256 rows in the mean, 4096 x
-// 2048: 518 us, one workgroup a tile 615; of 64 rows, 2048 x 1408 in tiles of 128: 115 and 132).
+// 2048: 484 us, one workgroup a tile 615; of 64 rows, 2048 x 1408 in tiles of 128: 101 and 132).  What is
+// left (with parts of it left out in turn): 234 the loops of four pairs, 80 to 100 what their copies wait, 100 the
+// stores' 1.1 GB, the rest their conversion.  Not waiting for a tile's stores before its next one's second pair changed
+// nothing.
+// (An expert's rows by scalar loads: a vector load would be waited for together with the copies and stores on
+// their way, twice a tile: 64 experts of 64 rows, 2048 x 1408, 108 us, 101 so.)
+__device__ __forceinline__ int64_t stream_rows(const SlotRows& at, int e, int64_t& first) {
+  typedef const __attribute__((address_space(4))) int32_t fixed;
+  first = 0;
+  if (at.offsets == nullptr) return at.rows;
+  fixed* p = (fixed*)(uintptr_t)(at.offsets + e);
+  first = bounded(p[0], at.rows);
+  return max((int64_t)0, bounded(p[1], at.rows) - first);
+}
 template <class T, int TI, int TJ, int SLOTS>
 struct DwStream {
   typedef kn::Tile<T, true, TI, TJ, SLOTS> G;
@@ -797,7 +875,7 @@ struct DwStream {
         m0 = (int64_t)ti * G::BM;
         n0 = (int64_t)tj * G::BN;
         int64_t row0;
-        k = expert_rows(a.at, (int)expert, row0);
+        k = stream_rows(a.at, (int)expert, row0);
         P = {(const char*)(a.g + row0 * a.ldg + m0), a.m - m0, (uint32_t)(a.ldg * 2)};
         Q = {(const char*)(a.x + row0 * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
         return true;
@@ -838,9 +916,18 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kW
   }
   const float f1 = a.f16 ? a.inverse[0] : 1.0f, f2 = a.f16 ? a.inverse[1] : 1.0f;
   typename S::Tiles tiles{a, sh, mt, ntl, (mt * ntl + 7) / 8, blockIdx.x >> 3, 0, 0, 0};
+  // (the scales' product may leave fp32's range where the result does not)
+  const int e = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(f1) >> 23) + (int)(__float_as_uint(f2) >> 23) - 254);
+  const bool aligned = a.ldo % 8 == 0 && (uintptr_t)a.out % 16 == 0 && a.ldo * 2 <= nt::kMaxRowBytes;
+  int wave = wave_here();
+  asm volatile("" : "+s"(wave));  // (kept: asked for again it would be read from scratch, behind all copies)
   G::stream(sh.ring, tiles, [&](const typename G::Acc& acc, const typename S::Tiles& t) {
-    store_tile<G>(sh.stage, acc, (bf16_t*)a.out + ((int64_t)t.expert * a.m + t.m0) * a.ldo + t.n0, a.ldo, a.m - t.m0,
-                  a.n - t.n0, f1, f2);
+    bf16_t* to = (bf16_t*)a.out + ((int64_t)t.expert * a.m + t.m0) * a.ldo + t.n0;
+    const int64_t rows = a.m - t.m0, cols = a.n - t.n0;
+    if (aligned && rows >= G::BM && cols >= G::BN)
+      store_whole<G>(sh.stage, acc, to, a.ldo, e, wave);
+    else
+      store_tile<G>(sh.stage, acc, to, a.ldo, rows, cols, f1, f2, wave);
   });
 }
 

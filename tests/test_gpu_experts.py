@@ -448,3 +448,20 @@ def test_refusals(gpu):
                      ((dy, x, W, r), dict(activation="relu", preact=k)), ((dy, None, W, r), {}), ((dy, x, None, r), {})):
         with pytest.raises(both):
             ffe.expert_linear_backward(*args, **kw)
+
+
+@pytest.mark.parametrize("scales", [(1e-30, 1e-8), (1e30, 1e-30), (1e18, 1e17), (1e-3, 1e3)])
+def test_large_gradients_of_any_magnitude(gpu, scales):
+    """As test_checkpoints_of_any_magnitude, in the tiles of a stream, whole ones and others."""
+    T, E, top, n, m = 2000, 2, 1, 1032, 2056
+    r = _routing(gpu, T, E, top, "even")
+    x, dy = _rand(gpu, T, n, scale=scales[0]), _rand(gpu, T * top, m, seed=1, scale=scales[1])
+    W = torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    kx = ffe.checkpoint_q8(x)
+    _, dw, g, _ = ffe.expert_linear_backward(dy, kx, W, r, need_input=False)
+    x64 = _value(kx)
+    for e, rows, t in _parts(r):
+        want, mag = g[rows].double().T @ x64[t], g[rows].double().abs().T @ x64[t].abs()
+        far = T * top * 2.0 ** -38 * float(dy.double().abs().max() * x64.abs().max())
+        # (a result below fp32's normal range is rounded to its step and to bf16's, 2^-133, there)
+        _close(dw[e], want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * 2.0 ** -24) * mag + far + 2.0 ** -133)
