@@ -1092,7 +1092,9 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
   int64_t total = 0;
   for (int k = 0; k < count; ++k) {
     const RowsArgs& a = jobs[k];
-    if (!fits(a.at) || (a.gather && a.at.order == nullptr) || a.cols <= 0 || a.cols > (int64_t(1) << 24)) return hipErrorInvalidValue;
+    // (rows that are no slots, those of all experts' weights, may be more than slots are)
+    const bool plain = a.at.offsets == nullptr && !a.gather && a.parts == nullptr && a.at.rows > 0 && a.at.rows <= (int64_t(1) << 30);
+    if ((!plain && !fits(a.at)) || (a.gather && a.at.order == nullptr) || a.cols <= 0 || a.cols > (int64_t(1) << 24)) return hipErrorInvalidValue;
     if ((uintptr_t)a.laid % 16 != 0 || (uintptr_t)a.scaled % 16 != 0 || (a.scaled != nullptr && a.peaks == nullptr))
       return hipErrorInvalidValue;
     if ((a.scaled != nullptr && a.inverse == nullptr) || (a.parts != nullptr && (k != 0 || (uintptr_t)a.parts % 16 != 0)))

@@ -465,3 +465,20 @@ def test_large_gradients_of_any_magnitude(gpu, scales):
         far = T * top * 2.0 ** -38 * float(dy.double().abs().max() * x64.abs().max())
         # (a result below fp32's normal range is rounded to its step and to bf16's, 2^-133, there)
         _close(dw[e], want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * 2.0 ** -24) * mag + far + 2.0 ** -133)
+
+
+def test_more_weight_rows_than_slots(gpu):
+    """Weights of more than 2^24 rows, whose rows are laid out for dx."""
+    T, E, top, n, m = 3, 1024, 2, 9, 16400
+    r = _routing(gpu, T, E, top, "all")
+    W = torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    W[E - 1] = _rand(gpu, m, n, seed=1)
+    dy = _rand(gpu, T * top, m, seed=2)
+    dx, dw, g, db = ffe.expert_linear_backward(dy, torch.zeros((T, n), dtype=BF16, device=gpu), W, r, need_weight=False, need_bias=False)
+    rows = torch.zeros((T * top, n), dtype=torch.float64, device=gpu)
+    mag = torch.zeros_like(rows)
+    for e, s, _ in _parts(r):
+        rows[s], mag[s] = g[s].double() @ W[e].double(), g[s].double().abs() @ W[e].double().abs()
+    at = r.place.long()
+    want, mag = rows[at].sum(1), mag[at].sum(1)
+    _close(dx, want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
