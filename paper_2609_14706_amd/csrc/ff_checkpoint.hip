@@ -4,7 +4,7 @@
 //   a group's scale = max |x| / 127 (2^shift columns of a row), q = rint(127 x / max |x|),
 //   and back: x' = q scale, off by at most half a scale.
 //
-// Both are bound by memory: 8192 x 8192 bf16 in 52 us (201 MB, 3.9 TB/s), and back, its
+// Both are bound by memory: 8192 x 8192 bf16 in 49 to 52 us (201 MB, 3.9 to 4.1 TB/s), and back, its
 // codes still in the last-level cache, in 32.  A thread takes eight columns (16 bytes of
 // bf16) of four pieces of the array at once, a group 2 to 64 neighbouring lanes, its largest
 // magnitude one reduction over them.  A code hangs on which side of a half 127 x / max lies:
