@@ -313,7 +313,7 @@ struct PeaksJobs {
 };
 template <class E>
 __device__ __forceinline__ uint32_t peak_bits(const PeaksArgs& a, int64_t block, int64_t blocks) {
-  constexpr int N = Vec<E>::N, U = 4;
+  constexpr int N = Vec<E>::N, U = 2;  // (4: as fast for large arrays, 5.5 us instead of 4.6 for 1021 x 777)
   uint32_t big = 0;
   const uint32_t per_row = (uint32_t)((a.cols + N - 1) / N);
   const int64_t rows = used_rows(a.at), total = rows * per_row;
@@ -451,8 +451,8 @@ __device__ __forceinline__ void store_piece(const RowsArgs& a, int64_t row, int6
 
 // The operands of the gradients' products: g = dy act'(z) as the caller's rows, as bf16 rows of whole
 // pieces and in fp16, and the sums of its columns; x and W as such rows.  All that a call needs are jobs of
-// one launch.  Bound by memory (16384 x 2048 and, gathered, 16384 x 4096 from checkpoints: 390 MB in 105 to
-// 114 us, 3.6 TB/s), small ones by latency (1021 x 777 and x 1000: 16 us).
+// one launch.  Bound by memory (16384 x 2048 and, gathered, 16384 x 4096 from checkpoints: 390 MB in 97 to
+// 106 us, 3.7 TB/s or more), small ones by latency (1021 x 777 and x 1000: 16 us).
 __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
   __shared__ uint32_t red[4];
   __shared__ float sums[256][9];
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-    constexpr int U = 4;  // rows a thread has in flight
+    constexpr int U = 2;  // rows a thread has in flight (4: 86 us where these take 73, 4096 x 11008 and x 4096)
     for (int k = r; n > 0 && k < rows; k += U * down) {
       float f[U][8];
       int64_t row[U], cols[U];
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
     return;
   }
   const int64_t total = a.at.rows * per_row, used = used_rows(a.at);
-  constexpr int U = 4;
+  constexpr int U = 2;
   for (int64_t b = (int64_t)w * (256 * U); b < total; b += (int64_t)blocks * (256 * U)) {
     const int64_t r = b / per_row;
     float f[U][8];
@@ -1107,7 +1107,7 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
       total += grid_for(a.at, q.part_rows, (per_row + across - 1) / across);
       if (total > kMaxGrid) return hipErrorInvalidValue;
     } else {
-      total += std::min<int64_t>((a.at.rows * per_row + 1023) / 1024, 4096);
+      total += std::min<int64_t>((a.at.rows * per_row + 511) / 512, 8192);
     }
     q.job[k] = a;
     q.end[k] = (uint32_t)total;
