@@ -451,9 +451,9 @@ def test_refusals(gpu):
 
 
 @pytest.mark.parametrize("scales", [(1e-30, 1e-8), (1e30, 1e-30), (1e18, 1e17), (1e-3, 1e3)])
-def test_large_gradients_of_any_magnitude(gpu, scales):
-    """As test_checkpoints_of_any_magnitude, in the tiles of a stream, whole ones and others."""
-    T, E, top, n, m = 2000, 2, 1, 1032, 2056
+@pytest.mark.parametrize("T,E,top,n,m", [(2000, 2, 1, 1032, 2056), (6144, 24, 1, 2056, 2056)])
+def test_large_gradients_of_any_magnitude(gpu, T, E, top, n, m, scales):
+    """As test_checkpoints_of_any_magnitude, in larger tiles and in a stream of the largest, whole ones and others."""
     r = _routing(gpu, T, E, top, "even")
     x, dy = _rand(gpu, T, n, scale=scales[0]), _rand(gpu, T * top, m, seed=1, scale=scales[1])
     W = torch.zeros((E, m, n), dtype=BF16, device=gpu)
@@ -482,3 +482,43 @@ def test_more_weight_rows_than_slots(gpu):
     at = r.place.long()
     want, mag = rows[at].sum(1), mag[at].sum(1)
     _close(dx, want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("T,E,n,m", [(1200, 2, 776, 1288), (900, 18, 776, 1288), (6144, 24, 2056, 2056)])
+@pytest.mark.parametrize("gap", [0, 3, 24])
+def test_weight_gradient_rows_apart(gpu, gap, T, E, n, m):
+    """dw with rows further apart than n, by the C ABI: the same bits as without gaps, which stay as they were."""
+    import paper_2609_14706_amd.experts as X
+    top = 1
+    r = _routing(gpu, T, E, top, "even")
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T * top, m, seed=1), torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    want, g = ffe.expert_linear_backward(dy, x, W, r, need_input=False, need_bias=False)[1:3]
+    dw = torch.full((E * m, n + gap), 7.0, dtype=BF16, device=gpu)
+    a = X.ff_expert_grad_args()
+    a.routing, a.n, a.m, a.dy_dtype, a.dy, a.lddy = X._routing(r, x.device), n, m, X._elem(dy, "dy"), dy.data_ptr(), m
+    a.x, a.ldx, a.w, a.ldw, a.g, a.ldg = x.data_ptr(), n, W.data_ptr(), n, g.data_ptr(), m
+    a.dw, a.lddw = dw.data_ptr(), n + gap
+    keep = X._workspace(a, X._bytes("ff_expert_linear_backward_workspace_size", a, functions=X._FN), None, x.device)
+    X._launch("ff_expert_linear_backward", a, x.device, X._FN)
+    del keep
+    assert torch.equal(dw[:, :n].reshape(E, m, n), want)
+    assert bool((dw[:, n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("T,E,n,m", [(6144, 24, 2056, 2056), (1024, 1, 4104, 8200)])
+def test_largest_weight_gradients(gpu, T, E, n, m):
+    """A stream of 256 x 256 tiles, in bf16 and, from a checkpoint, in fp16."""
+    r = _routing(gpu, T, E, 1, "some")
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T, m, seed=1), torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    kx = ffe.checkpoint_q8(x)
+    for kept in (x, kx):
+        _, dw, g, db = ffe.expert_linear_backward(dy, kept, W, r, need_input=False)
+        x64 = _value(kx) if kept is kx else x.double()
+        far = T * 2.0 ** -38 * float(dy.double().abs().max() * x64.abs().max())
+        for e, rows, t in _parts(r):
+            ge, xe = g[rows].double(), x64[t]
+            want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+            tol = HALF * 1.01 * want.abs() + T * 2.0 ** -24 * mag + 1e-30
+            _close(dw[e], want, tol + (2.0 ** -9 * mag + far if kept is kx else 0))
+            want, mag = ge.sum(0), ge.abs().sum(0)
+            _close(db[e], want, HALF * 1.01 * want.abs() + T * 2.0 ** -24 * mag + 1e-30)
