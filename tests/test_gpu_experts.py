@@ -522,3 +522,43 @@ def test_largest_weight_gradients(gpu, T, E, n, m):
             _close(dw[e], want, tol + (2.0 ** -9 * mag + far if kept is kx else 0))
             want, mag = ge.sum(0), ge.abs().sum(0)
             _close(db[e], want, HALF * 1.01 * want.abs() + T * 2.0 ** -24 * mag + 1e-30)
+
+
+# A size for each form of the products (tiles of 32 i x 32 j, pairs of k in flight, k in parts) that the
+# sizes above leave out, by the rules that choose them.
+FORMS = {"y skinny 2": (13, 1, 1, 40, 35), "y 4 8 3": (2744, 1, 1, 1233, 1427), "y 6 8 2": (13219, 1, 1, 45, 543),
+         "y 8 8 2": (3474, 1, 1, 166, 3528), "dx 2 4 3 in 16": (2, 1, 1, 32, 4889), "dx 2 4 3 in 2": (605, 1, 1, 883, 3972),
+         "dx 2 4 3 in 4": (1, 1, 1, 35, 1695), "dx 4 4 2": (19165, 1, 1, 134, 35), "dx 4 4 2 in 2": (17085, 1, 1, 37, 11007),
+         "dx 4 4 2 in 4": (2453, 8, 8, 51, 8865), "dx 4 8 3": (1926, 1, 1, 2098, 1277), "dx 4 8 3 in 2": (1594, 1, 1, 2112, 11008),
+         "dx 4 8 3 in 4": (4172, 2, 1, 458, 9945), "dx 6 8 2": (16541, 1, 1, 454, 33), "dx 6 8 2 in 2": (2788, 1, 1, 1832, 8712),
+         "dx 6 8 2 in 4": (2185, 1, 1, 994, 9517), "dx 8 8 2": (12853, 1, 1, 939, 155), "dw 2 4 3 in 8": (2084, 1, 1, 47, 40),
+         "dw 4 4 2": (162, 1, 1, 2539, 1603), "dw 4 4 2 in 2": (21217, 1, 1, 3081, 1068), "dw 4 4 2 in 4": (12755, 2, 2, 2007, 527),
+         "dw 4 4 2 in 8": (19264, 1, 1, 135, 2238), "dw 8 8 2 in 16": (22749, 2, 2, 1057, 903), "dw 8 8 2 in 2": (9301, 1, 1, 1965, 2591),
+         "dw 8 8 2 in 4": (11710, 1, 1, 943, 2477), "dw 8 8 2 in 8": (19693, 1, 1, 1561, 585)}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form(gpu, form):
+    T, E, top, n, m = FORMS[form]
+    r = _routing(gpu, T, E, top, "some")
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T * top, m, seed=1), _rand(gpu, E, m, n, seed=2, scale=0.05)
+    y, _ = ffe.expert_linear(x, W, r)
+    kx = ffe.checkpoint_q8(x)
+    dx, dw, g, _ = ffe.expert_linear_backward(dy, x, W, r)
+    dw8 = ffe.expert_linear_backward(dy, kx, W, r, need_input=False)[1]
+    sums = torch.zeros((T * top + 1, n), dtype=torch.float64, device=gpu)
+    mags = torch.zeros_like(sums)
+    far = T * top * 2.0 ** -38 * float(dy.double().abs().max() * x.double().abs().max())
+    for e, rows, t in _parts(r):
+        ge, xe, we = g[rows].double(), x[t].double(), W[e].double()
+        want = xe @ we.T
+        _close(y[rows], want, HALF * 1.01 * want.abs() + n * 2.0 ** -24 * (xe.abs() @ we.abs().T))
+        sums[rows], mags[rows] = ge @ we, ge.abs() @ we.abs()
+        want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+        _close(dw[e], want, HALF * 1.01 * want.abs() + T * top * 2.0 ** -24 * mag)
+        x8 = _value(kx)[t]
+        want, mag = ge.T @ x8, ge.abs().T @ x8.abs()
+        _close(dw8[e], want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * top * 2.0 ** -24) * mag + far)
+    at = r.place.long()   # (-1, no row: the zeros at the end)
+    want, mag = sums[at].sum(1), mags[at].sum(1)
+    _close(dx, want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
