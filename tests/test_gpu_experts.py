@@ -562,3 +562,17 @@ def test_every_form(gpu, form):
     at = r.place.long()   # (-1, no row: the zeros at the end)
     want, mag = sums[at].sum(1), mags[at].sum(1)
     _close(dx, want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("by_slot", [False, True])
+@pytest.mark.parametrize("n", [2100, 4200])   # eight and sixteen waves share a row's k
+@pytest.mark.parametrize("T,E,top", [(1, 1, 1), (5, 3, 2), (20, 1, 1), (40, 1, 1), (60, 2, 1)])
+def test_few_rows_of_long_k(gpu, T, E, top, n, by_slot):
+    m = 130
+    r = _routing(gpu, T, E, top, "even")
+    x, W, b = _rand(gpu, T * top if by_slot else T, n), _rand(gpu, E, m, n, seed=1, scale=0.05), _rand(gpu, E, m, seed=2)
+    y, _ = ffe.expert_linear(x, W, r, bias=b, by_slot=by_slot)
+    for e, rows, t in _parts(r):
+        xe, we = (x[rows] if by_slot else x[t]).double(), W[e].double()
+        want = xe @ we.T + b[e].double()
+        _close(y[rows], want, HALF * 1.01 * want.abs() + (n + 1) * 2.0 ** -24 * (xe.abs() @ we.abs().T + b[e].double().abs()))
