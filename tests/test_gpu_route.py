@@ -321,3 +321,19 @@ def test_refusals(gpu):
     for args in ((dw[:7], logits, e), (dw.double(), logits, e), (dw, logits, e[:7]), (dw, logits, e.long()), (dw, logits, None)):
         with pytest.raises((ValueError, TypeError)):
             ffe.route_backward(*args)
+
+
+# a wave a token for few experts and many choices, groups within, across and beside lanes' experts, two
+# experts a lane, one workgroup and many
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,E,top,groups,top_groups", [(30, 20, 17, 1, 1), (300, 50, 20, 5, 3), (70, 64, 64, 1, 1), (300, 64, 17, 64, 40), (9, 128, 24, 8, 2),
+                                                       (500, 128, 40, 1, 1), (333, 256, 32, 64, 16), (7, 250, 60, 10, 4), (600, 500, 33, 50, 20), (90, 30, 4, 3, 2), (2000, 32, 16, 2, 1),
+                                                       (400, 17, 2, 1, 1), (1000, 240, 16, 48, 9), (600, 252, 5, 63, 7)])
+def test_route_other_forms(gpu, T, E, top, groups, top_groups, dtype):
+    test_route(gpu, T, E, top, groups, top_groups, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,E,top", [(40, 200, 12), (600, 130, 64), (3, 256, 8), (2000, 30, 30)])
+def test_route_backward_other_forms(gpu, T, E, top, dtype):
+    test_route_backward(gpu, T, E, top, dtype)
