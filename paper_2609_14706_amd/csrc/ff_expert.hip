@@ -553,14 +553,22 @@ __device__ __forceinline__ int lane_here() {
 
 __device__ __forceinline__ int wave_here() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-// A tile of C to its rows: `rows` and `cols` from the tile's corner on exist, E is
+// What takes the sums of fp16 operands back is 2^e: one power of two for both, as the first of two
+// factors alone may leave fp32's range where the result does not.
+__device__ __forceinline__ int sums_exponent(const ExpertGradArgs& a) {
+  if (!a.f16) return 0;
+  const uint32_t g = __float_as_uint(a.inverse[0]) >> 23, x = __float_as_uint(a.inverse[1]) >> 23;
+  return __builtin_amdgcn_readfirstlane((int)(g + x)) - 254;
+}
+
+// A tile of C, times 2^e, to its rows: `rows` and `cols` from the tile's corner on exist, E is
 // bf16_t or float.  Each wave turns its own part over in its quarter of LDS that is free by then: a
 // lane has four columns of a row, and writes 16 bytes beside its neighbours', whole lines of a
 // row at once (8192 tiles of 256 x 256 with 256 rows each: 796 us with the lanes' own 8 bytes).
 // 16-byte piece c of row r sits at c ^ (r & 15) of its row: 64 banks for either way.
 template <class G, class E, class Free>
 __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& acc, E* corner, int64_t ld, int64_t rows,
-                                           int64_t cols, float f1, float f2, int wave) {
+                                           int64_t cols, int e, int wave) {
   constexpr int TI = (int)(sizeof(typename G::Acc) / sizeof(f32x4[G::BN / 32])), TJ = G::BN / 32;
   constexpr int kLine = 16 * TJ * (int)sizeof(E), kPieces = kLine / 16, kPer = 16 / (int)sizeof(E);  // of a wave's row
   constexpr int kSwz = kPieces < 16 ? kPieces - 1 : 15;
@@ -582,7 +590,7 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
       for (int j = 0; j < TJ; ++j) {
         __builtin_amdgcn_sched_barrier(0);  // (read here, not all of them beforehand)
         const f32x4 a = acc[h * H + i][j];
-        const float f[4] = {a[0] * f1 * f2, a[1] * f1 * f2, a[2] * f1 * f2, a[3] * f1 * f2};
+        const float f[4] = {ldexpf(a[0], e), ldexpf(a[1], e), ldexpf(a[2], e), ldexpf(a[3], e)};
         const int r = i * 16 + (lane & 15), at = (16 * j + 4 * (lane >> 4)) * (int)sizeof(E);
         char* to = mine + r * kLine + (((at >> 4) ^ (r & kSwz)) << 4) + (at & 15);
         if constexpr (sizeof(E) == 4) {
@@ -607,8 +615,8 @@ __device__ __forceinline__ void store_tile(Free& free, const typename G::Acc& ac
   }
 }
 
-// The same for a whole tile of bf16 whose rows begin at 16 bytes, times 2^e: in a stream of tiles
-// nothing else runs meanwhile, and the general way has two products, a conversion and half a test for each number
+// The same for a whole tile of bf16 whose rows begin at 16 bytes: in a stream of tiles
+// nothing else runs meanwhile, and the general way has a conversion and half a test more for each number
 // (64 experts of 256 rows in the mean, 4096 x 2048, 256 x 256 a tile: 520 us, 484 so; 64 of 64 rows, 2048 x 1408, in
 // tiles of 128: 120 and 101 with the scalar loads of stream_rows).
 template <class G, class Free>
@@ -695,9 +703,9 @@ struct DxTile {
       T::zero(acc);
       T::loop(ring, P, Q, k1 - k0, acc);
       if (a.out_f32)
-        store_tile<T>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f, wave_here());
+        store_tile<T>(ring, acc, (float*)a.out + z * a.part_stride + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 0, wave_here());
       else
-        store_tile<T>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 1.0f, 1.0f, wave_here());
+        store_tile<T>(ring, acc, (bf16_t*)a.out + g.row0 * a.ldo + n0, a.ldo, g.rows, a.n - n0, 0, wave_here());
     };
     if (half_of(TI) < TI && g.rows <= H::BM)
       one(rings.half, H());
@@ -751,7 +759,7 @@ struct DwTile {
     const int64_t k1 = min(rows, pairs * (z + 1) / splits * kn::kK);
     const kn::Side P{(const char*)(a.g + (row0 + k0) * a.ldg + m0), a.m - m0, (uint32_t)(a.ldg * 2)};
     const kn::Side Q{(const char*)(a.x + (row0 + k0) * a.ldx + n0), a.n - n0, (uint32_t)(a.ldx * 2)};
-    const float f1 = a.f16 ? a.inverse[0] : 1.0f, f2 = a.f16 ? a.inverse[1] : 1.0f;
+    const int scale = sums_exponent(a);
     if (a.db != nullptr && tj == 0 && z == 0 && threadIdx.x < G::BM && m0 + threadIdx.x < a.m)
       sum_column(a, e, row0, rows, m0 + threadIdx.x);
     typename G::Acc acc;
@@ -759,9 +767,9 @@ struct DwTile {
     if (k1 > k0) G::loop(ring, P, Q, k1 - k0, acc);
     const int64_t at = ((int64_t)e * a.m + m0) * a.ldo + n0;
     if (a.out_f32)
-      store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, f1, f2, wave_here());
+      store_tile<G>(ring, acc, (float*)a.out + z * a.part_stride + at, a.ldo, a.m - m0, a.n - n0, scale, wave_here());
     else
-      store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, f1, f2, wave_here());
+      store_tile<G>(ring, acc, (bf16_t*)a.out + at, a.ldo, a.m - m0, a.n - n0, scale, wave_here());
   }
 };
 
@@ -914,10 +922,8 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kW
       if (col < a.m) sum_column(a, e, row0, count, col);
     }
   }
-  const float f1 = a.f16 ? a.inverse[0] : 1.0f, f2 = a.f16 ? a.inverse[1] : 1.0f;
   typename S::Tiles tiles{a, sh, mt, ntl, (mt * ntl + 7) / 8, blockIdx.x >> 3, 0, 0, 0};
-  // (the scales' product may leave fp32's range where the result does not)
-  const int e = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(f1) >> 23) + (int)(__float_as_uint(f2) >> 23) - 254);
+  const int e = sums_exponent(a);
   const bool aligned = a.ldo % 8 == 0 && (uintptr_t)a.out % 16 == 0 && a.ldo * 2 <= nt::kMaxRowBytes;
   int wave = wave_here();
   asm volatile("" : "+s"(wave));  // (kept: asked for again it would be read from scratch, behind all copies)
@@ -927,7 +933,7 @@ __global__ __launch_bounds__(nt::kThreads, (kn::Tile<T, true, TI, TJ, SLOTS>::kW
     if (aligned && rows >= G::BM && cols >= G::BN)
       store_whole<G>(sh.stage, acc, to, a.ldo, e, wave);
     else
-      store_tile<G>(sh.stage, acc, to, a.ldo, rows, cols, f1, f2, wave);
+      store_tile<G>(sh.stage, acc, to, a.ldo, rows, cols, e, wave);
   });
 }
 

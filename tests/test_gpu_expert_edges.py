@@ -1,0 +1,77 @@
+"""The ends of what the operators around a layer of experts and of 8-bit checkpoints take:
+magnitudes, tokens that are not routed, rows in no expert, arrays that are no routing.
+
+References are the formulas in 64 bits (the routing's gradient: in 60 digits).  Tolerances as
+for the operators' other tests: an fp32 sum of n terms is off by at most n 2^-24 of the sum of
+magnitudes, a rounding by half a step (bf16 2^-8, fp32 2^-24), the fp16 operands of a
+checkpoint's dW by 2^-11 of each value or 2^-38 of the largest."""
+import decimal
+import math
+
+import pytest
+import torch
+
+import paper_2609_14706_amd as ffe
+import paper_2609_14706_amd.experts as X
+
+pytestmark = pytest.mark.gpu
+
+HALF, BF16, F32 = 2.0 ** -8, torch.bfloat16, torch.float32
+
+
+def _rand(gpu, *shape, seed=0, scale=1.0, dtype=BF16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).to(dtype).to(gpu)
+
+
+def _routing(gpu, T, E, top, idle=0.0, seed=0):
+    """Random choices, `idle` of them none."""
+    g = torch.Generator().manual_seed(1000 * T + E + seed)
+    e = torch.argsort(torch.rand((T, E), generator=g) * torch.linspace(0.3, 1, E), dim=1)[:, :top].int()
+    e[torch.rand((T, top), generator=g) < idle] = -1
+    w = torch.rand((T, top), generator=g) + 0.1
+    return ffe.expert_order(e.to(gpu).contiguous(), E, weights=w.to(gpu))
+
+
+def _parts(r):
+    """(expert, its rows, their tokens) of the experts that have rows."""
+    ends, order, top = r.offsets.tolist(), r.order.long(), r.experts.shape[1]
+    return [(e, slice(a, b), order[a:b] // top) for e, (a, b) in enumerate(zip(ends, ends[1:])) if b > a]
+
+
+def _value(k):
+    return k.codes.double() * torch.repeat_interleave(k.scale.double(), k.group, dim=1)[:, :k.codes.shape[1]]
+
+
+def _close(got, want, tol):
+    assert got.shape == want.shape, (got.shape, want.shape)
+    bad = ~((got.double() - want).abs() <= tol)
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+# tokens, experts, n, m: both gradients in one launch, smaller tiles, sums cut along the rows, the largest
+# tiles in a stream, whole ones and edges
+@pytest.mark.parametrize("scales", [(1e-30, 1e35), (1e-35, 1e36), (1e35, 1e-30)])
+@pytest.mark.parametrize("T,E,n,m", [(200, 3, 72, 40), (1000, 1, 136, 72), (162, 1, 2539, 1603), (2000, 2, 1032, 2056),
+                                     (9301, 1, 1965, 2591), (6144, 24, 2056, 2056)])
+def test_weight_gradient_of_opposite_magnitudes(gpu, T, E, n, m, scales):
+    """One operand near the end of fp32's range, the other far below one: neither power of two alone
+    takes the sums back, both together do."""
+    r = _routing(gpu, T, E, 1)
+    x, dy = _rand(gpu, T, n, scale=scales[0]), _rand(gpu, T, m, seed=1, scale=scales[1])
+    W = torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    kx = ffe.checkpoint_q8(x)
+    x64, g64 = _value(kx), dy.double()
+    got = [ffe.expert_linear_backward(dy, kx, W, r, need_input=need)[1] for need in (False, True)]
+    far = T * 2.0 ** -38 * float(g64.abs().max() * x64.abs().max())
+
+    def check(dw, ge, xe):
+        want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+        assert bool(torch.isfinite(dw).all())
+        _close(dw, want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * 2.0 ** -24) * mag + far + 2.0 ** -133)
+    for e, rows, t in _parts(r):
+        for dw in got:
+            check(dw[e], g64[rows], x64[t])
+    if E == 1:   # the plain layer, whose rows lie in their order
+        for need in (False, True):
+            check(ffe.linear_backward(dy, kx, W[0], need_input=need)[1], g64, x64)
