@@ -608,8 +608,8 @@ ff_status ff_route(const ff_route_args* args);
 ff_status ff_expert_order(const ff_route_args* args);
 
 /* Gradient of the weights of ff_route with respect to the logits (bias and choice count as
- * constants), in 64 bits.  Choices outside 0 .. experts - 1 have none.  dlogits may be the
- * logits themselves (the same rows and ld). */
+ * constants), in 64 bits.  Choices outside 0 .. experts - 1 have none; a token that has no other gets
+ * zeros, whatever its logits are.  dlogits may be the logits themselves (the same rows and ld). */
 typedef struct {
   int64_t tokens, experts, top;
   ff_dtype dtype;           /* logits and dlogits */

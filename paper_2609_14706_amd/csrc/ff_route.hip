@@ -617,6 +617,8 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
       if (taken(e, a.experts)) dw = (double)a.dweights[t * a.top + lane] * a.scale;
       else e = -1;
     }
+    // A token that takes no expert has no gradient, whatever its logits hold (a padded one's may be NaN)
+    const bool idle = __ballot(e >= 0) == 0;
     if (a.renormalise) {
       // d_j = (dw_j - sum dw w / sum w) / sum w, w the chosen scores
       double w = 0.0;
@@ -645,7 +647,7 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (e0 + i < a.experts)
-        out[e0 + i] = Elem<L>::from_f32((float)(a.sigmoid ? d[i] * s[i] * (1.0 - s[i]) : s[i] * (d[i] - dot)));
+        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * (1.0 - s[i]) : s[i] * (d[i] - dot)));
   }
 }
 

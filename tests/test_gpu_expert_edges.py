@@ -75,3 +75,30 @@ def test_weight_gradient_of_opposite_magnitudes(gpu, T, E, n, m, scales):
     if E == 1:   # the plain layer, whose rows lie in their order
         for need in (False, True):
             check(ffe.linear_backward(dy, kx, W[0], need_input=need)[1], g64, x64)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("E,top", [(7, 2), (60, 4), (130, 8), (1000, 20)])
+def test_route_gradient_of_tokens_that_are_not_routed(gpu, E, top, dtype):
+    """Their logits may hold anything: their rows of the gradient are zeros, the others as they were."""
+    T = 75
+    g = torch.Generator().manual_seed(E)
+    logits = (2 * torch.randn((T, E), generator=g)).to(dtype)
+    dw = torch.randn((T, top), generator=g)
+    mask = torch.arange(T) % 3 > 0
+    bad = logits.clone()
+    for k, v in enumerate((math.nan, math.inf, -math.inf)):
+        bad[9 * k] = v                  # (token 27 of no kind: finite)
+        bad[9 * k + 3, E // 2] = v
+        bad[9 * k + 6, E - 1] = v
+    assert not bool(mask[:27:3].any())
+    for score in ("softmax", "sigmoid"):
+        r = ffe.route(bad.to(gpu), top, score=score, mask=mask.to(gpu))
+        for renorm in (True, False):
+            want = ffe.route_backward(dw.to(gpu), logits.to(gpu), r.experts, score=score, renormalise=renorm)
+            got = ffe.route_backward(dw.to(gpu), bad.to(gpu), r.experts, score=score, renormalise=renorm)
+            assert not bool(got[~mask].any()) and torch.equal(got, want) and bool(got[mask].any())
+            # choices that are none, in place of the logits, of which nothing is left
+            out = bad.to(gpu)
+            none = torch.full((T, top), E, dtype=torch.int32, device=gpu)
+            assert not bool(ffe.route_backward(dw.to(gpu), out, none, score=score, renormalise=renorm).any())
