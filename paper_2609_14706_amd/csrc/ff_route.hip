@@ -166,15 +166,22 @@ __device__ __forceinline__ void load_neighbours(const L* row, int left, float ot
   }
 }
 
-// Scores of the V experts from e0 on of a lane from their logits (those beyond the last: 0).
+// Scores of the V experts from e0 on of a lane from their logits (those beyond the last: 0).  rest, where
+// it is asked for: 1 - s under sigmoid, as exp(-l) s; the difference would lose what s has lost to
+// its rounding, from l = 21 on more than fp32's, from 37 on all of it.
 template <class L, int V, int LANES>
-__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, int e0, double (&s)[V]) {
+__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, int e0, double (&s)[V],
+                                          double* rest = nullptr) {
   typedef Lanes<LANES> G;
   float l[V];
   load_neighbours<L, V>(row + e0, experts - e0, -INFINITY, l);
   if (sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = 1.0 / (1.0 + exp(-(double)l[i]));  // (beyond the last: 0)
+    for (int i = 0; i < V; ++i) {
+      const double t = exp(-(double)l[i]);
+      s[i] = 1.0 / (1.0 + t);  // (beyond the last: 0)
+      if (rest != nullptr) rest[i] = t == INFINITY ? 1.0 : t * s[i];
+    }
     return;
   }
   float big = -INFINITY;
@@ -599,14 +606,14 @@ __global__ __launch_bounds__(512) void k_route_few(RouteArgs a) {
 
 // --------------------------------------------------------------- gradient
 // A wave a token.  d = gradient of each score (zeros but for the chosen), then
-// softmax: dl = s (d - sum s d), sigmoid: dl = d s (1 - s).  In 64 bits: with
+// softmax: dl = s (d - sum s d), sigmoid: dl = d s sigmoid(-l).  In 64 bits: with
 // renormalised weights d is a difference that cancels for a single expert.
 template <class L, int V>
 __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
   const int lane = threadIdx.x & 63, e0 = lane * V;
   for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += (int64_t)gridDim.x * 4) {
-    double s[V], d[V];
-    scores_of<L, V, 64>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, e0, s);
+    double s[V], rest[V], d[V];
+    scores_of<L, V, 64>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, e0, s, rest);
 #pragma unroll
     for (int i = 0; i < V; ++i) d[i] = 0.0;
     // lane j has the j-th choice
@@ -647,7 +654,7 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (e0 + i < a.experts)
-        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * (1.0 - s[i]) : s[i] * (d[i] - dot)));
+        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * rest[i] : s[i] * (d[i] - dot)));
   }
 }
 

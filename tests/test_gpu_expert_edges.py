@@ -102,3 +102,69 @@ def test_route_gradient_of_tokens_that_are_not_routed(gpu, E, top, dtype):
             out = bad.to(gpu)
             none = torch.full((T, top), E, dtype=torch.int32, device=gpu)
             assert not bool(ffe.route_backward(dw.to(gpu), out, none, score=score, renormalise=renorm).any())
+
+
+def _digits(values):
+    return [decimal.Decimal(float(v)) for v in values]
+
+
+def _route_gradient(logits, dw, chosen, score, renorm):
+    """A token's gradient of the weights by its logits in 60 digits, and the magnitudes of the terms that a
+    sum of differences has: dl_i = s_i sum_k s_k (d_i - d_k), d_j = sum_k w_k (dw_j - dw_k) / sum."""
+    with decimal.localcontext() as c:
+        c.prec = 60
+        l, zero = _digits(logits), decimal.Decimal(0)
+        if score == "sigmoid":
+            s = [1 / (1 + (-v).exp()) for v in l]
+            slope = [1 / (1 + v.exp()) for v in l]   # 1 - s
+        else:
+            e = [(v - max(l)).exp() for v in l]
+            s = [v / sum(e) for v in e]
+        dw = _digits(dw)
+        d, m = [zero] * len(l), [zero] * len(l)
+        total = sum(s[e] for e in chosen)
+        for j, e in enumerate(chosen):
+            if renorm:
+                terms = [s[f] / total * (dw[j] - dw[k]) / total for k, f in enumerate(chosen)]
+                d[e], m[e] = d[e] + sum(terms), m[e] + sum(abs(v) for v in terms)
+            else:
+                d[e], m[e] = d[e] + dw[j], m[e] + abs(dw[j])
+        if score == "sigmoid":
+            return ([float(a * b * q) for a, b, q in zip(d, s, slope)], [float(a * b * q) for a, b, q in zip(m, s, slope)])
+        out, mag = [], []
+        for i in range(len(l)):
+            others = [k for k in range(len(l)) if k != i]
+            out.append(float(s[i] * sum(s[k] * (d[i] - d[k]) for k in others)))
+            mag.append(float(s[i] * sum(s[k] * (abs(d[i] - d[k]) + m[i] + m[k]) for k in others)))
+        return out, mag
+
+
+def _check_route_gradient(gpu, score, renorm, top, dtype):
+    E = 9
+    g = torch.Generator().manual_seed(top)
+    logits = torch.randn((40, E), generator=g)
+    for t in range(40):   # one expert, or all of them, further and further ahead of the others
+        logits[t, t % E] += t
+    if score == "sigmoid":
+        logits[20:] += torch.arange(20.0)[:, None]
+    logits = logits.to(dtype)
+    dw = torch.randn((40, top), generator=g)
+    r = ffe.route(logits.to(gpu), top, score=score)
+    chosen = r.experts.cpu()
+    chosen[5:40:7] = chosen[5:40:7].flip(1)
+    chosen[3] = torch.arange(1, top + 1)      # not the largest scores: as a bias or the caller has it
+    got = ffe.route_backward(dw.to(gpu), logits.to(gpu), chosen.to(gpu), score=score, renormalise=renorm).double().cpu()
+    half = 2.0 ** -24 if dtype is F32 else 2.0 ** -8
+    for t in range(40):
+        want, mag = (torch.tensor(v, dtype=torch.float64)
+                     for v in _route_gradient(logits[t].tolist(), dw[t].tolist(), chosen[t].tolist(), score, renorm))
+        # (2^-149, 2^-133: the types' smallest steps)
+        tol = half * 1.0001 * want.abs() + 1e-12 * mag + (2.0 ** -149 if dtype is F32 else 2.0 ** -133)
+        assert bool(((got[t] - want).abs() <= tol).all()), (t, got[t].tolist(), want.tolist())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", [1, 3])
+def test_route_gradient_of_sigmoids_near_one(gpu, top, dtype):
+    """1 - sigmoid(l) is sigmoid(-l), not a difference of rounded numbers: nothing is left of that from l = 37 on."""
+    _check_route_gradient(gpu, "sigmoid", False, top, dtype)
