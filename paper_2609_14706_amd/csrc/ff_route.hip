@@ -606,8 +606,13 @@ __global__ __launch_bounds__(512) void k_route_few(RouteArgs a) {
 
 // --------------------------------------------------------------- gradient
 // A wave a token.  d = gradient of each score (zeros but for the chosen), then
-// softmax: dl = s (d - sum s d), sigmoid: dl = d s sigmoid(-l).  In 64 bits: with
-// renormalised weights d is a difference that cancels for a single expert.
+// softmax: dl = s (d - sum s d), sigmoid: dl = d s sigmoid(-l), in 64 bits.  Of one
+// expert far ahead of the others, m, d_m - sum s d cancels to what the others' scores leave
+// (and so does the gradient of its renormalised weight).  As the s sum to one, it is
+//   d_i - sum_k s_k d_k = (d_i - d_m) + sum_k s_k (d_m - d_k)
+// for any d_m; with m the score above one half, or d_m = 0 where there is none, no
+// term is larger than what it is off by matters.  (A single chosen expert's renormalised
+// weight is one whatever its logits: its gradient comes out as zero.)
 template <class L, int V>
 __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
   const int lane = threadIdx.x & 63, e0 = lane * V;
@@ -627,15 +632,19 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
     // A token that takes no expert has no gradient, whatever its logits hold (a padded one's may be NaN)
     const bool idle = __ballot(e >= 0) == 0;
     if (a.renormalise) {
-      // d_j = (dw_j - sum dw w / sum w) / sum w, w the chosen scores
+      // d_j = (dw_j - sum dw w) / sum, w = s / sum, sum that of the chosen scores
       double w = 0.0;
 #pragma unroll
       for (int i = 0; i < V; ++i) {  // (the lane's choice lies with lane e / V)
         const double v = __shfl(s[i], e < 0 ? 0 : e / V);
         if (e >= 0 && e % V == i) w = v;
       }
-      const double sum = wave_sum(w), dot = wave_sum(dw * w);
-      dw = sum == 0.0 ? 0.0 : (dw - dot / sum) / sum;
+      const double sum = wave_sum(w);
+      w /= sum;
+      const u64 ahead = __ballot(w > 0.5);
+      const double most = ahead != 0 ? lane_value(dw, __ffsll((long long)ahead) - 1) : 0.0;
+      const double dot = wave_sum(w * (most - dw));
+      dw = sum == 0.0 ? 0.0 : (dw - most + dot) / sum;
     }
     for (int j = 0; j < a.top; ++j) {
       const int ej = __builtin_amdgcn_readlane(e, j);
@@ -644,17 +653,26 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
       for (int i = 0; i < V; ++i)
         if (ej == e0 + i) d[i] += dj;
     }
-    double dot = 0.0;
+    double most = 0.0, dot = 0.0;
     if (!a.sigmoid) {
+      bool mine = false;
 #pragma unroll
-      for (int i = 0; i < V; ++i) dot += s[i] * d[i];
+      for (int i = 0; i < V; ++i)
+        if (s[i] > 0.5) {
+          mine = true;
+          most = d[i];
+        }
+      const u64 ahead = __ballot(mine);
+      most = ahead != 0 ? lane_value(most, __ffsll((long long)ahead) - 1) : 0.0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) dot += s[i] * (most - d[i]);
       dot = wave_sum(dot);
     }
     L* out = (L*)a.dlogits + t * a.ldd;
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (e0 + i < a.experts)
-        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * rest[i] : s[i] * (d[i] - dot)));
+        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * rest[i] : s[i] * (d[i] - most + dot)));
   }
 }
 

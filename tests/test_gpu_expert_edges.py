@@ -168,3 +168,12 @@ def _check_route_gradient(gpu, score, renorm, top, dtype):
 def test_route_gradient_of_sigmoids_near_one(gpu, top, dtype):
     """1 - sigmoid(l) is sigmoid(-l), not a difference of rounded numbers: nothing is left of that from l = 37 on."""
     _check_route_gradient(gpu, "sigmoid", False, top, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("top", [1, 3])
+def test_route_gradient_of_one_expert_far_ahead(gpu, top, score, renorm, dtype):
+    """A score, or a weight, next to one: its gradient is a sum over the others, not one less a rounded number."""
+    _check_route_gradient(gpu, score, renorm, top, dtype)
