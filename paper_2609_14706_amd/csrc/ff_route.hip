@@ -166,22 +166,15 @@ __device__ __forceinline__ void load_neighbours(const L* row, int left, float ot
   }
 }
 
-// Scores of the V experts from e0 on of a lane from their logits (those beyond the last: 0).  rest, where
-// it is asked for: 1 - s under sigmoid, as exp(-l) s; the difference would lose what s has lost to
-// its rounding, from l = 21 on more than fp32's, from 37 on all of it.
+// Scores of the V experts from e0 on of a lane from their logits (those beyond the last: 0).
 template <class L, int V, int LANES>
-__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, int e0, double (&s)[V],
-                                          double* rest = nullptr) {
+__device__ __forceinline__ void scores_of(const L* row, int experts, bool sigmoid, int e0, double (&s)[V]) {
   typedef Lanes<LANES> G;
   float l[V];
   load_neighbours<L, V>(row + e0, experts - e0, -INFINITY, l);
   if (sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const double t = exp(-(double)l[i]);
-      s[i] = 1.0 / (1.0 + t);  // (beyond the last: 0)
-      if (rest != nullptr) rest[i] = t == INFINITY ? 1.0 : t * s[i];
-    }
+    for (int i = 0; i < V; ++i) s[i] = 1.0 / (1.0 + exp(-(double)l[i]));  // (beyond the last: 0)
     return;
   }
   float big = -INFINITY;
@@ -612,18 +605,16 @@ __global__ __launch_bounds__(512) void k_route_few(RouteArgs a) {
 //   d_i - sum_k s_k d_k = (d_i - d_m) + sum_k s_k (d_m - d_k)
 // for any d_m; with m the score above one half, or d_m = 0 where there is none, no
 // term is larger than what it is off by matters.  (A single chosen expert's renormalised
-// weight is one whatever its logits: its gradient comes out as zero.)
+// weight is one whatever its logits: its gradient comes out as zero.)  Under sigmoid
+// only the chosen logits are read: the others' gradients are zeros.
 template <class L, int V>
 __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
   const int lane = threadIdx.x & 63, e0 = lane * V;
   for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += (int64_t)gridDim.x * 4) {
-    double s[V], rest[V], d[V];
-    scores_of<L, V, 64>((const L*)a.logits + t * a.ldl, a.experts, a.sigmoid, e0, s, rest);
-#pragma unroll
-    for (int i = 0; i < V; ++i) d[i] = 0.0;
-    // lane j has the j-th choice
+    const L* row = (const L*)a.logits + t * a.ldl;
+    // lane j has the j-th choice: the gradient of its weight, and its score w
     int e = -1;
-    double dw = 0.0;
+    double dw = 0.0, w = 0.0, slope = 1.0;
     if (lane < a.top) {
       e = a.chosen[t * a.top + lane];
       if (taken(e, a.experts)) dw = (double)a.dweights[t * a.top + lane] * a.scale;
@@ -631,14 +622,27 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
     }
     // A token that takes no expert has no gradient, whatever its logits hold (a padded one's may be NaN)
     const bool idle = __ballot(e >= 0) == 0;
-    if (a.renormalise) {
-      // d_j = (dw_j - sum dw w) / sum, w = s / sum, sum that of the chosen scores
-      double w = 0.0;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {  // (the lane's choice lies with lane e / V)
-        const double v = __shfl(s[i], e < 0 ? 0 : e / V);
-        if (e >= 0 && e % V == i) w = v;
+    double s[V], d[V];
+    if (a.sigmoid) {
+      // 1 - w as exp(-l) w: the difference would lose what w has lost to its rounding, from l = 21
+      // on more than fp32's, from 37 on all of it
+      if (e >= 0) {
+        const double x = exp(-(double)Elem<L>::to_f32(row[e]));
+        w = 1.0 / (1.0 + x);
+        slope = x == INFINITY ? 0.0 : x * w * w;
       }
+    } else {
+      scores_of<L, V, 64>(row, a.experts, false, e0, s);
+      if (a.renormalise) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {  // (the lane's choice lies with lane e / V)
+          const double v = __shfl(s[i], e < 0 ? 0 : e / V);
+          if (e >= 0 && e % V == i) w = v;
+        }
+      }
+    }
+    if (a.renormalise) {
+      // d_j = (dw_j - sum dw w) / sum, w over sum, that of the chosen scores
       const double sum = wave_sum(w);
       w /= sum;
       const u64 ahead = __ballot(w > 0.5);
@@ -646,6 +650,9 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
       const double dot = wave_sum(w * (most - dw));
       dw = sum == 0.0 ? 0.0 : (dw - most + dot) / sum;
     }
+    dw *= slope;
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = 0.0;
     for (int j = 0; j < a.top; ++j) {
       const int ej = __builtin_amdgcn_readlane(e, j);
       const double dj = lane_value(dw, j);
@@ -653,8 +660,8 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
       for (int i = 0; i < V; ++i)
         if (ej == e0 + i) d[i] += dj;
     }
-    double most = 0.0, dot = 0.0;
-    if (!a.sigmoid) {
+    if (!a.sigmoid && !idle) {
+      double most = 0.0, dot = 0.0;
       bool mine = false;
 #pragma unroll
       for (int i = 0; i < V; ++i)
@@ -667,12 +674,13 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGradArgs a) {
 #pragma unroll
       for (int i = 0; i < V; ++i) dot += s[i] * (most - d[i]);
       dot = wave_sum(dot);
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[i] = s[i] * (d[i] - most + dot);
     }
     L* out = (L*)a.dlogits + t * a.ldd;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (e0 + i < a.experts)
-        out[e0 + i] = Elem<L>::from_f32(idle ? 0.0f : (float)(a.sigmoid ? d[i] * s[i] * rest[i] : s[i] * (d[i] - most + dot)));
+      if (e0 + i < a.experts) out[e0 + i] = Elem<L>::from_f32((float)d[i]);
   }
 }
 
