@@ -543,7 +543,7 @@ ff_status ff_checkpoint_restore(const ff_checkpoint_args* args);
 /* ff_linear_backward from checkpoints: x_q8 (q not NULL) stands for x, preact_q8 for preact
  * (its values are not rounded); the other one may be bf16 as before.  For dw of a checkpoint g
  * and x are rounded to 11 bits (fp16, scaled by powers of two) instead of bf16's 8: each value
- * to 2^-11 of itself or 2^-38 of the largest.  FF_ACT_NONE: g, where given, receives a copy of dy. */
+ * to 2^-11 of itself or 2^-38 of the largest (of x: of 127 times the largest scale).  FF_ACT_NONE: g, where given, receives a copy of dy. */
 typedef struct {
   ff_linear_grad_args grad; /* x, preact: NULL where a checkpoint is given */
   ff_q8_rows x_q8;          /* tokens x n */
@@ -697,7 +697,8 @@ ff_status ff_expert_combine_backward(const ff_expert_combine_grad_args* args);
  * bf16, but dy in either type.  g is rounded before it is used (an expert's rows of x and g
  * are the tokens that ff_config takes).  x_q8 and preact_q8 (q not NULL) are checkpoints that stand
  * for x and preact; for dw of a checkpoint g and x are rounded to 11 bits (fp16, scaled by powers
- * of two) instead, each value to 2^-11 of itself or 2^-38 of the largest.  Reads order, offsets and (without by_slot) place. */
+ * of two) instead, each value to 2^-11 of itself or 2^-38 of the largest (of x: of 127 times the largest
+ * scale).  Reads order, offsets and (without by_slot) place. */
 typedef struct {
   ff_routing routing;
   int64_t n, m;             /* <= 2^20 */

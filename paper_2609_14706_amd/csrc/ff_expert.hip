@@ -308,51 +308,6 @@ __device__ __forceinline__ uint32_t peak_of(const uint32_t* peaks, uint32_t* red
   return v;
 }
 
-struct PeaksJobs {
-  PeaksArgs job[2];
-};
-template <class E>
-__device__ __forceinline__ uint32_t peak_bits(const PeaksArgs& a, int64_t block, int64_t blocks) {
-  constexpr int N = Vec<E>::N, U = 2;  // (4: as fast for large arrays, 5.5 us instead of 4.6 for 1021 x 777)
-  uint32_t big = 0;
-  const uint32_t per_row = (uint32_t)((a.cols + N - 1) / N);
-  const int64_t rows = used_rows(a.at), total = rows * per_row;
-  for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
-    const int64_t r = b / per_row;
-    Vec<E> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
-      const int64_t col = (int64_t)(c % per_row) * N;
-      int64_t row = r + c / per_row;
-      v[u].w = u32x4{0, 0, 0, 0};
-      if (row < rows && (!a.gather || (row = token_of(a.at, row)) >= 0))
-        v[u] = load_row((const E*)a.src + row * a.ld + col, a.cols - col);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t bits = __float_as_uint(v[u].get(i)) & 0x7fffffffu;
-        if (bits < 0x7f800000u) big = max(big, bits);
-      }
-  }
-  return big;
-}
-// The largest finite magnitudes of kPeaks parts of each array: no atomic, and no values to clear
-// beforehand (4096 x 11008 of bf16, 90 MB, and the other operand's scales: 24 us, 3.8 TB/s).
-__global__ __launch_bounds__(256) void k_peaks(PeaksJobs jobs) {
-  __shared__ uint32_t red[4];
-  const PeaksArgs& a = jobs.job[blockIdx.x >= kPeaks];
-  const int block = blockIdx.x % kPeaks;
-  uint32_t big = a.f32 ? peak_bits<float>(a, block, kPeaks) : peak_bits<bf16_t>(a, block, kPeaks);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
-  __syncthreads();
-  if (threadIdx.x == 0) a.peaks[block] = max(max(red[0], red[1]), max(red[2], red[3]));
-}
-
 struct RowsJobs {
   RowsArgs job[3];
   uint32_t end[3];  // first workgroup after the job
@@ -360,8 +315,9 @@ struct RowsJobs {
 };
 
 // Pieces of eight columns, `n` of them in their row (0: no such row, zeros), zeros beyond
-// them.  All of a kind's loads go out before the first is waited for.
-template <int U>
+// them, times act'(z).  All of a kind's loads go out before the first is waited for.  ONCE: which
+// activation it is is decided once, not for each number; k_rows needs 91 registers so, 75 otherwise.
+template <bool ONCE, int U>
 __device__ __forceinline__ void load_pieces(const RowsArgs& a, const int64_t (&row)[U], const int64_t (&col)[U],
                                             const int (&n)[U], float (&f)[U][8]) {
   int64_t from[U];
@@ -408,7 +364,6 @@ __device__ __forceinline__ void load_pieces(const RowsArgs& a, const int64_t (&r
       for (int i = 0; i < 8; ++i) use(u, i, v[u].get(i));
   };
   auto put = [&](int u, int i, float v) { f[u][i] = v; };
-  auto slope = [&](int u, int i, float v) { f[u][i] *= act_slope(v, a.act); };
   if (a.src_q8.q != nullptr) {
     codes(a.src_q8, from, put);
   } else if (a.src_f32) {
@@ -427,11 +382,111 @@ __device__ __forceinline__ void load_pieces(const RowsArgs& a, const int64_t (&r
   } else {
     values((const bf16_t*)a.src, a.lds, from, put);
   }
-  if (a.z_q8.q != nullptr)
-    codes(a.z_q8, row, slope);
-  else if (a.z != nullptr)
-    values(a.z, a.ldz, row, slope);
+  if (a.z_q8.q == nullptr && a.z == nullptr) return;
+  auto slopes = [&](auto act) {
+    auto slope = [&](int u, int i, float v) { f[u][i] *= act_slope(v, act); };
+    if (a.z_q8.q != nullptr)
+      codes(a.z_q8, row, slope);
+    else
+      values(a.z, a.ldz, row, slope);
+  };
+  if (!ONCE)
+    slopes(a.act);
+  else if (a.act == kActRelu)
+    slopes(std::integral_constant<int, kActRelu>());
+  else if (a.act == kActGelu)
+    slopes(std::integral_constant<int, kActGelu>());
+  else
+    slopes(std::integral_constant<int, kActSilu>());
 }
+
+struct PeaksJobs {
+  RowsArgs job[2];
+  uint32_t* peaks[2];
+};
+template <class E>
+__device__ __forceinline__ uint32_t peak_bits(const RowsArgs& a, int64_t block, int64_t blocks) {
+  constexpr int N = Vec<E>::N, U = 2;  // (4: as fast for large arrays, 5.5 us instead of 4.6 for 1021 x 777)
+  uint32_t big = 0;
+  const uint32_t per_row = (uint32_t)((a.cols + N - 1) / N);
+  const int64_t rows = used_rows(a.at), total = rows * per_row;
+  for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
+    const int64_t r = b / per_row;
+    Vec<E> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
+      const int64_t col = (int64_t)(c % per_row) * N;
+      int64_t row = r + c / per_row;
+      v[u].w = u32x4{0, 0, 0, 0};
+      if (row < rows && (!a.gather || (row = token_of(a.at, row)) >= 0))
+        v[u] = load_row((const E*)a.src + row * a.lds + col, a.cols - col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t bits = __float_as_uint(v[u].get(i)) & 0x7fffffffu;
+        if (bits < 0x7f800000u) big = max(big, bits);
+      }
+  }
+  return big;
+}
+// The same of dy act'(z): where the slope is zero, or next to it, dy may be far above all of g.  Bound by the
+// slopes' instructions and the reads, hardly overlapped (4096 x 11008 of bf16 and codes, 137 MB, 50 us).
+__device__ __forceinline__ uint32_t peak_bits_of_g(const RowsArgs& a, int64_t block, int64_t blocks) {
+  constexpr int U = 2;
+  uint32_t big = 0;
+  const uint32_t per_row = (uint32_t)((a.cols + 7) / 8);
+  const int64_t rows = used_rows(a.at), total = rows * per_row;
+  for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
+    const int64_t r = b / per_row;
+    int64_t row[U], col[U];
+    int count[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
+      row[u] = r + c / per_row;
+      col[u] = (int64_t)(c % per_row) * 8;
+      count[u] = row[u] < rows ? (int)min((int64_t)8, a.cols - col[u]) : 0;
+    }
+    float f[U][8];
+    load_pieces<true>(a, row, col, count, f);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(f[u][i]) & 0x7fffffffu);
+      if (most >= 0x7f800000u) {  // (hardly ever: one by one)
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t bits = __float_as_uint(f[u][i]) & 0x7fffffffu;
+          if (bits < 0x7f800000u) most = max(most, bits);
+        }
+      }
+      big = max(big, most);
+    }
+  }
+  return big;
+}
+// The largest finite magnitudes of kPeaks parts of each array: no atomic, and no values to clear
+// beforehand (4096 x 11008 of bf16, 90 MB, and the other operand's scales: 24 us, 3.8 TB/s).
+__global__ __launch_bounds__(256) void k_peaks(PeaksJobs jobs) {
+  __shared__ uint32_t red[4];
+  const int which = blockIdx.x >= kPeaks;
+  const RowsArgs& a = jobs.job[which];
+  const int block = blockIdx.x % kPeaks;
+  uint32_t big = a.z != nullptr || a.z_q8.q != nullptr ? peak_bits_of_g(a, block, kPeaks)
+                 : a.src_f32                           ? peak_bits<float>(a, block, kPeaks)
+                                                       : peak_bits<bf16_t>(a, block, kPeaks);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
+  __syncthreads();
+  if (threadIdx.x == 0) jobs.peaks[which][block] = max(max(red[0], red[1]), max(red[2], red[3]));
+}
+
 // Its outputs; the rounded values to `o`.
 __device__ __forceinline__ void store_piece(const RowsArgs& a, int64_t row, int64_t col, int n, const float (&f)[8], float scale,
                                             Vec<bf16_t>& o) {
@@ -453,6 +508,7 @@ __device__ __forceinline__ void store_piece(const RowsArgs& a, int64_t row, int6
 // pieces and in fp16, and the sums of its columns; x and W as such rows.  All that a call needs are jobs of
 // one launch.  Bound by memory (16384 x 2048 and, gathered, 16384 x 4096 from checkpoints: 390 MB in 97 to
 // 106 us, 3.7 TB/s or more), small ones by latency (1021 x 777 and x 1000: 16 us).
+template <bool ONCE>
 __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
   __shared__ uint32_t red[4];
   __shared__ float sums[256][9];
@@ -495,7 +551,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
         cols[u] = col;
         count[u] = k + u * down < rows ? n : 0;
       }
-      load_pieces(a, row, cols, count, f);
+      load_pieces<ONCE>(a, row, cols, count, f);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (count[u] > 0) {
@@ -533,7 +589,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
       count[u] = row[u] < a.at.rows ? (int)min((int64_t)8, a.cols - col[u]) : 0;
       have[u] = row[u] < used ? count[u] : 0;
     }
-    load_pieces(a, row, col, have, f);
+    load_pieces<ONCE>(a, row, col, have, f);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       Vec<bf16_t> o;
@@ -1119,16 +1175,22 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
     q.end[k] = (uint32_t)total;
   }
   for (int k = count; k < 3; ++k) q.end[k] = (uint32_t)total;
-  hipLaunchKernelGGL(k_rows, dim3((uint32_t)total), dim3(256), 0, s, q);
+  // Few rows are bound by latency, many by memory, which more waves keep busy (1021 x 777 and x 1000 from checkpoints:
+  // 15.5 us with the activation decided once, 17.3 without; 4096 x 11008 and x 4096: 89 and 80)
+  if (jobs[0].at.rows * jobs[0].cols < (int64_t(1) << 22))
+    hipLaunchKernelGGL(k_rows<true>, dim3((uint32_t)total), dim3(256), 0, s, q);
+  else
+    hipLaunchKernelGGL(k_rows<false>, dim3((uint32_t)total), dim3(256), 0, s, q);
   return hipGetLastError();
 }
 
-hipError_t launch_peaks(const PeaksArgs (&jobs)[2], hipStream_t s) {
-  PeaksJobs q{};
+hipError_t launch_peaks(const RowsArgs& g, uint32_t* g_peaks, const RowsArgs& scales, uint32_t* x_peaks, hipStream_t s) {
+  const PeaksJobs q{{g, scales}, {g_peaks, x_peaks}};
   for (int k = 0; k < 2; ++k) {
-    if (!fits(jobs[k].at) || (jobs[k].gather && jobs[k].at.order == nullptr) || jobs[k].cols <= 0 || jobs[k].cols > (int64_t(1) << 24) || (uintptr_t)jobs[k].peaks % 16 != 0)
+    const RowsArgs& a = q.job[k];
+    if (!fits(a.at) || (a.gather && a.at.order == nullptr) || a.cols <= 0 || a.cols > (int64_t(1) << 24) || a.src == nullptr ||
+        q.peaks[k] == nullptr || (uintptr_t)q.peaks[k] % 16 != 0)
       return hipErrorInvalidValue;
-    q.job[k] = jobs[k];
   }
   hipLaunchKernelGGL(k_peaks, dim3(2 * kPeaks), dim3(256), 0, s, q);
   return hipGetLastError();

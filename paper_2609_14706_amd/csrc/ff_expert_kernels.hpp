@@ -145,18 +145,11 @@ inline int64_t part_count(int64_t rows, int experts, int64_t cols) { return rows
 inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 // One to three jobs in one launch.
 hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s);
-// peaks: kPeaks bit patterns of largest finite magnitudes among the `cols` elements of the rows that
-// are in an expert (gather: of their tokens' rows), zeros where there are none.  Two jobs in one launch.
+// peaks: kPeaks bit patterns of largest finite magnitudes among the `cols` elements that launch_rows makes of
+// the rows that are in an expert (gather: of their tokens' rows), zeros where there are none; of a
+// checkpoint given as its scales (src fp32) among those.  Two jobs in one launch, the second without z.
 constexpr int kPeaks = 1024;
-struct PeaksArgs {
-  SlotRows at;
-  bool gather;
-  const void* src;  // bf16 or fp32
-  int64_t ld, cols;
-  bool f32;
-  uint32_t* peaks;
-};
-hipError_t launch_peaks(const PeaksArgs (&jobs)[2], hipStream_t s);
+hipError_t launch_peaks(const RowsArgs& g, uint32_t* g_peaks, const RowsArgs& scales, uint32_t* x_peaks, hipStream_t s);
 
 // Gradients of the products; g rows of bf16, or (f16) of fp16 scaled by its peaks, 16-byte
 // aligned with zeros up to a multiple of 8.

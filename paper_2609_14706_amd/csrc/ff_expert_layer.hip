@@ -261,14 +261,6 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
   const bool act = a.act != FF_ACT_NONE;
   uint32_t* peaks = (uint32_t*)(ws + w.off_peaks);
   float* inverse = (float*)(peaks + 2 * kPeaks);
-  // slopes of the activations are below 1.13; codes end at 127
-  const float g_factor = act ? 1.13f : 1.0f, x_factor = 127.0f;
-  if (w.scale) {
-    const int64_t groups = (a.n + a.x_q8.group - 1) / a.x_q8.group;
-    const PeaksArgs jobs[2] = {{a.at, false, a.dy, a.lddy, a.m, a.dy_f32, peaks},
-                               {a.at, a.gather, a.x_q8.scale, a.x_q8.ld_scale, groups, true, peaks + kPeaks}};
-    if ((rc = hip(launch_peaks(jobs, s), "peaks of dy and x")) != FF_OK) return rc;
-  }
   RowsArgs jobs[3];
   int count = 0;
   RowsArgs r{};
@@ -283,13 +275,23 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
     r.ldz = a.ldz;
     r.z_q8 = q8_of(a.z_q8);
   }
+  if (w.scale) {
+    RowsArgs x{};
+    x.at = a.at;
+    x.gather = a.gather;
+    x.cols = (a.n + a.x_q8.group - 1) / a.x_q8.group;
+    x.src = a.x_q8.scale;
+    x.lds = a.x_q8.ld_scale;
+    x.src_f32 = true;
+    if ((rc = hip(launch_peaks(r, peaks, x, peaks + kPeaks, s), "peaks of g and x")) != FF_OK) return rc;
+  }
   r.out = (bf16_t*)a.g;
   r.ldo = a.ldg;
   if (w.lay_g) r.laid = (uint16_t*)(ws + w.off_g);
   if (w.scale) {
     r.scaled = (uint16_t*)(ws + w.off_g16);
     r.peaks = peaks;
-    r.peak_factor = g_factor;
+    r.peak_factor = 1.0f;
     r.inverse = inverse;
   }
   if (a.db != nullptr) r.parts = (float*)(ws + w.off_parts);
@@ -315,7 +317,7 @@ ff_status run_gradient(const Gradient& a, const GradWs& w, char* ws, hipStream_t
       x.src_q8 = q8_of(a.x_q8);
       x.scaled = (uint16_t*)(ws + w.off_x);
       x.peaks = peaks + kPeaks;
-      x.peak_factor = x_factor;
+      x.peak_factor = 127.0f;  // (codes end there)
       x.inverse = inverse + 1;
     } else {
       x.laid = (uint16_t*)(ws + w.off_x);

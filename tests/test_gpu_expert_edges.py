@@ -177,3 +177,30 @@ def test_route_gradient_of_sigmoids_near_one(gpu, top, dtype):
 def test_route_gradient_of_one_expert_far_ahead(gpu, top, score, renorm, dtype):
     """A score, or a weight, next to one: its gradient is a sum over the others, not one less a rounded number."""
     _check_route_gradient(gpu, score, renorm, top, dtype)
+
+
+@pytest.mark.parametrize("z8", [False, True])
+@pytest.mark.parametrize("act,off", [("relu", -1.0), ("silu", -60.0), ("gelu", -9.0)])
+@pytest.mark.parametrize("T,E,top,n,m", [(150, 3, 2, 72, 40), (700, 2, 2, 513, 129), (1500, 1, 1, 1032, 2056)])
+def test_weight_gradient_beside_units_that_are_off(gpu, T, E, top, n, m, act, off, z8):
+    """The largest dy where the activation has no slope: dW's other sums are as good as without it."""
+    r = _routing(gpu, T, E, top, 0.1)
+    S = T * top
+    x, W, z, dy = _rand(gpu, T, n), _rand(gpu, E, m, n, seed=1, scale=0.05), _rand(gpu, S, m, seed=2), _rand(gpu, S, m, seed=3)
+    z[:, 16:32] = off                   # a group of its own
+    dy[1::5, 16:32] *= 2.0 ** 60
+    kx = ffe.checkpoint_q8(x)
+    kz = ffe.checkpoint_q8(z, group=16) if z8 else z
+    _, dw, g, _ = ffe.expert_linear_backward(dy, kx, W, r, preact=kz, activation=act)
+    g64, x64 = g.double(), _value(kx)
+    far = S * 2.0 ** -38 * float(g64.abs().max() * x64.abs().max()) * 1.01
+
+    def check(dw, ge, xe):   # (g unrounded: 2^-8 of the returned one)
+        want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+        _close(dw, want, HALF * 1.01 * want.abs() + (HALF * 1.01 + 2.0 ** -10 + S * 2.0 ** -24) * mag + far)
+    assert float(g64.abs().max()) < 2.0 ** 10     # (what the slopes leave)
+    for e, rows, t in _parts(r):
+        check(dw[e], g64[rows], x64[t])
+    if E == 1:
+        _, dw, g, _ = ffe.linear_backward(dy, kx, W[0], preact=kz, activation=act)
+        check(dw, g.double(), x64)
