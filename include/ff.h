@@ -674,7 +674,8 @@ ff_status ff_expert_combine(const ff_expert_combine_args* args);
 
 /* Its gradient (the residual's is dout itself): dy of a row is its weight times dout of its token
  * (fp32: it is rounded once, as part of g; zeros for rows in no expert), dweights_tj =
- * <dout_t, y[place_tj]> (0 where there is no row).  Reads all of the routing. */
+ * <dout_t, y[place_tj]> (0 where there is no row of an expert that order says is the slot's).  Reads all of
+ * the routing. */
 typedef struct {
   ff_routing routing;
   int64_t cols;             /* <= 2^20 */

@@ -237,16 +237,21 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a, uint32_t per_row
   }
 }
 
-// A wave a row: the row's gradient and its weight's (2042 rows of 333: 6.3 us, latency).  The wave of number p also
-// clears the weight's gradient of slot p where that is in no row.
+// A wave a row: the row's gradient and its weight's (2042 rows of 333: 6.3 us, latency).  A slot is in a row of an
+// expert where place and order name each other: the wave of that row writes its weight's gradient, and
+// the wave of number p zero for slot p where there is no such row, so that each is written once.
 __global__ __launch_bounds__(256) void k_combine_grad(CombineGradArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t used = used_rows(a.at);
   for (int64_t p = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); p < a.at.rows; p += (int64_t)gridDim.x * 4) {
-    const int32_t place = a.at.place[p];
-    if (a.dweights != nullptr && lane == 0 && (place < 0 || place >= a.at.rows)) a.dweights[p] = 0.0f;
     const int32_t slot = p < used ? a.at.order[p] : -1;
     const bool live = slot >= 0 && slot < a.at.rows;
+    bool own = false;
+    if (a.dweights != nullptr && lane == 0) {
+      const int32_t place = a.at.place[p];
+      if (place < 0 || place >= used || a.at.order[place] != p) a.dweights[p] = 0.0f;
+      own = live && a.at.place[slot] == p;
+    }
     const int64_t t = live ? slot / a.at.top : 0;
     const float w = live ? a.at.weights[slot] : 0.0f;
     float dot = 0.0f;
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(CombineGradArgs a) {
     if (a.dweights != nullptr && live) {
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-      if (lane == 0) a.dweights[slot] = dot;
+      if (own) a.dweights[slot] = dot;
     }
   }
 }

@@ -204,3 +204,49 @@ def test_weight_gradient_beside_units_that_are_off(gpu, T, E, top, n, m, act, of
     if E == 1:
         _, dw, g, _ = ffe.linear_backward(dy, kx, W[0], preact=kz, activation=act)
         check(dw, g.double(), x64)
+
+
+def _combine_gradient(r, dout, y):
+    """(dy, dweights) by the C ABI, among rows and numbers that stay as they were."""
+    S, m, dev = y.shape[0], y.shape[1], y.device
+    dy, dw = torch.full((S + 4, m), 7.0, device=dev), torch.full((S + 64,), 7.0, device=dev)
+    X._library()
+    a = X.ff_expert_combine_grad_args(X._routing(r, dev), m, dout.data_ptr(), m, y.data_ptr(), m, dy[2:].data_ptr(), m,
+                                      dw[32:].data_ptr())
+    X._launch("ff_expert_combine_backward", a, dev, X._FN)
+    assert bool((dy[:2] == 7.0).all()) and bool((dy[-2:] == 7.0).all())
+    assert bool((dw[:32] == 7.0).all()) and bool((dw[-32:] == 7.0).all())
+    return dy[2:-2], dw[32:-32].view(-1, r.experts.shape[1])
+
+
+def test_weights_gradient_of_wrong_routings(gpu):
+    """Arrays that are no routing: every weight's gradient is written, zero where order and place do not
+    name each other, and dy's rows by order."""
+    T, E, top, m = 150, 5, 2, 72
+    r = _routing(gpu, T, E, top, 0.1)
+    S, big = T * top, 2 ** 31 - 1
+    dout, y = _rand(gpu, T, m), _rand(gpu, S, m, seed=1)
+    order, place, turned = r.order.clone(), r.place.clone(), r.order.clone()
+    order[::3], order[1::7], order[2::11] = big, -big, S
+    place[::3], place[1::5], place[2::9] = big, -5, S
+    turned[40:60] = turned[40:60].flip(0)
+    twice = r.place.clone()
+    twice[:, 1] = twice[:, 0]
+    bad = [r, r._replace(order=order), r._replace(place=place), r._replace(order=order, place=place), r._replace(order=turned),
+           r._replace(place=twice)]
+    for o in ([0, 3, 9, 20, 40, 50], [0, 10, 20, 30, 40, 0], [0, big, 3, -4, big, 7], [-1] * 6, [0, 300, 0, 300, 0, 290]):
+        bad.append(r._replace(offsets=torch.tensor(o, dtype=torch.int32, device=gpu)))
+    for q in bad:
+        used = min(max(int(q.offsets[-1]), 0), S)
+        dy, dw = _combine_gradient(q, dout, y)
+        o, p = q.order.cpu().long(), q.place.cpu().long().reshape(-1)
+        d64, y64, w = dout.double().cpu(), y.double().cpu(), q.weights.double().cpu().reshape(-1)
+        rows, mag, want = torch.zeros(S, m).double(), torch.zeros(S).double(), torch.zeros(S).double()
+        for k in range(S):
+            if k < used and 0 <= int(o[k]) < S:
+                rows[k] = w[o[k]] * d64[o[k] // top]
+            if 0 <= int(p[k]) < used and int(o[p[k]]) == k:
+                terms = d64[k // top] * y64[p[k]]
+                want[k], mag[k] = terms.sum(), terms.abs().sum()
+        _close(dw.cpu().reshape(-1), want, (m + 1) * 2.0 ** -24 * mag)
+        _close(dy.cpu(), rows, 2.0 ** -24 * rows.abs())
