@@ -557,9 +557,10 @@ ff_status ff_linear_backward_q8(const ff_linear_grad_q8_args* args);
 /* ---- Layers of experts ----
  * Each of `tokens` tokens takes `top` of `experts` experts: slot s = t top + j is token t's
  * j-th choice.  The products work on rows, one for each slot, sorted by expert and by
- * slot within one.  top <= 64, experts <= 1024, tokens top <= 2^24.  What the arrays of a
- * routing hold is not trusted: entries out of range are left out (no token's row, no
- * slot's row). */
+ * slot within one.  offsets may be a part of those that the rows are sorted by (experts lo .. hi - 1, with
+ * their weights): the other experts' rows are in no expert then.  top <= 64, experts <= 1024,
+ * tokens top <= 2^24.  What the arrays of a routing hold is not trusted: entries out of range are
+ * left out (no token's row, no slot's row). */
 typedef struct {
   int64_t tokens, experts, top;
   const float* weights;     /* tokens x top; where it is read, see below */

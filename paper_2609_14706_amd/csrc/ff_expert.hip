@@ -26,10 +26,18 @@ namespace {
 constexpr int kClearers = 16;  // workgroups there at least for rows in no expert
 
 __device__ __forceinline__ int64_t bounded(int32_t v, int64_t rows) { return v < 0 ? 0 : min((int64_t)v, rows); }
-// Rows of the batch that are in an expert, and an expert's: their number, and the first.
-__device__ __forceinline__ int64_t used_rows(const SlotRows& at) {
-  return at.offsets == nullptr ? at.rows : bounded(at.offsets[at.experts], at.rows);
+// Rows of the batch that are in an expert: lo .. hi - 1.  (lo is not 0 where the experts are some of those that the
+// rows are sorted by.)
+struct Used {
+  int64_t lo, hi;
+  __device__ __forceinline__ bool has(int64_t row) const { return row >= lo && row < hi; }
+};
+__device__ __forceinline__ Used used_rows(const SlotRows& at) {
+  if (at.offsets == nullptr) return {0, at.rows};
+  const int64_t lo = bounded(at.offsets[0], at.rows);
+  return {lo, max(lo, bounded(at.offsets[at.experts], at.rows))};
 }
+// An expert's rows: their number, and the first.
 __device__ __forceinline__ int64_t expert_rows(const SlotRows& at, int e, int64_t& first) {
   if (at.offsets == nullptr) {
     first = 0;
@@ -112,12 +120,15 @@ __device__ __forceinline__ bool find_tile(const SlotRows& at, int bm, uint32_t c
   return true;
 }
 
-// Rows in no expert, `bytes` each (a multiple of E's), are set to zeros.
+// Rows in no expert, of `cols` elements, `ld` apart, are set to zeros.
 template <class E>
 __device__ __forceinline__ void clear_rows(const SlotRows& at, E* p, int64_t ld, int64_t cols, uint32_t extra,
                                            uint32_t extras) {
-  for (int64_t r = used_rows(at) + extra; r < at.rows; r += extras)
+  const Used used = used_rows(at);
+  for (int64_t i = extra; i < used.lo + at.rows - used.hi; i += extras) {
+    const int64_t r = i < used.lo ? i : i - used.lo + used.hi;
     for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) p[r * ld + c] = E(0);
+  }
 }
 
 // The arguments of expert e's rows.
@@ -242,14 +253,14 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a, uint32_t per_row
 // the wave of number p zero for slot p where there is no such row, so that each is written once.
 __global__ __launch_bounds__(256) void k_combine_grad(CombineGradArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t used = used_rows(a.at);
+  const Used used = used_rows(a.at);
   for (int64_t p = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); p < a.at.rows; p += (int64_t)gridDim.x * 4) {
-    const int32_t slot = p < used ? a.at.order[p] : -1;
+    const int32_t slot = used.has(p) ? a.at.order[p] : -1;
     const bool live = slot >= 0 && slot < a.at.rows;
     bool own = false;
     if (a.dweights != nullptr && lane == 0) {
       const int32_t place = a.at.place[p];
-      if (place < 0 || place >= used || a.at.order[place] != p) a.dweights[p] = 0.0f;
+      if (!used.has(place) || a.at.order[place] != p) a.dweights[p] = 0.0f;
       own = live && a.at.place[slot] == p;
     }
     const int64_t t = live ? slot / a.at.top : 0;
@@ -414,7 +425,8 @@ __device__ __forceinline__ uint32_t peak_bits(const RowsArgs& a, int64_t block, 
   constexpr int N = Vec<E>::N, U = 2;  // (4: as fast for large arrays, 5.5 us instead of 4.6 for 1021 x 777)
   uint32_t big = 0;
   const uint32_t per_row = (uint32_t)((a.cols + N - 1) / N);
-  const int64_t rows = used_rows(a.at), total = rows * per_row;
+  const Used used = used_rows(a.at);
+  const int64_t total = (used.hi - used.lo) * per_row;
   for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
     const int64_t r = b / per_row;
     Vec<E> v[U];
@@ -422,9 +434,9 @@ __device__ __forceinline__ uint32_t peak_bits(const RowsArgs& a, int64_t block, 
     for (int u = 0; u < U; ++u) {
       const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
       const int64_t col = (int64_t)(c % per_row) * N;
-      int64_t row = r + c / per_row;
+      int64_t row = used.lo + r + c / per_row;
       v[u].w = u32x4{0, 0, 0, 0};
-      if (row < rows && (!a.gather || (row = token_of(a.at, row)) >= 0))
+      if (row < used.hi && (!a.gather || (row = token_of(a.at, row)) >= 0))
         v[u] = load_row((const E*)a.src + row * a.lds + col, a.cols - col);
     }
 #pragma unroll
@@ -443,7 +455,8 @@ __device__ __forceinline__ uint32_t peak_bits_of_g(const RowsArgs& a, int64_t bl
   constexpr int U = 2;
   uint32_t big = 0;
   const uint32_t per_row = (uint32_t)((a.cols + 7) / 8);
-  const int64_t rows = used_rows(a.at), total = rows * per_row;
+  const Used used = used_rows(a.at);
+  const int64_t total = (used.hi - used.lo) * per_row;
   for (int64_t b = block * (256 * U); b < total; b += blocks * (256 * U)) {
     const int64_t r = b / per_row;
     int64_t row[U], col[U];
@@ -451,9 +464,9 @@ __device__ __forceinline__ uint32_t peak_bits_of_g(const RowsArgs& a, int64_t bl
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t c = (uint32_t)(b - r * per_row) + u * 256 + threadIdx.x;
-      row[u] = r + c / per_row;
+      row[u] = used.lo + r + c / per_row;
       col[u] = (int64_t)(c % per_row) * 8;
-      count[u] = row[u] < rows ? (int)min((int64_t)8, a.cols - col[u]) : 0;
+      count[u] = row[u] < used.hi ? (int)min((int64_t)8, a.cols - col[u]) : 0;
     }
     float f[U][8];
     load_pieces<true>(a, row, col, count, f);
@@ -579,7 +592,8 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
     }
     return;
   }
-  const int64_t total = a.at.rows * per_row, used = used_rows(a.at);
+  const int64_t total = a.at.rows * per_row;
+  const Used used = used_rows(a.at);
   constexpr int U = 2;
   for (int64_t b = (int64_t)w * (256 * U); b < total; b += (int64_t)blocks * (256 * U)) {
     const int64_t r = b / per_row;
@@ -592,7 +606,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
       row[u] = r + c / per_row;
       col[u] = (int64_t)(c % per_row) * 8;
       count[u] = row[u] < a.at.rows ? (int)min((int64_t)8, a.cols - col[u]) : 0;
-      have[u] = row[u] < used ? count[u] : 0;
+      have[u] = used.has(row[u]) ? count[u] : 0;
     }
     load_pieces<ONCE>(a, row, col, have, f);
 #pragma unroll

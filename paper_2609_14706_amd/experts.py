@@ -27,7 +27,9 @@ SCORES = {"softmax": FF_SCORE_SOFTMAX, "sigmoid": FF_SCORE_SIGMOID}
 class Routing(NamedTuple):
     """Which experts T tokens take and where their slots lie: weights (T, top)
     float32 (None: no weights), experts (T, top), order (T top), offsets (E + 1)
-    and place (T, top) int32; see route."""
+    and place (T, top) int32; see route.  With offsets[a : b + 1] for offsets (and
+    their weights) the products take experts a .. b - 1 alone: rows of the others are
+    in no expert."""
     weights: Optional[torch.Tensor]
     experts: torch.Tensor
     order: torch.Tensor

@@ -250,3 +250,89 @@ def test_weights_gradient_of_wrong_routings(gpu):
                 want[k], mag[k] = terms.sum(), terms.abs().sum()
         _close(dw.cpu().reshape(-1), want, (m + 1) * 2.0 ** -24 * mag)
         _close(dy.cpu(), rows, 2.0 ** -24 * rows.abs())
+
+
+def _dirty(gpu, *tensors):
+    """Leaves NaN in the memory that tensors like these are made of next."""
+    gone = [torch.full_like(t, math.nan) for t in tensors for _ in range(2)]
+    del gone
+
+
+@pytest.mark.parametrize("lo,hi", [(2, 5), (0, 4), (3, 7), (4, 5)])
+@pytest.mark.parametrize("T,top,n,m", [(9, 2, 64, 40), (40, 3, 250, 77), (700, 2, 200, 333), (1500, 2, 520, 1032), (2500, 3, 1032, 1288)])
+def test_some_of_the_experts(gpu, T, top, n, m, lo, hi):
+    """offsets and weights of neighbouring experts alone, as a program has them that spreads its experts: the
+    others' rows are in no expert, before the first one's as well as behind the last."""
+    S = T * top
+    r = _routing(gpu, T, 7, top, 0.1)
+    q = r._replace(offsets=r.offsets[lo:hi + 1])
+    a, b = int(q.offsets[0]), int(q.offsets[-1])
+    out = torch.ones(S, dtype=torch.bool, device=gpu)
+    out[a:b] = False
+    W, bias = _rand(gpu, hi - lo, m, n, seed=1, scale=1 / math.sqrt(n)), _rand(gpu, hi - lo, m, seed=2)
+    W64, b64 = W.double(), bias.double()
+    z, dy = _rand(gpu, S, m, seed=3), _rand(gpu, S, m, seed=4)
+    dy[out] = math.nan
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device=gpu)
+
+    def zeros(*shape):
+        return torch.zeros(shape, dtype=torch.float64, device=gpu)
+    for by_slot in (False, True):
+        x = _rand(gpu, S if by_slot else T, n, seed=5)
+        _dirty(gpu, dy)
+        ws.fill_(255)
+        y, pre = ffe.expert_linear(x, W, q, bias=bias, activation="relu", keep_preact=True, by_slot=by_slot, workspace=ws)
+        assert not bool(y[out].any()) and not bool(pre[out].any())
+        assert torch.equal(y, torch.where(pre > 0, pre, torch.zeros_like(pre)))
+        for e, rows, t in _parts(q):
+            xe = x[rows if by_slot else t].double()
+            want, mag = xe @ W64[e].T + b64[e], xe.abs() @ W64[e].abs().T + b64[e].abs()
+            _close(pre[rows], want, HALF * 1.01 * want.abs() + (n + 1) * 2.0 ** -24 * mag)
+        if by_slot:
+            x[out] = 1e30
+        for kept in (x, ffe.checkpoint_q8(x)):
+            x64 = x.double() if kept is x else _value(kept)
+            _dirty(gpu, dy, x, W, bias)
+            ws.fill_(255)
+            dx, dw, g, db = ffe.expert_linear_backward(dy, kept, W, q, preact=z, activation="relu", by_slot=by_slot, workspace=ws)
+            assert torch.equal(g, torch.where(out[:, None] | (z <= 0), torch.zeros_like(dy), dy))
+            g64 = g.double()
+            far = S * 2.0 ** -38 * float(g64.abs().max() * (x64[a:b] if by_slot else x64).abs().max()) if b > a else 0.0
+            rows_x, mags_x = zeros(S + 1, n), zeros(S + 1, n)
+            ww, mw, wb, mb = zeros(*W.shape), zeros(*W.shape), zeros(hi - lo, m), zeros(hi - lo, m)
+            for e, rows, t in _parts(q):
+                ge, xe = g64[rows], x64[rows if by_slot else t]
+                rows_x[rows], mags_x[rows] = ge @ W64[e], ge.abs() @ W64[e].abs()
+                ww[e], mw[e], wb[e], mb[e] = ge.T @ xe, ge.abs().T @ xe.abs(), ge.sum(0), ge.abs().sum(0)
+            if by_slot:
+                assert not bool(dx[out].any())
+                want, mag = rows_x[:S], mags_x[:S]
+            else:   # (-1, no row: the zeros at the end)
+                want, mag = rows_x[r.place.long()].sum(1), mags_x[r.place.long()].sum(1)
+            _close(dx, want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
+            _close(db, wb, HALF * 1.01 * wb.abs() + S * 2.0 ** -24 * mb)
+            extra = 0 if kept is x else 2.0 ** -9 * mw + far
+            _close(dw, ww, HALF * 1.01 * ww.abs() + S * 2.0 ** -24 * mw + extra)
+    # the sums' gradient: of all rows and of these
+    dout, y = _rand(gpu, T, m, seed=6), _rand(gpu, S, m, seed=7)
+    (dyp, dwp), (dyf, dwf) = _combine_gradient(q, dout, y), _combine_gradient(r, dout, y)
+    assert torch.equal(dyp, torch.where(out[:, None], torch.zeros_like(dyf), dyf))
+    here = (r.place >= a) & (r.place < b)
+    assert torch.equal(dwp, torch.where(here, dwf, torch.zeros_like(dwf)))
+
+
+def test_rows_before_the_first_expert_do_not_count(gpu):
+    """Numbers in rows before the first expert's do not set the powers of two around fp16."""
+    T, E, n, m = 400, 4, 72, 40
+    r = _routing(gpu, T, E, 1)
+    q = r._replace(offsets=r.offsets[2:])
+    a = int(q.offsets[0])
+    assert a > 0
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T, m, seed=1), _rand(gpu, 2, m, n, seed=2)
+    z = _rand(gpu, T, m, seed=3)
+    x2, dy2 = x.clone(), dy.clone()
+    x2[:a], dy2[:a] = 1e30, -1e35
+    for kw in ({}, dict(preact=z, activation="silu"), dict(preact=ffe.checkpoint_q8(z), activation="gelu")):
+        want = ffe.expert_linear_backward(dy, ffe.checkpoint_q8(x), W, q, by_slot=True, **kw)
+        got = ffe.expert_linear_backward(dy2, ffe.checkpoint_q8(x2), W, q, by_slot=True, **kw)
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
