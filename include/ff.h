@@ -518,7 +518,8 @@ ff_status ff_linear_backward(const ff_linear_grad_args* args);
 
 /* 8-bit checkpoints of activations: rows x cols in groups of columns with a scale each,
  *     scale = max |x| / 127 over the group,  q = rint(127 x / max |x|),  back: x' = q scale
- * (x' is off by at most half a scale).  A group that is not finite gets a NaN scale and
+ * (x' is off by at most half a scale; in a group whose largest is fp32's largest number q = 127 stands for the
+ * number below it, not for infinity).  A group that is not finite gets a NaN scale and
  * zero codes, one whose largest magnitude is below 2^-118 a zero scale and zero codes.
  * A group is 16, 32, 64, 128, 256 or 512 columns; a row's last one may be shorter. */
 typedef struct {

@@ -336,3 +336,31 @@ def test_rows_before_the_first_expert_do_not_count(gpu):
         want = ffe.expert_linear_backward(dy, ffe.checkpoint_q8(x), W, q, by_slot=True, **kw)
         got = ffe.expert_linear_backward(dy2, ffe.checkpoint_q8(x2), W, q, by_slot=True, **kw)
         assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
+def test_checkpoint_of_the_largest_number(gpu):
+    """The one group whose scale times 127 leaves fp32: that of its largest number, which a mask may have put
+    there.  Restored it is within half a scale, as any other, and dW of it is finite."""
+    most = torch.finfo(F32).max
+    x = _rand(gpu, 40, 96, dtype=F32)
+    x[0, 3], x[1, 20], x[2] = most, -most, most
+    x[3, 40] = float(torch.nextafter(torch.tensor(most), torch.tensor(0.0)))
+    kept = ffe.checkpoint_q8(x, group=16)
+    back = ffe.checkpoint_restore(kept, dtype=F32)
+    assert bool(torch.isfinite(back).all())
+    scale = torch.repeat_interleave(kept.scale.double(), 16, dim=1)
+    # half a scale, and the scale's and the product's roundings and the step down: 127 times 2^-24, 2^-24 and 2^-23
+    assert bool(((back.double() - x.double()).abs() <= scale * (0.5 + 127 * 2.0 ** -22)).all())
+    assert float(back[0, 3]) == -float(back[1, 20]) and abs(float(back[0, 3]) / most - 1) <= 2.0 ** -22
+    dy = torch.zeros((40, 24), dtype=BF16, device=gpu)
+    dy[0], dy[1] = 2.0 ** -20, 2.0 ** -21
+    dw = ffe.linear_backward(dy, kept, torch.zeros((24, 96), dtype=BF16, device=gpu), need_input=False)[1]
+    want = dy.double().T @ x.double()
+    assert bool(torch.isfinite(dw).all())
+    _close(dw[:, 3], want[:, 3], 2 * HALF * want[:, 3].abs())
+    _close(dw[:, 20], want[:, 20], 2 * HALF * want[:, 20].abs())
+    # NaN and infinite scales stay what they are
+    odd = ffe.Checkpoint(kept.codes, kept.scale.clone(), 16)
+    odd.scale[5, 0], odd.scale[6, 0] = math.nan, math.inf
+    back = ffe.checkpoint_restore(odd, dtype=F32)
+    assert bool(back[5, :16].isnan().all()) and not bool(torch.isfinite(back[6, :16]).any())
