@@ -29,10 +29,5 @@ __device__ __forceinline__ void values_of(const uint32_t (&w)[2], float scale, f
 #pragma unroll
   for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4))) * scale;
 }
-__device__ __forceinline__ void load_q8(const Q8Rows& a, int64_t row, int64_t col, int count, float (&f)[8]) {
-  uint32_t w[2];
-  load_codes(a.q + row * a.ldq + col, count, w);
-  values_of(w, a.scale[row * a.lds + (col >> a.shift)], f);
-}
 
 }  // namespace ff

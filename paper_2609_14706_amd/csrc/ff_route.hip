@@ -63,7 +63,7 @@ __device__ __forceinline__ u64 key_of(double c) {
 }
 
 // The lane that holds the largest of the lanes' keys, the lowest one among equals
-// (lanes hold ascending experts); largest: its key.
+// (lanes hold ascending experts).
 __device__ __forceinline__ int best_lane(u64 mine) {
   const uint32_t hi = (uint32_t)(mine >> 32), top = wave_max(hi);
   u64 who = __ballot(hi == top);

@@ -331,16 +331,6 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   }
-
-  // A lane's row of C within the tile for i, and the first of its four columns for j.
-  static __device__ __forceinline__ int row_of(int i) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    return (wave >> 1) * 16 * TI + i * 16 + (lane & 15);
-  }
-  static __device__ __forceinline__ int col_of(int j) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    return (wave & 1) * 16 * TJ + j * 16 + 4 * (lane >> 4);
-  }
 };
 
 }  // namespace kn
