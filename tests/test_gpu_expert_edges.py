@@ -364,3 +364,64 @@ def test_checkpoint_of_the_largest_number(gpu):
     odd.scale[5, 0], odd.scale[6, 0] = math.nan, math.inf
     back = ffe.checkpoint_restore(odd, dtype=F32)
     assert bool(back[5, :16].isnan().all()) and not bool(torch.isfinite(back[6, :16]).any())
+
+
+class _Guarded:
+    """Tensors among numbers that have to stay as they were."""
+
+    def __init__(self, gpu):
+        self.gpu, self.all = gpu, []
+
+    def new(self, *shape, dtype=BF16):
+        n, pad = math.prod(shape), 4096
+        whole = torch.full((n + 2 * pad,), 7 if dtype is torch.uint8 else 7.0, dtype=dtype, device=self.gpu)
+        self.all.append(whole)
+        return whole[pad:pad + n].view(shape)
+
+    def check(self):
+        for whole in self.all:
+            assert bool((whole[:4096] == 7).all()) and bool((whole[-4096:] == 7).all())
+
+
+# tiles and streams of them, forms for few rows, ragged and whole
+@pytest.mark.parametrize("T,E,top,n,m", [(150, 5, 2, 64, 72), (20, 40, 2, 130, 77), (900, 3, 2, 264, 520), (1500, 2, 1, 1032, 2056)])
+def test_wrong_routings_write_nothing_else(gpu, T, E, top, n, m):
+    """Arrays that are no routing: outputs and workspaces are written, nothing around them."""
+    r, S, big = _routing(gpu, T, E, top, 0.1), T * top, 2 ** 31 - 1
+    order, place = r.order.clone(), r.place.clone()
+    order[::3], order[1::7], order[2::11] = big, -big, S
+    place[::3], place[1::5], place[2::9] = big, -5, S
+    g = torch.Generator().manual_seed(1)
+    bad = [r._replace(order=order), r._replace(place=place), r._replace(order=order, place=place)]
+    for o in ([big] * (E + 1), [-1] * (E + 1), [k % 2 * S for k in range(E + 1)], [(k + 1) % 2 * S for k in range(E + 1)],
+              torch.randint(-S, 2 * S, (E + 1,), generator=g).tolist()):
+        bad.append(r._replace(offsets=torch.tensor(o, dtype=torch.int32, device=gpu), order=order))
+    W, b, z = _rand(gpu, E, m, n, seed=1), _rand(gpu, E, m, seed=2), _rand(gpu, S, m, seed=3)
+    for by_slot in (False, True):
+        x, dy = _rand(gpu, S if by_slot else T, n, seed=4), _rand(gpu, S, m, seed=5)
+        kx = ffe.checkpoint_q8(x)
+        X._library()
+        for q in bad:
+            at, mem = X._routing(q, x.device), _Guarded(gpu)
+
+            def run(name, a):
+                need = X._bytes(name + "_workspace_size", a, functions=X._FN)
+                X._workspace(a, need, mem.new(need + 255, dtype=torch.uint8) if need else None, x.device)
+                X._launch(name, a, x.device, X._FN)
+            y, pre = mem.new(S, m), mem.new(S, m)
+            run("ff_expert_linear", X.ff_expert_linear_args(at, n, m, x.data_ptr(), n, by_slot, W.data_ptr(), n, b.data_ptr(), 2,
+                                                            y.data_ptr(), m, pre.data_ptr(), m))
+            for kept in (x, kx):
+                a = X.ff_expert_grad_args()
+                a.routing, a.n, a.m, a.dy_dtype, a.dy, a.lddy, a.by_slot = at, n, m, X._elem(dy, "dy"), dy.data_ptr(), m, by_slot
+                if kept is x:
+                    a.x, a.ldx = x.data_ptr(), n
+                else:
+                    a.x_q8 = X._q8_rows(kx, "x", x.device)[0]
+                gr, dx, dw, db = mem.new(S, m), mem.new(*x.shape), mem.new(E, m, n), mem.new(E, m)
+                a.w, a.ldw, a.preact, a.ldz, a.activation, a.g, a.ldg = W.data_ptr(), n, z.data_ptr(), m, 3, gr.data_ptr(), m
+                a.dx, a.lddx, a.dw, a.lddw, a.db = dx.data_ptr(), n, dw.data_ptr(), n, db.data_ptr()
+                run("ff_expert_linear_backward", a)
+            out = mem.new(T, m)
+            X._launch("ff_expert_combine", X.ff_expert_combine_args(at, m, y.data_ptr(), m, None, 0, out.data_ptr(), m), x.device, X._FN)
+            mem.check()
