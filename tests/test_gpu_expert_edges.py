@@ -425,3 +425,24 @@ def test_wrong_routings_write_nothing_else(gpu, T, E, top, n, m):
             out = mem.new(T, m)
             X._launch("ff_expert_combine", X.ff_expert_combine_args(at, m, y.data_ptr(), m, None, 0, out.data_ptr(), m), x.device, X._FN)
             mem.check()
+
+
+@pytest.mark.parametrize("T,E,n,m", [(200, 3, 72, 40), (2000, 2, 1032, 2056)])
+def test_weight_gradient_of_wide_ranges(gpu, T, E, n, m):
+    """Columns of g, and of x, far below the largest: among fp16's last bits they count still."""
+    r = _routing(gpu, T, E, 1)
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T, m, seed=1), torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    dy[:, :8] *= 2.0 ** -20
+    dy[:, 8:16] *= 2.0 ** -32
+    x[:, :16] *= 2.0 ** -16
+    x[:, 16:32] *= 2.0 ** -31
+    kx = ffe.checkpoint_q8(x, group=16)
+    _, dw, g, _ = ffe.expert_linear_backward(dy, kx, W, r, need_input=False)
+    x64 = _value(kx)
+    for e, rows, t in _parts(r):
+        ge, xe = g[rows].double(), x64[t]
+        want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+        # 2^-38 of the largest g beside each x, and of the largest x (127 times the largest scale) beside each g
+        far = 2.0 ** -38 * (float(ge.abs().max()) * xe.abs().sum(0)[None] + ge.abs().sum(0)[:, None] * float(x64.abs().max()))
+        far = far + len(t) * 2.0 ** -76 * float(ge.abs().max() * x64.abs().max())
+        _close(dw[e], want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * 2.0 ** -24) * mag + far)
