@@ -1103,9 +1103,19 @@ ExpertPlan rows_plan(int64_t rows, int experts, int64_t k, int64_t cols, bool sp
                     row_tiles, cols, pairs, pairs, experts == 1, split, (double)rows * (double)cols);
 }
 
-ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m) {
+// The few-row form's 16 outputs a workgroup read x anew each time, and start for little where k is short; tiles
+// take as long for one row of an expert as for 64, and read W packed where it does not lie in whole 16 bytes.
+// us, few-row form and tiles: 4096 -> 2048, 8 experts of one row 33 and 39, of 12 rows 38 and 40, of 48 rows 75 and 42; 64
+// experts of one row 189 and 176, of 48 rows 536 and 187.  2048 -> 1408, 24 experts of 8 rows 35 and 43, 64 of 4 rows 67
+// and 83, of 12 rows 89 and 83.  1024 -> 1024, 24 of one row 14 and 14, 64 of one 33 and 26.  256 -> 2048, 24 of one
+// row 12 and 10, 128 of one 73 and 38.  Packed, 4095 -> 2048: 8 experts of 12 rows 72 and 86, of 24 rows 97 and 86; 64 of 12
+// rows 628 and 754, of 24 rows 878 and 766; 1001 -> 777: 8 of 24 rows 16 and 23, 64 of 24 rows 75 and 56.
+// 16-row tiles of it a workgroup, 2 experts, 4096 -> 2048: 16 rows by one 12.1 us, by two 12.0; 24 rows by one 18.4, by
+// two 14.7 and by four 14.7; 48 rows by two 25.6, by four 20.9.
+ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m, bool w_lies) {
   const int64_t active = std::min<int64_t>(experts, rows), each = (rows + active - 1) / active;
-  if (each <= 48) {
+  const bool little = rows * m <= (int64_t(1) << 18);
+  if (each <= 48 && (w_lies ? little && n > 512 : little || each <= 12)) {
     ExpertPlan p{};
     p.nt = each <= 12 ? 1 : each <= 24 ? 2 : 4;
     const int64_t groups = active * ((m + 15) / 16), steps = (n * 2 + 127) / 128;
@@ -1170,7 +1180,7 @@ hipError_t launch_combine_grad(const CombineGradArgs& a, hipStream_t s) {
 hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
   if (count < 1 || count > 3) return hipErrorInvalidValue;
   RowsJobs q{};
-  int64_t total = 0;
+  int64_t total = 0, numbers = 0;
   for (int k = 0; k < count; ++k) {
     const RowsArgs& a = jobs[k];
     // (rows that are no slots, those of all experts' weights, may be more than slots are)
@@ -1181,6 +1191,7 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
     if ((a.scaled != nullptr && a.inverse == nullptr) || (a.parts != nullptr && (k != 0 || (uintptr_t)a.parts % 16 != 0)))
       return hipErrorInvalidValue;
     const int64_t per_row = (a.cols + 7) / 8;
+    numbers += a.at.rows * a.cols;
     if (a.parts != nullptr) {
       q.part_rows = part_rows(a.at.rows, a.cols);
       int64_t across = 64;  // as k_rows has it
@@ -1194,9 +1205,10 @@ hipError_t launch_rows(const RowsArgs* jobs, int count, hipStream_t s) {
     q.end[k] = (uint32_t)total;
   }
   for (int k = count; k < 3; ++k) q.end[k] = (uint32_t)total;
-  // Few rows are bound by latency, many by memory, which more waves keep busy (1021 x 777 and x 1000 from checkpoints:
-  // 15.5 us with the activation decided once, 17.3 without; 4096 x 11008 and x 4096: 89 and 80)
-  if (jobs[0].at.rows * jobs[0].cols < (int64_t(1) << 22))
+  // Few numbers are bound by latency, many by memory, which more waves keep busy.  dW from checkpoints with the activation
+  // decided once and not: 1021 x 777 and x 1000 32.5 and 34.3 us, 2048 x 2048 and x 1024 51 and 59, 8192 x 2048 twice 135 and
+  // 140, 4096 x 11008 and x 4096 443 and 439; gradients of 64 experts 777 x 1001, whose weights are laid out, 105 and 93
+  if (numbers <= (int64_t(1) << 25))
     hipLaunchKernelGGL(k_rows<true>, dim3((uint32_t)total), dim3(256), 0, s, q);
   else
     hipLaunchKernelGGL(k_rows<false>, dim3((uint32_t)total), dim3(256), 0, s, q);
@@ -1230,8 +1242,10 @@ hipError_t launch_expert_dw(const ExpertGradArgs& a, const ExpertPlan& p, hipStr
   if (p.ti == I && p.tj == J && p.slots == S && p.splits == 1 && !a.out_f32)                                 \
     return a.f16 ? dw_stream<nt::F16, I, J, S>(a, s) : dw_stream<nt::Bf16, I, J, S>(a, s);
   FF_STREAM(8, 8, 2)
-  // (beyond two pairs the two workgroups of a unit hide each other's ends as well: 620 us, 599 without a stream)
-  if (a.at.rows <= 128 * (int64_t)a.at.experts) FF_STREAM(4, 4, 2)
+  // (with more pairs the two workgroups of a unit hide each other's ends as well: in a stream and without, 64 experts of
+  // 128 rows, 2048 x 1408, 147 and 162 us, of 256 rows 232 and 270, of 512 rows 380 and 401; 8 experts of 1024 rows
+  // 79.7 and 79.0, of 4096 rows 294 and 290; one of 4096 rows, 2048 x 2048, 71 and 67)
+  if (a.at.rows <= 512 * (int64_t)a.at.experts) FF_STREAM(4, 4, 2)
 #undef FF_STREAM
 #define FF_TILE(I, J, S)                       \
   if (p.ti == I && p.tj == J && p.slots == S)  \

@@ -77,7 +77,8 @@ struct ExpertPlan {
   int nt, waves;
   int ti, tj, slots, splits;
 };
-ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m);
+// w_lies: whether tiles can read the weights as they lie.
+ExpertPlan expert_plan(int64_t rows, int experts, int64_t n, int64_t m, bool w_lies);
 hipError_t launch_expert_linear(const ExpertArgs& a, const ExpertPlan& p, hipStream_t s);
 
 // out_t = residual_t + sum over the token's slots of weight y (rows of bf16), or the
@@ -139,7 +140,8 @@ struct RowsArgs {
                       // laid_ld(cols)); or null
 };
 // Rows of an expert that are summed together, and how many such sums there can be; expert e's
-// are those from offsets[e] / part_rows + e on.
+// are those from offsets[e] / part_rows + e on.  With 16 and 64 (g and db alone): 2042 rows of 333 17.3 and 23.5 us,
+// 1021 of 777 17.1 and 18.5, 1024 of 4096 the same, 4096 of 11008 45.7 and 38.3.
 inline int part_rows(int64_t rows, int64_t cols) { return rows * cols >= (int64_t(1) << 22) ? 64 : 16; }
 inline int64_t part_count(int64_t rows, int experts, int64_t cols) { return rows / part_rows(rows, cols) + experts + 1; }
 inline int64_t laid_ld(int64_t cols) { return (cols + 7) / 8 * 8; }

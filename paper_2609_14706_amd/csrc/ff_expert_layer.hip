@@ -154,9 +154,10 @@ struct ForwardWs {
 ForwardWs forward_ws(const ff_expert_linear_args* a) {
   ForwardWs w{};
   const int64_t T = a->routing.tokens, S = T * a->routing.top;
-  w.plan = expert_plan(S, (int)a->routing.experts, a->n, a->m);
+  const bool w_lies = tile_rows_ok(a->w, a->ldw, a->n, 2);
+  w.plan = expert_plan(S, (int)a->routing.experts, a->n, a->m, w_lies);
   if (w.plan.nt > 0) return w;
-  w.pack_w = !tile_rows_ok(a->w, a->ldw, a->n, 2);
+  w.pack_w = !w_lies;
   w.pack_x = !tile_rows_ok(a->x, a->ldx, a->n, 2);
   w.gather_x = a->by_slot == 0 && (T * (w.pack_x ? packed_ld(a->n, 2) : a->ldx) + a->n) * 2 > int64_t(0x7fffffff);
   if (w.gather_x) w.pack_x = false;

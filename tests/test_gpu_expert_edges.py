@@ -446,3 +446,42 @@ def test_weight_gradient_of_wide_ranges(gpu, T, E, n, m):
         far = 2.0 ** -38 * (float(ge.abs().max()) * xe.abs().sum(0)[None] + ge.abs().sum(0)[:, None] * float(x64.abs().max()))
         far = far + len(t) * 2.0 ** -76 * float(ge.abs().max() * x64.abs().max())
         _close(dw[e], want, HALF * 1.01 * want.abs() + (2.0 ** -9 + T * 2.0 ** -24) * mag + far)
+
+
+# tokens, experts, top, n, m: the form for few rows with one, two and four 16-row tiles a workgroup (k short and among
+# many waves), beside it tiles with few rows an expert; weights as they lie and packed
+@pytest.mark.parametrize("by_slot", [False, True])
+@pytest.mark.parametrize("T,E,top,n,m", [(1, 64, 8, 1000, 777), (13, 1, 1, 520, 35), (20, 3, 2, 4096, 130), (40, 1, 1, 600, 333),
+                                         (70, 4, 2, 1024, 1000), (30, 3, 2, 1001, 250), (100, 3, 1, 4097, 130), (8, 70, 5, 75, 2050),
+                                         (60, 64, 1, 1024, 4104), (37, 130, 7, 264, 520), (400, 24, 2, 520, 2056),
+                                         (9, 24, 8, 512, 777), (200, 16, 3, 1001, 900)])
+def test_few_rows_an_expert(gpu, T, E, top, n, m, by_slot):
+    for idle in (0.0, 0.5):
+        r = _routing(gpu, T, E, top, idle)
+        x, W, b = _rand(gpu, T * top if by_slot else T, n), _rand(gpu, E, m, n, seed=1, scale=0.05), _rand(gpu, E, m, seed=2)
+        y, z = ffe.expert_linear(x, W, r, bias=b, activation="relu", keep_preact=True, by_slot=by_slot)
+        used = int(r.offsets[-1])
+        assert not bool(y[used:].any()) and not bool(z[used:].any())
+        assert torch.equal(y, torch.where(z > 0, z, torch.zeros_like(z)))
+        for e, rows, t in _parts(r):
+            xe, we = x[rows if by_slot else t].double(), W[e].double()
+            want, mag = xe @ we.T + b[e].double(), xe.abs() @ we.abs().T + b[e].double().abs()
+            _close(z[rows], want, HALF * 1.01 * want.abs() + (n + 1) * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("T,E,n,m", [(140, 1, 1290, 2949), (859, 3, 2315, 1675), (1091, 2, 2572, 2315), (623, 1, 1774, 2308)])
+def test_weight_gradients_of_128_wide_tiles(gpu, T, E, n, m):
+    """In a stream up to 512 rows an expert, without one beyond."""
+    r = _routing(gpu, T, E, 1, 0.05)
+    x, dy, W = _rand(gpu, T, n), _rand(gpu, T, m, seed=1), torch.zeros((E, m, n), dtype=BF16, device=gpu)
+    kx = ffe.checkpoint_q8(x)
+    for kept in (x, kx):
+        _, dw, g, db = ffe.expert_linear_backward(dy, kept, W, r, need_input=False)
+        x64 = x.double() if kept is x else _value(kx)
+        far = 0.0 if kept is x else T * 2.0 ** -38 * float(dy.double().abs().max() * x64.abs().max())
+        for e, rows, t in _parts(r):
+            ge, xe = g[rows].double(), x64[t]
+            want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+            _close(dw[e], want, HALF * 1.01 * want.abs() + (T * 2.0 ** -24 + (0 if kept is x else 2.0 ** -9)) * mag + far)
+            want, mag = ge.sum(0), ge.abs().sum(0)
+            _close(db[e], want, HALF * 1.01 * want.abs() + T * 2.0 ** -24 * mag)
