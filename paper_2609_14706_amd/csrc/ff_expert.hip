@@ -332,7 +332,7 @@ struct RowsJobs {
 
 // Pieces of eight columns, `n` of them in their row (0: no such row, zeros), zeros beyond
 // them, times act'(z).  All of a kind's loads go out before the first is waited for.  ONCE: which
-// activation it is is decided once, not for each number; k_rows needs 91 registers so, 75 otherwise.
+// activation it is is decided once, not for each number; k_rows needs 92 registers so, 78 otherwise.
 template <bool ONCE, int U>
 __device__ __forceinline__ void load_pieces(const RowsArgs& a, const int64_t (&row)[U], const int64_t (&col)[U],
                                             const int (&n)[U], float (&f)[U][8]) {
@@ -525,7 +525,7 @@ __device__ __forceinline__ void store_piece(const RowsArgs& a, int64_t row, int6
 // The operands of the gradients' products: g = dy act'(z) as the caller's rows, as bf16 rows of whole
 // pieces and in fp16, and the sums of its columns; x and W as such rows.  All that a call needs are jobs of
 // one launch.  Bound by memory (16384 x 2048 and, gathered, 16384 x 4096 from checkpoints: 390 MB in 97 to
-// 106 us, 3.7 TB/s or more), small ones by latency (1021 x 777 and x 1000: 16 us).
+// 106 us, 3.7 TB/s or more), small ones by latency (1021 x 777 and x 1000: 15 us).
 template <bool ONCE>
 __global__ __launch_bounds__(256) void k_rows(RowsJobs jobs) {
   __shared__ uint32_t red[4];
