@@ -485,3 +485,98 @@ def test_weight_gradients_of_128_wide_tiles(gpu, T, E, n, m):
             _close(dw[e], want, HALF * 1.01 * want.abs() + (T * 2.0 ** -24 + (0 if kept is x else 2.0 ** -9)) * mag + far)
             want, mag = ge.sum(0), ge.abs().sum(0)
             _close(db[e], want, HALF * 1.01 * want.abs() + T * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,dtype", [(7, F32), (61, BF16), (300, F32), (1000, BF16)])
+def test_route_gradient_in_place(gpu, E, dtype, score):
+    """dlogits as the logits' own rows, which lie apart."""
+    T, top = 333, 4
+    wide = _rand(gpu, T, E + 5, scale=2.0, dtype=dtype)
+    logits, before = wide[:, 2:2 + E], wide.clone()
+    r = ffe.route(logits, top, score=score)
+    dw = _rand(gpu, T, top, seed=1, dtype=F32)
+    want = ffe.route_backward(dw, logits, r.experts, score=score)
+    X._library()
+    a = X.ff_route_grad_args(T, E, top, X._elem(logits, "logits"), logits.data_ptr(), E + 5, dw.data_ptr(), r.experts.data_ptr(),
+                             X.SCORES[score], 1, 1.0, logits.data_ptr(), E + 5)
+    X._launch("ff_route_backward", a, wide.device, X._FN)
+    assert torch.equal(logits, want)
+    assert torch.equal(wide[:, :2], before[:, :2]) and torch.equal(wide[:, 2 + E:], before[:, 2 + E:])
+
+
+def test_sums_onto_the_residual(gpu):
+    """out as the residual's own rows."""
+    T, E, top, m = 200, 5, 3, 133
+    r = _routing(gpu, T, E, top, 0.2)
+    y, wide = _rand(gpu, T * top, m), _rand(gpu, T, m + 7, seed=1)
+    out, before = wide[:, 3:3 + m], wide.clone()
+    want = ffe.expert_combine(y, r, residual=out)
+    X._library()
+    a = X.ff_expert_combine_args(X._routing(r, y.device), m, y.data_ptr(), m, out.data_ptr(), m + 7, out.data_ptr(), m + 7)
+    X._launch("ff_expert_combine", a, y.device, X._FN)
+    assert torch.equal(out, want)
+    assert torch.equal(wide[:, :3], before[:, :3]) and torch.equal(wide[:, 3 + m:], before[:, 3 + m:])
+
+
+def test_most_slots(gpu):
+    """2^24 slots, the most that are taken: their order is the stable sort by expert."""
+    T, E, top = 1 << 22, 9, 4
+    logits = torch.randn((T, E), device=gpu, generator=torch.Generator(device=gpu).manual_seed(1))
+    r = ffe.route(logits, top)
+    assert torch.equal(r.experts.long(), torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :top])
+    key = r.experts.reshape(-1)
+    order = torch.sort(key, stable=True).indices
+    place = torch.empty_like(order)
+    place[order] = torch.arange(T * top, device=gpu)
+    assert torch.equal(r.order.long(), order) and torch.equal(r.place.long().reshape(-1), place)
+    assert r.offsets.tolist() == [int((key < e).sum()) for e in range(E + 1)]
+    with pytest.raises(ffe.FlipFlopError):
+        ffe.expert_order(torch.zeros((T + 1, top), dtype=torch.int32, device=gpu), E)
+
+
+@pytest.mark.parametrize("top", [1, 2])
+def test_results_of_more_than_2_31_numbers(gpu, top):
+    """Rows, codes and gradients whose offsets do not fit 32 bits: the last rows, and sums over all."""
+    T, E, n, m = (1 << 18) // top, 2, 64, 8264
+    S = T * top
+    assert S * m > 1 << 31
+    r = _routing(gpu, T, E, top)
+    g = torch.Generator(device=gpu).manual_seed(2)
+    x, W = _rand(gpu, T, n), _rand(gpu, E, m, n, seed=1, scale=0.1)
+    y, _ = ffe.expert_linear(x, W, r)
+    tokens = r.order.long() // top
+    starts = r.offsets.tolist()
+    rows = torch.tensor([0, 1, starts[1] - 1, starts[1], S // 2, S - 2, S - 1], device=gpu)
+    experts = (rows >= starts[1]).long()
+    want = torch.einsum("rn,rmn->rm", x[tokens[rows]].double(), W[experts].double())
+    mag = torch.einsum("rn,rmn->rm", x[tokens[rows]].double().abs(), W[experts].double().abs())
+    _close(y[rows], want, HALF * 1.01 * want.abs() + n * 2.0 ** -24 * mag)
+    # the checkpoint of them, back, and as pre-activations
+    kept = ffe.checkpoint_q8(y, group=256)
+    some = ffe.checkpoint_q8(y[rows].contiguous(), group=256)
+    assert torch.equal(kept.codes[rows], some.codes) and torch.equal(kept.scale[rows], some.scale)
+    back = ffe.checkpoint_restore(kept)
+    assert torch.equal(back[rows], ffe.checkpoint_restore(some))
+    del back
+    dy = torch.empty((S, m), dtype=BF16, device=gpu).normal_(generator=g)
+    dx, dw, gr, db = ffe.expert_linear_backward(dy, x, W, r, preact=kept, activation="relu")
+    assert torch.equal(gr[rows], torch.where(some.codes > 0, dy[rows], torch.zeros_like(dy[rows])))
+    out = ffe.expert_combine(y, r)
+    last = torch.tensor([0, T - 1], device=gpu)
+    at = r.place[last].long()
+    terms = r.weights[last].double()[:, :, None] * y[at].double()
+    want = terms.sum(1)
+    _close(out[last], want, HALF * 1.01 * want.abs() + (top + 1) * 2.0 ** -24 * terms.abs().sum(1))
+    del y, out, dy, kept
+    W64 = W.double()
+    of = (at >= starts[1]).long()
+    want = sum(torch.einsum("tm,tmn->tn", gr[at[:, j]].double(), W64[of[:, j]]) for j in range(top))
+    mag = sum(torch.einsum("tm,tmn->tn", gr[at[:, j]].double().abs(), W64[of[:, j]].abs()) for j in range(top))
+    _close(dx[last], want, HALF * 1.01 * want.abs() + (m + top) * 2.0 ** -24 * mag)
+    for e, part, t in _parts(r):
+        cols = torch.tensor([0, m // 2, m - 1], device=gpu)
+        ge, xe = gr[part][:, cols].double(), x[t].double()
+        want, mag = ge.T @ xe, ge.abs().T @ xe.abs()
+        _close(dw[e][cols], want, HALF * 1.01 * want.abs() + S * 2.0 ** -24 * mag)
+        _close(db[e][cols], ge.sum(0), HALF * 1.01 * ge.sum(0).abs() + S * 2.0 ** -24 * ge.abs().sum(0))
